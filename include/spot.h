@@ -616,6 +616,232 @@ spot_status spot_sparse_prefill(const void *q, const void *k, const void *v, int
                                 int h_q, int h_kv, int d, float sm_scale, void *out, float *lse,
                                 void *stream);
 
+/* ------------------------------------------------------------------------
+ * Operators on a paged cache.
+ *
+ * Keys and values of a layer lie in two pools of pages, each page
+ * [h_kv, page_size, d]: k_pages and v_pages are [n_pages, h_kv, page_size, d], and
+ * token t of sequence s lies in page page_table[s, t / page_size] at offset
+ * t % page_size.  page_size is a multiple of 16.  (A contiguous cache
+ * [batch, h_kv, l_cap, d] is a pool of batch pages of l_cap tokens.)  A token whose
+ * page id lies outside [0, n_pages), or which lies at or past max_pages *
+ * page_size, is not there: it is neither read nor written nor seen.
+ *
+ * A call takes the new tokens of n_seq sequences packed one after the other, one
+ * row each: sequence s owns rows [seq_start[s], seq_start[s + 1]) of the `rows`
+ * rows, n_s of them (none, one in a decode step, a chunk, a whole prompt), and
+ * seq_len[s] counts its tokens with the new ones, so row i of the sequence is
+ * token (and position) p = seq_len[s] - n_s + i of the cache.  seq_start is
+ * ascending; its values are clamped to [0, rows] and a negative seq_len to 0.
+ * Rows before seq_start[0] and from seq_start[n_seq] on belong to no sequence:
+ * their outputs are left as they were.  The lengths are read on the device only,
+ * so a captured call may be replayed with others in place.
+ *
+ * Element types: SPOT_DTYPE_BF16 or SPOT_DTYPE_FP16, the same for every array of a
+ * call that has no other type given.  Arrays of no rows (rows = 0) or no sequences
+ * may be NULL.  Limits: max_pages * page_size <= 2^30,
+ * n_pages * h_kv * page_size < 2^31, rows * h_q < 2^31 (SPOT_ERR_SHAPE).
+ */
+#define SPOT_DTYPE_BF16 0
+#define SPOT_DTYPE_FP16 1
+
+/* Scaling of rotary frequencies for contexts longer than the trained one. */
+#define SPOT_ROPE_NONE 0
+#define SPOT_ROPE_LINEAR 1 /* f / factor                                               */
+#define SPOT_ROPE_BASE 2   /* base * factor^(r / (r - 2)) for base, r = rope_dim > 2     */
+#define SPOT_ROPE_PARTS 3  /* by parts: f where a pair turns more than `high` times over */
+                           /* orig_len tokens, f / factor below `low` times, and between */
+                           /* them g f + (1 - g) f / factor with                         */
+                           /* g = (orig_len f / (2 pi) - low) / (high - low)             */
+
+/* Flags of the rotations. */
+#define SPOT_ROPE_INTERLEAVED 1 /* pairs (2i, 2i + 1) instead of (i, i + rope_dim / 2) */
+#define SPOT_ROPE_INVERSE 2     /* by the negative angle: undoes a rotation (times amp), */
+                                /* and takes the gradient of a rotation's output to that */
+                                /* of its input                                          */
+
+/*
+ * spot_rope_frequencies -- rotary frequencies of the pairs of a head, on the host.
+ *
+ * Table 1 of the paper extends contexts beyond 32K tokens by YaRN with factor 16;
+ * Appendix A rotates part of each head.  Frequency i of rope_dim / 2 is
+ * f_i = rope_base^(-2i / rope_dim), scaled as the constants above say.  YaRN is
+ * SPOT_ROPE_PARTS with low = 1, high = 32 and, in the rotations, the factor
+ * amp = 0.1 ln(factor) + 1.
+ *
+ *  freq   host double [rope_dim / 2] (output; may be NULL where rope_dim is 0)
+ *
+ * rope_dim even, 0 <= rope_dim <= 256; rope_base finite and > 0; with a scaling,
+ * factor finite and >= 1; for SPOT_ROPE_PARTS orig_len >= 1 and low < high, finite
+ * (otherwise SPOT_ERR_UNSUPPORTED).  Nothing is enqueued.
+ */
+spot_status spot_rope_frequencies(int rope_dim, double rope_base, int scaling, double factor,
+                                  int orig_len, double low, double high, double *freq);
+
+/*
+ * spot_rotary -- rotary positions of the heads of `rows` tokens (Section 2.1 and
+ * Appendix A: rotary embedding of part of a head; Table 1: scaled by YaRN):
+ *     (a, b) of pair i -> amp * (a cos - b sin, b cos + a sin) of pos[row] * freq[i]
+ * for the pairs of the first rope_dim elements of every head; the others are copied.
+ * Angles in FP64 and their sine and cosine in FP32 as in spot_selector_project;
+ * FP32 arithmetic, one rounding.
+ *
+ *  x        device [rows, heads, d], row r at x + r * x_stride elements (a slice of
+ *           a fused projection's output may be given)
+ *  pos      device int32 [rows]
+ *  freq     host double [rope_dim / 2], finite (read during the call; may be NULL where
+ *           rope_dim is 0)
+ *  amp      factor of sine and cosine, finite
+ *  flags    SPOT_ROPE_INTERLEAVED, SPOT_ROPE_INVERSE
+ *  out      device [rows, heads, d], row r at out + r * out_stride elements
+ *           (output); x itself (the same pointer and stride) or no byte of it
+ *
+ * Any d and rope_dim that are even, rope_dim <= min(d, 256), d <= 1024; arrays on a
+ * 2-byte boundary (16-byte chunks are used where pointers, strides, d and rope_dim
+ * are multiples of 16 bytes resp. elements).  Strides >= heads * d.
+ */
+spot_status spot_rotary(const void *x, int64_t x_stride, const int32_t *pos, int rows, int heads,
+                        int d, int rope_dim, const double *freq, float amp, int flags, int dtype,
+                        void *out, int64_t out_stride, void *stream);
+
+/*
+ * spot_rotary_append -- the rotations of a step's queries and keys and the append of
+ * its keys and values to a paged cache, in one launch (Section 2.1 and Appendix A;
+ * Table 1 for the scaling): spot_rotary of every head of q into q_out and of every
+ * head of k into the slot of its token in k_pages; v is copied to v_pages.  Tokens
+ * that are not there (see above) and those with a negative position store nothing.
+ *
+ *  q, k, v  device [rows, h_q, d], [rows, h_kv, d] twice, with row strides in
+ *           elements (slices of a fused projection's output may be given)
+ *  pos      device int32 [rows]: positions of the angles, or NULL (the token's
+ *           place in the cache; after an eviction the two differ)
+ *  page_table device int32 [n_seq, max_pages]
+ *  q_out    device [rows, h_q, d] (output; q itself if q_stride is h_q * d)
+ *  k_pages, v_pages device (the slots of the new tokens are written)
+ * The rest as spot_rotary and above.  Two rows of one slot (a page that two
+ * sequences share) must not be written in one call.
+ */
+spot_status spot_rotary_append(const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                               const void *v, int64_t v_stride, int dtype, const int32_t *pos,
+                               const int32_t *page_table, int n_pages, int page_size,
+                               int max_pages, const int32_t *seq_start, const int32_t *seq_len,
+                               int n_seq, int rows, int h_q, int h_kv, int d, int rope_dim,
+                               const double *freq, float amp, int flags, void *q_out,
+                               void *k_pages, void *v_pages, void *stream);
+
+/*
+ * spot_paged_attend -- attention of new tokens over a paged cache (Section 3: dense
+ * attention, the method's baseline; Appendix B: attention in the prefill regime),
+ * for decode steps, chunks of prompts and whole prompts alike.  For row i of
+ * sequence s (position p) and query head h with KV head g = h / (h_q / h_kv):
+ *     x_t = c(sm_scale * q[row, h] . k[s, g, t]) - slopes[h] * |p - t|
+ *     c(y) = softcap * tanh(y / softcap), or y where softcap is 0
+ *     out[row, h] = sum_t softmax_t(x_t) v[s, g, t],  lse[row, h] = log sum_t exp(x_t)
+ * over the tokens t of [lo, hi) that are there:
+ *     hi = max(p + 1, min(prefix[s], seq_len[s])): causal, and a prefix that every row
+ *          of the sequence sees;
+ *     lo = max(0, first[row], p - window + 1): the start of the row's document, and a
+ *          sliding window.
+ * A row that sees no token gets out = 0 and lse = -inf.  Keys and values of tokens
+ * that no row of a tile of rows sees may hold anything, NaN included; a NaN or an
+ * infinity in a value that only some rows of a tile see makes no other row's
+ * output NaN either.
+ *
+ *  q          device [rows, h_q, d], 16-byte aligned
+ *  page_table device int32 [n_seq, max_pages]
+ *  slopes     device float [h_q] or NULL (no bias)
+ *  window     tokens a row sees at most, its own included; 0: no limit
+ *  prefix     device int32 [n_seq] or NULL;  first  device int32 [rows] or NULL
+ *  out        device [rows, h_q, d] (output, rounded to nearest even), 16-byte aligned
+ *  lse        device float [rows, h_q] (output, may be NULL)
+ *  ws         device, at least spot_paged_workspace_bytes(...) of these sizes, 16-byte
+ *             aligned, zero-filled before its first use; every call leaves it ready
+ *             for the next one, of any sizes it is large enough for.  Calls that may
+ *             overlap in time need separate workspaces.
+ *
+ * Numerics: FP32 scores and softmax, the probabilities rounded to the element type
+ * for the product with V (FP32 accumulation).  The division of the work depends on
+ * the sizes and lengths only, and there are no floating-point atomics: the same
+ * inputs give the same bits.
+ * Supported: d 64 or 128, h_q any multiple of h_kv, finite sm_scale, softcap finite
+ * and >= 0 (SPOT_ERR_UNSUPPORTED otherwise).
+ */
+size_t spot_paged_workspace_bytes(int n_seq, int rows, int h_q, int h_kv, int d);
+
+spot_status spot_paged_attend(const void *q, int dtype, const void *k_pages, const void *v_pages,
+                              const int32_t *page_table, int n_pages, int page_size,
+                              int max_pages, const int32_t *seq_start, const int32_t *seq_len,
+                              int n_seq, int rows, int h_q, int h_kv, int d, float sm_scale,
+                              float softcap, const float *slopes, int window,
+                              const int32_t *prefix, const int32_t *first, void *out, float *lse,
+                              void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * spot_paged_weights -- the attention weight that each cached token receives, summed
+ * per KV head (Section 2.2 takes the heads' mean of these probabilities as the
+ * teacher of its selector; here they rank tokens for an eviction):
+ *     acc_out[s, g, t] = decay * acc[s, g, t]
+ *                        + sum over rows i of s and heads h of g of exp(x_t - lse[row, h])
+ * with x_t, the tokens a row sees and all arguments as in spot_paged_attend, whose lse
+ * this takes (rows with lse = -inf add nothing).  Every t < max_pages * page_size is
+ * written; a token that no row sees gets decay * acc.
+ *
+ *  lse      device float [rows, h_q]
+ *  acc      device float [n_seq, h_kv, max_pages * page_size] or NULL (0)
+ *  decay    finite
+ *  acc_out  device float, of acc's shape (output); may be acc itself
+ *
+ * FP32 sums in a fixed order (deterministic).  n_seq <= 65535
+ * (SPOT_ERR_UNSUPPORTED).
+ */
+spot_status spot_paged_weights(const void *q, const float *lse, int dtype, const void *k_pages,
+                               const int32_t *page_table, int n_pages, int page_size,
+                               int max_pages, const int32_t *seq_start, const int32_t *seq_len,
+                               int n_seq, int rows, int h_q, int h_kv, int d, float sm_scale,
+                               float softcap, const float *slopes, int window,
+                               const int32_t *prefix, const int32_t *first, const float *acc,
+                               float decay, float *acc_out, void *stream);
+
+/*
+ * spot_cache_evict -- keeps the heaviest tokens of a paged cache and copies them to
+ * new pages.  As Section 2.3 does for blocks, a sink prefix and a recency suffix
+ * always stay; per sequence s and KV head g, with len = seq_len[s] (clamped to
+ * [0, max_pages * page_size]):
+ *     len <= budget: every token stays;
+ *     otherwise the tokens [0, n_sink) and [len - n_recent, len), and of the others the
+ *     budget - n_sink - n_recent of the largest acc[s, g, t] (equal weights: the lower
+ *     token first; NaN ranks below every number).
+ * The kept tokens, ascending, become tokens 0, 1, ... of the head in the pages of
+ * dst_table, with their weights, so that causal order stays; the heads of a sequence
+ * keep different tokens, but equally many.  Later attention counts distances and
+ * windows in places of the new cache, and rotated keys keep their angles (give
+ * spot_rotary_append the text positions).
+ *
+ *  acc        device float [n_seq, h_kv, max_pages * page_size]
+ *  k_pages, v_pages, page_table   the cache, 16-bit elements of either type
+ *  k_dst, v_dst  device [n_dst_pages, h_kv, page_size, d] (output): the same pools or
+ *             others.  Pages of dst_table must not be pages of page_table that the
+ *             call reads, nor occur twice.
+ *  dst_table  device int32 [n_seq, dst_max_pages]; a kept token whose page id lies
+ *             outside [0, n_dst_pages) is not stored
+ *  idx        device int32 [n_seq, h_kv, budget] (output): the kept tokens, ascending,
+ *             padded with -1
+ *  new_len    device int32 [n_seq] (output): min(len, budget); not seq_len itself
+ *  acc_out    device float [n_seq, h_kv, out_cap] (output): their weights, then zeros;
+ *             not acc itself.  out_cap >= budget
+ *
+ * Supported: d a multiple of 8, 8 <= d <= 1024; n_seq, h_kv <= 65535.  Errors:
+ * SPOT_ERR_RULE where budget < 1, n_sink or n_recent < 0 or n_sink + n_recent >
+ * budget; SPOT_ERR_SHAPE where budget exceeds dst_max_pages * page_size or out_cap.
+ */
+spot_status spot_cache_evict(const float *acc, const void *k_pages, const void *v_pages,
+                             const int32_t *page_table, int n_pages, int page_size,
+                             int max_pages, const int32_t *seq_len, int n_seq, int h_kv, int d,
+                             int budget, int n_sink, int n_recent, void *k_dst, void *v_dst,
+                             const int32_t *dst_table, int n_dst_pages, int dst_max_pages,
+                             int32_t *idx, int32_t *new_len, float *acc_out, int out_cap,
+                             void *stream);
+
 /*
  * spot_probe_stream_read -- measurement helper, not part of the attention
  * path: reads `bytes` bytes of device memory at `buf` once with 16-byte

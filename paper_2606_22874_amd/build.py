@@ -24,8 +24,9 @@ SO = os.path.join(PKG, "libspot.so")
 BINDING = os.path.join(PKG, "_binding.so")
 ARCH = "gfx950"
 
-SOURCES = ["api.hip", "frontend.hip", "frontend_mfma.hip", "score.hip", "score_many.hip", "score_tokens.hip", "select.hip", "decode.hip", "step.hip", "prefill.hip",
-           "probe.hip"]
+SOURCES = ["api.hip", "api_paged.hip", "frontend.hip", "frontend_mfma.hip", "score.hip",
+           "score_many.hip", "score_tokens.hip", "select.hip", "decode.hip", "step.hip",
+           "prefill.hip", "rotary.hip", "attend_few.hip", "weights.hip", "evict.hip", "probe.hip"]
 
 HIPCC_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",

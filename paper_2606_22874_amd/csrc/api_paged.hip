@@ -1,0 +1,279 @@
+// C ABI of the operators on a paged cache: argument validation, then kernel
+// launches.  Nothing is enqueued unless every argument check passes.
+#include <math.h>
+
+#include "paged_core.h"
+
+using namespace spot;
+using namespace spot::paged;
+
+namespace {
+
+spot_status from_hip(hipError_t e) { return e == hipSuccess ? SPOT_OK : SPOT_ERR_HIP; }
+
+bool aligned(const void* p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+bool valid_dtype(int dtype) { return dtype == SPOT_DTYPE_BF16 || dtype == SPOT_DTYPE_FP16; }
+
+// A pool's sizes and those of a page table over it.
+bool valid_pages(int n_pages, int page_size, int max_pages, int h_kv) {
+  return n_pages >= 0 && page_size >= kGroupKeys && page_size % kGroupKeys == 0 &&
+         max_pages >= 0 && h_kv >= 1 && (int64_t)max_pages * page_size <= 1 << 30 &&
+         (__int128)n_pages * h_kv * page_size < (__int128)1 << 31;
+}
+
+// What spot_paged_attend and spot_paged_weights share.
+spot_status check_attend(int dtype, int n_pages, int page_size, int max_pages, int n_seq, int rows,
+                         int h_q, int h_kv, int d, float sm_scale, float softcap, int window) {
+  if (n_seq < 0 || rows < 0 || h_q < 1 || window < 0 ||
+      !valid_pages(n_pages, page_size, max_pages, h_kv) || (int64_t)rows * h_q > 0x7fffffff)
+    return SPOT_ERR_SHAPE;
+  if (!valid_dtype(dtype) || (d != 64 && d != 128) || h_q % h_kv) return SPOT_ERR_UNSUPPORTED;
+  if (!isfinite(sm_scale) || !(softcap >= 0.f) || !isfinite(softcap) ||
+      (softcap > 0.f && !isfinite(sm_scale / softcap)))
+    return SPOT_ERR_UNSUPPORTED;
+  return SPOT_OK;
+}
+
+spot_status check_rope(int d, int rope_dim, const double* freq, float amp, int flags, int dtype) {
+  if (d < 2 || d % 2 || d > 1024 || rope_dim < 0 || rope_dim % 2 || rope_dim > d ||
+      rope_dim > 2 * kMaxPairs || !valid_dtype(dtype) || !isfinite(amp) ||
+      (flags & ~(SPOT_ROPE_INTERLEAVED | SPOT_ROPE_INVERSE)))
+    return SPOT_ERR_UNSUPPORTED;
+  for (int i = 0; i < rope_dim / 2; ++i)
+    if (!isfinite(freq[i])) return SPOT_ERR_UNSUPPORTED;
+  return SPOT_OK;
+}
+
+const uint16_t* in16(const void* p) { return static_cast<const uint16_t*>(p); }
+uint16_t* out16(void* p) { return static_cast<uint16_t*>(p); }
+
+}  // namespace
+
+extern "C" {
+
+spot_status spot_rope_frequencies(int rope_dim, double rope_base, int scaling, double factor,
+                                  int orig_len, double low, double high, double* freq) {
+  if (!freq && rope_dim > 0) return SPOT_ERR_NULL;
+  if (rope_dim < 0 || rope_dim % 2 || rope_dim > 2 * kMaxPairs || !(rope_base > 0.0) ||
+      !isfinite(rope_base) || scaling < SPOT_ROPE_NONE || scaling > SPOT_ROPE_PARTS)
+    return SPOT_ERR_UNSUPPORTED;
+  if (scaling != SPOT_ROPE_NONE && (!(factor >= 1.0) || !isfinite(factor)))
+    return SPOT_ERR_UNSUPPORTED;
+  if (scaling == SPOT_ROPE_BASE && rope_dim == 2) return SPOT_ERR_UNSUPPORTED;
+  if (scaling == SPOT_ROPE_PARTS && (orig_len < 1 || !isfinite(low) || !isfinite(high) || !(low < high)))
+    return SPOT_ERR_UNSUPPORTED;
+  double base = rope_base;
+  if (scaling == SPOT_ROPE_BASE && rope_dim > 2)
+    base *= pow(factor, (double)rope_dim / (rope_dim - 2));
+  for (int i = 0; i < rope_dim / 2; ++i) {
+    double f = pow(base, -2.0 * i / rope_dim);
+    if (scaling == SPOT_ROPE_LINEAR) f /= factor;
+    if (scaling == SPOT_ROPE_PARTS) {
+      const double turns = orig_len * f / 6.283185307179586;
+      const double g = fmin(fmax((turns - low) / (high - low), 0.0), 1.0);
+      f = g * f + (1.0 - g) * (f / factor);
+    }
+    freq[i] = f;
+  }
+  return SPOT_OK;
+}
+
+spot_status spot_rotary(const void* x, int64_t x_stride, const int32_t* pos, int rows, int heads,
+                        int d, int rope_dim, const double* freq, float amp, int flags, int dtype,
+                        void* out, int64_t out_stride, void* stream) {
+  if ((!freq && rope_dim > 0) || (rows > 0 && (!x || !pos || !out))) return SPOT_ERR_NULL;
+  if (rows < 0 || heads < 1) return SPOT_ERR_SHAPE;
+  const spot_status st = check_rope(d, rope_dim, freq, amp, flags, dtype);
+  if (st != SPOT_OK) return st;
+  const int64_t row = (int64_t)heads * d;
+  if (row > 1 << 24 || x_stride < row || out_stride < row || !aligned(x, 2) || !aligned(out, 2))
+    return SPOT_ERR_SHAPE;
+  if (rows == 0) return SPOT_OK;
+  RotaryArgs a = {};
+  a.q = in16(x);
+  a.q_stride = x_stride;
+  a.out_stride = out_stride;
+  a.pos = pos;
+  a.q_out = out16(out);
+  a.rows = rows;
+  a.h_q = heads;
+  a.h_kv = 1;
+  a.d = d;
+  a.rope_dim = rope_dim;
+  a.amp = amp;
+  a.inverse = flags & SPOT_ROPE_INVERSE;
+  for (int i = 0; i < rope_dim / 2; ++i) a.freq.f[i] = freq[i];
+  return from_hip(launch_rotary(a, dtype, flags & SPOT_ROPE_INTERLEAVED,
+                                static_cast<hipStream_t>(stream)));
+}
+
+spot_status spot_rotary_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, int dtype, const int32_t* pos,
+                               const int32_t* page_table, int n_pages, int page_size,
+                               int max_pages, const int32_t* seq_start, const int32_t* seq_len,
+                               int n_seq, int rows, int h_q, int h_kv, int d, int rope_dim,
+                               const double* freq, float amp, int flags, void* q_out,
+                               void* k_pages, void* v_pages, void* stream) {
+  if ((!freq && rope_dim > 0) ||
+      (rows > 0 && n_seq > 0 && (!q || !k || !v || !page_table || !seq_start || !seq_len || !q_out ||
+                                 !k_pages || !v_pages)))
+    return SPOT_ERR_NULL;
+  if (n_seq < 0 || rows < 0 || h_q < 1 || !valid_pages(n_pages, page_size, max_pages, h_kv) ||
+      (int64_t)rows * h_q > 0x7fffffff)
+    return SPOT_ERR_SHAPE;
+  const spot_status st = check_rope(d, rope_dim, freq, amp, flags, dtype);
+  if (st != SPOT_OK) return st;
+  if ((int64_t)h_q * d > 1 << 24 || (int64_t)h_kv * d > 1 << 24 || q_stride < (int64_t)h_q * d ||
+      k_stride < (int64_t)h_kv * d || v_stride < (int64_t)h_kv * d)
+    return SPOT_ERR_SHAPE;
+  if (rows > 0 && q_out == q && q_stride != (int64_t)h_q * d) return SPOT_ERR_SHAPE;
+  for (const void* p : {q, k, v, (const void*)q_out, (const void*)k_pages, (const void*)v_pages})
+    if (!aligned(p, 2)) return SPOT_ERR_SHAPE;
+  if (rows == 0 || n_seq == 0) return SPOT_OK;
+  RotaryArgs a = {};
+  a.q = in16(q);
+  a.k = in16(k);
+  a.v = in16(v);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.out_stride = (int64_t)h_q * d;
+  a.pos = pos;
+  a.q_out = out16(q_out);
+  a.k_pages = out16(k_pages);
+  a.v_pages = out16(v_pages);
+  a.pages = Pages{page_table, n_pages, page_size, max_pages};
+  a.seq_start = seq_start;
+  a.seq_len = seq_len;
+  a.n_seq = n_seq;
+  a.rows = rows;
+  a.h_q = h_q;
+  a.h_kv = h_kv;
+  a.d = d;
+  a.rope_dim = rope_dim;
+  a.amp = amp;
+  a.inverse = flags & SPOT_ROPE_INVERSE;
+  for (int i = 0; i < rope_dim / 2; ++i) a.freq.f[i] = freq[i];
+  return from_hip(launch_rotary(a, dtype, flags & SPOT_ROPE_INTERLEAVED,
+                                static_cast<hipStream_t>(stream)));
+}
+
+size_t spot_paged_workspace_bytes(int n_seq, int rows, int h_q, int h_kv, int d) {
+  if (n_seq < 1 || rows < 1 || h_q < 1 || h_kv < 1 || d < 1) return 0;
+  return attend_few_workspace(d);
+}
+
+spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, const void* v_pages,
+                              const int32_t* page_table, int n_pages, int page_size, int max_pages,
+                              const int32_t* seq_start, const int32_t* seq_len, int n_seq, int rows,
+                              int h_q, int h_kv, int d, float sm_scale, float softcap,
+                              const float* slopes, int window, const int32_t* prefix,
+                              const int32_t* first, void* out, float* lse, void* ws,
+                              size_t ws_bytes, void* stream) {
+  if (rows > 0 && n_seq > 0 &&
+      (!q || !k_pages || !v_pages || !page_table || !seq_start || !seq_len || !out))
+    return SPOT_ERR_NULL;
+  const spot_status st = check_attend(dtype, n_pages, page_size, max_pages, n_seq, rows, h_q, h_kv,
+                                      d, sm_scale, softcap, window);
+  if (st != SPOT_OK) return st;
+  if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16))
+    return SPOT_ERR_SHAPE;
+  if (rows == 0 || n_seq == 0) return SPOT_OK;
+  if (!ws || ws_bytes < spot_paged_workspace_bytes(n_seq, rows, h_q, h_kv, d) || !aligned(ws, 16))
+    return SPOT_ERR_WORKSPACE;
+  AttendArgs a = {};
+  a.q = in16(q);
+  a.k = in16(k_pages);
+  a.v = in16(v_pages);
+  a.pages = Pages{page_table, n_pages, page_size, max_pages};
+  a.seq_start = seq_start;
+  a.seq_len = seq_len;
+  a.n_seq = n_seq;
+  a.rows = rows;
+  a.h_q = h_q;
+  a.h_kv = h_kv;
+  a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first};
+  a.out = out16(out);
+  a.lse = lse;
+  return from_hip(launch_attend_few(a, dtype, d, ws, static_cast<hipStream_t>(stream)));
+}
+
+spot_status spot_paged_weights(const void* q, const float* lse, int dtype, const void* k_pages,
+                               const int32_t* page_table, int n_pages, int page_size,
+                               int max_pages, const int32_t* seq_start, const int32_t* seq_len,
+                               int n_seq, int rows, int h_q, int h_kv, int d, float sm_scale,
+                               float softcap, const float* slopes, int window,
+                               const int32_t* prefix, const int32_t* first, const float* acc,
+                               float decay, float* acc_out, void* stream) {
+  if (n_seq > 0 && (!k_pages || !page_table || !seq_start || !seq_len || !acc_out ||
+                    (rows > 0 && (!q || !lse))))
+    return SPOT_ERR_NULL;
+  const spot_status st = check_attend(dtype, n_pages, page_size, max_pages, n_seq, rows, h_q, h_kv,
+                                      d, sm_scale, softcap, window);
+  if (st != SPOT_OK) return st;
+  if (!aligned(q, 16) || !aligned(k_pages, 16)) return SPOT_ERR_SHAPE;
+  if (!isfinite(decay) || n_seq > 65535) return SPOT_ERR_UNSUPPORTED;
+  if (n_seq == 0) return SPOT_OK;
+  WeightArgs a = {};
+  a.q = in16(q);
+  a.lse = lse;
+  a.k = in16(k_pages);
+  a.pages = Pages{page_table, n_pages, page_size, max_pages};
+  a.seq_start = seq_start;
+  a.seq_len = seq_len;
+  a.n_seq = n_seq;
+  a.rows = rows;
+  a.h_q = h_q;
+  a.h_kv = h_kv;
+  a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first};
+  a.acc = acc;
+  a.decay = decay;
+  a.acc_out = acc_out;
+  return from_hip(launch_weights(a, dtype, d, static_cast<hipStream_t>(stream)));
+}
+
+spot_status spot_cache_evict(const float* acc, const void* k_pages, const void* v_pages,
+                             const int32_t* page_table, int n_pages, int page_size, int max_pages,
+                             const int32_t* seq_len, int n_seq, int h_kv, int d, int budget,
+                             int n_sink, int n_recent, void* k_dst, void* v_dst,
+                             const int32_t* dst_table, int n_dst_pages, int dst_max_pages,
+                             int32_t* idx, int32_t* new_len, float* acc_out, int out_cap,
+                             void* stream) {
+  if (!acc || !k_pages || !v_pages || !page_table || !seq_len || !k_dst || !v_dst || !dst_table ||
+      !idx || !new_len || !acc_out)
+    return SPOT_ERR_NULL;
+  if (n_seq < 0 || !valid_pages(n_pages, page_size, max_pages, h_kv) ||
+      !valid_pages(n_dst_pages, page_size, dst_max_pages, h_kv))
+    return SPOT_ERR_SHAPE;
+  if (budget < 1 || n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > budget)
+    return SPOT_ERR_RULE;
+  if (d < 8 || d % 8 || d > 1024 || n_seq > 65535 || h_kv > 65535) return SPOT_ERR_UNSUPPORTED;
+  if (budget > (int64_t)dst_max_pages * page_size || budget > out_cap) return SPOT_ERR_SHAPE;
+  if (!aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(k_dst, 16) || !aligned(v_dst, 16))
+    return SPOT_ERR_SHAPE;
+  if (acc_out == acc || new_len == seq_len) return SPOT_ERR_SHAPE;
+  if (n_seq == 0) return SPOT_OK;
+  EvictArgs a = {};
+  a.acc = acc;
+  a.k = in16(k_pages);
+  a.v = in16(v_pages);
+  a.pages = Pages{page_table, n_pages, page_size, max_pages};
+  a.seq_len = seq_len;
+  a.n_seq = n_seq;
+  a.h_kv = h_kv;
+  a.d = d;
+  a.budget = budget;
+  a.n_sink = n_sink;
+  a.n_recent = n_recent;
+  a.k_dst = out16(k_dst);
+  a.v_dst = out16(v_dst);
+  a.dst = Pages{dst_table, n_dst_pages, page_size, dst_max_pages};
+  a.idx = idx;
+  a.new_len = new_len;
+  a.acc_out = acc_out;
+  a.out_cap = out_cap;
+  return from_hip(launch_evict(a, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -32,7 +32,7 @@ __attribute__((used)) const char kBuiltFor[] = "spot binding for torch " SPOT_TO
 // Entry points of the loaded libspot, in the order spot.py passes them.
 enum Fn {
   kScore, kScoreQ, kScoreTokensBlk, kProject, kProjectPooled, kPool, kSelect, kSparseBlk, kDense,
-  kPrefill, kStep, kStepQ, kStepStatic, kFns
+  kPrefill, kStep, kStepQ, kStepStatic, kRotary, kRotaryAppend, kAttend, kWeights, kEvict, kFns
 };
 void* g_fn[kFns];
 PyObject* g_stream_type;    // torch.cuda.Stream
@@ -66,6 +66,7 @@ struct Args {
   PyObject* const* a;
   Py_ssize_t n, i = 0;
   bool ok = true;
+  PyObject* given = nullptr;   // the stream object, where one was passed
 
   PyObject* next() {
     if (i >= n) ok = false;
@@ -105,6 +106,7 @@ struct Args {
     if (!o) return nullptr;
     if (o == Py_None) return c10::hip::getCurrentHIPStream().stream();
     if ((PyObject*)Py_TYPE(o) != g_stream_type) return ok = false, nullptr;
+    given = o;
     PyObject* v = PyObject_GetAttr(o, g_stream_attr);
     void* p = v ? PyLong_AsVoidPtr(v) : nullptr;
     Py_XDECREF(v);
@@ -468,6 +470,223 @@ PyObject* decode_step_static(Args a) {
   });
 }
 
+// ---------------------------------------------------------- paged cache
+// The operators' tensors all lie on one device, and on the current one.
+struct Place {
+  int device = -1;
+  void see(Args& a, const Dev& t) {
+    if (!a.ok || t.none()) return;
+    if (!THPVariable_CheckExact(t.o)) {
+      a.ok = false;
+      return;
+    }
+    const int d = THPVariable_Unpack(t.o).get_device();
+    if (device < 0) device = c10::hip::current_device();
+    if (d != device) a.ok = false;
+  }
+  template <typename... Ts>
+  Place(Args& a, const Ts&... t) {
+    (see(a, t), ...);
+    if (!a.ok || !a.given) return;
+    PyObject* i = PyObject_GetAttrString(a.given, "device_index");
+    if (!i || PyLong_AsLong(i) != device) a.ok = false;
+    Py_XDECREF(i);
+    PyErr_Clear();
+  }
+};
+
+// The element type that the call's 16-bit tensors share: its bit, and SPOT_DTYPE.
+struct Element {
+  unsigned bit = 0;
+  int dtype = 0;
+  Element(Args& a, const Dev& t) {
+    if (!a.ok || !THPVariable_CheckExact(t.o)) {
+      a.ok = false;
+      return;
+    }
+    bit = dtype_bit(THPVariable_Unpack(t.o).scalar_type()) & (BF16 | F16);
+    dtype = bit == F16 ? SPOT_DTYPE_FP16 : SPOT_DTYPE_BF16;
+    if (!bit) a.ok = false;
+  }
+};
+
+int64_t wide(Args& a) {
+  PyObject* o = a.next();
+  if (!o || !PyLong_Check(o)) return a.ok = false, 0;
+  int over = 0;
+  const long long v = PyLong_AsLongLongAndOverflow(o, &over);
+  if (over) a.ok = false;
+  return v;
+}
+
+// Rows of `row` elements, `stride` apart, inside a tensor's storage.
+void* rows_of(Args& a, const Dev& t, unsigned bit, big rows, big stride, big row) {
+  if (!a.ok || !THPVariable_CheckExact(t.o)) return a.ok = false, nullptr;
+  const at::Tensor& x = THPVariable_Unpack(t.o);
+  if (!x.is_cuda() || dtype_bit(x.scalar_type()) != bit) return a.ok = false, nullptr;
+  const big left = (big)(x.storage().nbytes() / 2) - x.storage_offset();
+  if (rows > 0 && (rows - 1) * stride + row > left) a.ok = false;
+  return x.data_ptr();
+}
+
+const double* freq_of(Args& a, const Dev& t, int rope_dim) {
+  if (!a.ok || !THPVariable_CheckExact(t.o)) return a.ok = false, nullptr;
+  const at::Tensor& x = THPVariable_Unpack(t.o);
+  if (!x.is_cpu() || x.scalar_type() != at::kDouble || !x.is_contiguous() ||
+      x.numel() < rope_dim / 2)
+    return a.ok = false, nullptr;
+  return static_cast<const double*>(x.data_ptr());
+}
+
+// x, x_stride, pos, rows, heads, d, rope_dim, freq, amp, flags, out, out_stride, stream
+PyObject* rotary(Args a) {
+  Dev x(a);
+  const int64_t xs = wide(a);
+  Dev pos(a);
+  const int rows = a.integer(), heads = a.integer(), d = a.integer(), rope = a.integer();
+  Dev freq(a);
+  const float amp = a.real();
+  const int flags = a.integer();
+  Dev out(a);
+  const int64_t os = wide(a);
+  void* st = a.stream();
+  const Element el(a, x);
+  const Place place(a, x, pos, out);
+  void *xp = rows_of(a, x, el.bit, rows, xs, (big)heads * d), *pp = pos.ptr(a, I32, rows),
+       *op = rows_of(a, out, el.bit, rows, os, (big)heads * d);
+  const double* fr = freq_of(a, freq, rope);
+  return finish(a, [&] {
+    return fn(kRotary, &spot_rotary)(xp, xs, ip(pp), rows, heads, d, rope, fr, amp, flags, el.dtype,
+                                     op, os, st);
+  });
+}
+
+// q, q_stride, k, k_stride, v, v_stride, pos, page_table, n_pages, page_size, max_pages, seq_start,
+// seq_len, n_seq, rows, h_q, h_kv, d, rope_dim, freq, amp, flags, q_out, k_pages, v_pages, stream
+PyObject* rotary_append(Args a) {
+  Dev q(a);
+  const int64_t qs = wide(a);
+  Dev k(a);
+  const int64_t ks = wide(a);
+  Dev v(a);
+  const int64_t vs = wide(a);
+  Dev pos(a), tab(a);
+  const int np = a.integer(), ps = a.integer(), mp = a.integer();
+  Dev start(a), len(a);
+  const int ns = a.integer(), rows = a.integer(), hq = a.integer(), hkv = a.integer(),
+            d = a.integer(), rope = a.integer();
+  Dev freq(a);
+  const float amp = a.real();
+  const int flags = a.integer();
+  Dev qo(a), kp(a), vp(a);
+  void* st = a.stream();
+  const Element el(a, q);
+  const Place place(a, q, k, v, pos, tab, start, len, qo, kp, vp);
+  const big pool = (big)np * hkv * ps * d;
+  void *qp = rows_of(a, q, el.bit, rows, qs, (big)hq * d),
+       *kip = rows_of(a, k, el.bit, rows, ks, (big)hkv * d),
+       *vip = rows_of(a, v, el.bit, rows, vs, (big)hkv * d), *pp = pos.opt(a, I32, rows),
+       *tp = tab.ptr(a, I32, (big)ns * mp), *sp = start.ptr(a, I32, (big)ns + 1),
+       *lp = len.ptr(a, I32, ns), *qop = qo.ptr(a, el.bit, (big)rows * hq * d),
+       *kpp = kp.ptr(a, el.bit, pool), *vpp = vp.ptr(a, el.bit, pool);
+  const double* fr = freq_of(a, freq, rope);
+  return finish(a, [&] {
+    return fn(kRotaryAppend, &spot_rotary_append)(
+        qp, qs, kip, ks, vip, vs, el.dtype, ip(pp), ip(tp), np, ps, mp, ip(sp), ip(lp), ns, rows, hq,
+        hkv, d, rope, fr, amp, flags, qop, kpp, vpp, st);
+  });
+}
+
+// q, k_pages, v_pages, page_table, n_pages, page_size, max_pages, seq_start, seq_len, n_seq, rows,
+// h_q, h_kv, d, sm_scale, softcap, slopes, window, prefix, first, out, lse, ws, stream
+PyObject* paged_attend(Args a) {
+  Dev q(a), kp(a), vp(a), tab(a);
+  const int np = a.integer(), ps = a.integer(), mp = a.integer();
+  Dev start(a), len(a);
+  const int ns = a.integer(), rows = a.integer(), hq = a.integer(), hkv = a.integer(),
+            d = a.integer();
+  const float scale = a.real(), softcap = a.real();
+  Dev slopes(a);
+  const int window = a.integer();
+  Dev prefix(a), first(a), out(a), lse(a), ws(a);
+  void* st = a.stream();
+  const Element el(a, q);
+  const Place place(a, q, kp, vp, tab, start, len, slopes, prefix, first, out, lse, ws);
+  const big pool = (big)np * hkv * ps * d, n = (big)rows * hq * d;
+  void *qp = q.ptr(a, el.bit, n), *kpp = kp.ptr(a, el.bit, pool), *vpp = vp.ptr(a, el.bit, pool),
+       *tp = tab.ptr(a, I32, (big)ns * mp), *sp = start.ptr(a, I32, (big)ns + 1),
+       *lp = len.ptr(a, I32, ns), *slp = slopes.opt(a, F32, hq), *prp = prefix.opt(a, I32, ns),
+       *fp_ = first.opt(a, I32, rows), *op = out.ptr(a, el.bit, n),
+       *lsp = lse.opt(a, F32, (big)rows * hq), *wp = ws.ptr(a, ANY, 0);
+  const size_t wb = a.ok ? ws.bytes() : 0;
+  return finish(a, [&] {
+    return fn(kAttend, &spot_paged_attend)(
+        qp, el.dtype, kpp, vpp, ip(tp), np, ps, mp, ip(sp), ip(lp), ns, rows, hq, hkv, d, scale,
+        softcap, fp(slp), window, ip(prp), ip(fp_), op, static_cast<float*>(lsp), wp, wb, st);
+  });
+}
+
+// q, lse, k_pages, page_table, n_pages, page_size, max_pages, seq_start, seq_len, n_seq, rows, h_q,
+// h_kv, d, sm_scale, softcap, slopes, window, prefix, first, acc, decay, acc_out, stream
+PyObject* paged_weights(Args a) {
+  Dev q(a), lse(a), kp(a), tab(a);
+  const int np = a.integer(), ps = a.integer(), mp = a.integer();
+  Dev start(a), len(a);
+  const int ns = a.integer(), rows = a.integer(), hq = a.integer(), hkv = a.integer(),
+            d = a.integer();
+  const float scale = a.real(), softcap = a.real();
+  Dev slopes(a);
+  const int window = a.integer();
+  Dev prefix(a), first(a), acc(a);
+  const float decay = a.real();
+  Dev out(a);
+  void* st = a.stream();
+  const Element el(a, q);
+  const Place place(a, q, lse, kp, tab, start, len, slopes, prefix, first, acc, out);
+  const big n_acc = (big)ns * hkv * mp * ps;
+  void *qp = q.ptr(a, el.bit, (big)rows * hq * d), *lsp = lse.ptr(a, F32, (big)rows * hq),
+       *kpp = kp.ptr(a, el.bit, (big)np * hkv * ps * d), *tp = tab.ptr(a, I32, (big)ns * mp),
+       *sp = start.ptr(a, I32, (big)ns + 1), *lp = len.ptr(a, I32, ns),
+       *slp = slopes.opt(a, F32, hq), *prp = prefix.opt(a, I32, ns),
+       *fp_ = first.opt(a, I32, rows), *ap = acc.opt(a, F32, n_acc), *op = out.ptr(a, F32, n_acc);
+  return finish(a, [&] {
+    return fn(kWeights, &spot_paged_weights)(
+        qp, fp(lsp), el.dtype, kpp, ip(tp), np, ps, mp, ip(sp), ip(lp), ns, rows, hq, hkv, d, scale,
+        softcap, fp(slp), window, ip(prp), ip(fp_), fp(ap), decay, static_cast<float*>(op), st);
+  });
+}
+
+// acc, k_pages, v_pages, page_table, n_pages, page_size, max_pages, seq_len, n_seq, h_kv, d, budget,
+// n_sink, n_recent, k_dst, v_dst, dst_table, n_dst_pages, dst_max_pages, idx, new_len, acc_out,
+// out_cap, stream
+PyObject* cache_evict(Args a) {
+  Dev acc(a), kp(a), vp(a), tab(a);
+  const int np = a.integer(), ps = a.integer(), mp = a.integer();
+  Dev len(a);
+  const int ns = a.integer(), hkv = a.integer(), d = a.integer(), budget = a.integer(),
+            sink = a.integer(), recent = a.integer();
+  Dev kd(a), vd(a), dtab(a);
+  const int nd = a.integer(), md = a.integer();
+  Dev idx(a), nl(a), ao(a);
+  const int oc = a.integer();
+  void* st = a.stream();
+  const Element el(a, kp);
+  const Place place(a, acc, kp, vp, tab, len, kd, vd, dtab, idx, nl, ao);
+  const big page = (big)hkv * ps * d, heads = (big)ns * hkv;
+  void *ap = acc.ptr(a, F32, heads * mp * ps), *kpp = kp.ptr(a, el.bit, np * page),
+       *vpp = vp.ptr(a, el.bit, np * page), *tp = tab.ptr(a, I32, (big)ns * mp),
+       *lp = len.ptr(a, I32, ns), *kdp = kd.ptr(a, el.bit, nd * page),
+       *vdp = vd.ptr(a, el.bit, nd * page), *dtp = dtab.ptr(a, I32, (big)ns * md),
+       *ixp = idx.ptr(a, I32, heads * budget), *nlp = nl.ptr(a, I32, ns),
+       *aop = ao.ptr(a, F32, heads * oc);
+  return finish(a, [&] {
+    return fn(kEvict, &spot_cache_evict)(fp(ap), kpp, vpp, ip(tp), np, ps, mp, ip(lp), ns, hkv, d,
+                                         budget, sink, recent, kdp, vdp, ip(dtp), nd, md,
+                                         static_cast<int32_t*>(ixp), static_cast<int32_t*>(nlp),
+                                         static_cast<float*>(aop), oc, st);
+  });
+}
+
 // A tensor without storage or of a wrapped kind throws from its accessors:
 // the Python path then raises as it always did.
 template <PyObject* (*F)(Args)>
@@ -515,6 +734,11 @@ PyMethodDef methods[] = {{"init", init, METH_VARARGS, nullptr},
                          SPOT_ENTRY(sparse_prefill),
                          SPOT_ENTRY(decode_step),
                          SPOT_ENTRY(decode_step_static),
+                         SPOT_ENTRY(rotary),
+                         SPOT_ENTRY(rotary_append),
+                         SPOT_ENTRY(paged_attend),
+                         SPOT_ENTRY(paged_weights),
+                         SPOT_ENTRY(cache_evict),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods};
 

@@ -1,0 +1,287 @@
+// Shared by the operators on a paged cache (gfx950): element types, the rows of
+// a chunk and what they see, the scores' cap and distance bias, page look-up, and
+// the division of the attention's work among workgroups.
+//
+// A sequence's new tokens and the G query heads that share a KV head form the
+// rows of one matrix: row j is token j / G, head j % G of the group, so a tile of
+// rows reads each key once for all its heads, whatever G is.
+#pragma once
+
+#include "spot_internal.h"
+
+#include "paged_map.h"
+
+namespace spot {
+namespace paged {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// Element types.  c + A B of 16x16 tiles: lane l holds 8 (mfma32) or 4 (mfma16)
+// consecutive k of row l%16 of A (column l%16 of B) from k = 8(l/16) or 4(l/16),
+// and rows 4(l/16) ..+3 of column l%16 of c.  pack2 rounds to nearest even.
+struct Bf16 {
+  // Largest probability before rounding: the reference maximum itself.
+  static constexpr float kShift = 0.f, kLazy = 8.f;
+  static __device__ __forceinline__ f32x4 mfma32(const u32x4& a, const u32x4& b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 mfma16(s16x4 a, s16x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack2(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2_t));
+  }
+  static __device__ __forceinline__ float lo(uint32_t x) { return bf16_lo(x); }
+  static __device__ __forceinline__ float hi(uint32_t x) { return bf16_hi(x); }
+  static __device__ __forceinline__ float one(uint16_t x) { return bf16_lo(x); }
+  static __device__ __forceinline__ uint16_t round(float x) { return (uint16_t)pack2(x, 0.f); }
+  static constexpr uint32_t kExponent = 0x7f80u;   // all ones: infinite or NaN
+};
+struct Fp16 {
+  // FP16 has 24 bits below 1, FP32's exponentials many more: probabilities are
+  // kept 2^10 times larger (the reference lies 10 below the maximum), so that
+  // many small ones still count; 2^14 at most, below FP16's largest number.
+  static constexpr float kShift = 10.f, kLazy = 4.f;
+  static __device__ __forceinline__ f32x4 mfma32(const u32x4& a, const u32x4& b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 mfma16(s16x4 a, s16x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, a),
+                                                 __builtin_bit_cast(f16x4, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack2(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
+  }
+  static __device__ __forceinline__ float lo(uint32_t x) {
+    return (float)__builtin_bit_cast(f16x2, x)[0];
+  }
+  static __device__ __forceinline__ float hi(uint32_t x) {
+    return (float)__builtin_bit_cast(f16x2, x)[1];
+  }
+  static __device__ __forceinline__ float one(uint16_t x) { return lo(x); }
+  static __device__ __forceinline__ uint16_t round(float x) { return (uint16_t)pack2(x, 0.f); }
+  static constexpr uint32_t kExponent = 0x7c00u;
+};
+
+// Wait states between matrix instructions and the ordinary ones that read their
+// results.  The compiler (ROCm 7.2) puts 8 after a chain of dependent MFMAs whose last
+// result lands in other registers than its addend, and then scores came back without
+// the chain's last product; 13 were enough, here are 16 more.
+__device__ __forceinline__ void settle(f32x4& a) { asm volatile("s_nop 15" : "+v"(a)); }
+__device__ __forceinline__ void settle(f32x4 (&a)[4]) {
+  asm volatile("s_nop 15" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]));
+}
+__device__ __forceinline__ void settle(f32x4 (&a)[8]) {
+  asm volatile("s_nop 15"
+               : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(a[4]), "+v"(a[5]),
+                 "+v"(a[6]), "+v"(a[7]));
+}
+
+// Whether one of a pair of elements is infinite or NaN, and the pair with such
+// elements zero.
+template <class T>
+__device__ __forceinline__ bool odd2(uint32_t x) {
+  return (~x & T::kExponent) == 0u || (~x & (T::kExponent << 16)) == 0u;
+}
+template <class T>
+__device__ __forceinline__ uint32_t clean2(uint32_t x) {
+  if ((~x & T::kExponent) == 0u) x &= 0xffff0000u;
+  if ((~x & (T::kExponent << 16)) == 0u) x &= 0xffffu;
+  return x;
+}
+
+// tanh to 2e-7 relative: e^(-2|y|) beyond 0.3, where 1 - e keeps its bits, and the
+// Taylor polynomial below (its first dropped term is 5e-8 there).
+__device__ __forceinline__ float tanh_f(float y) {
+  const float a = fabsf(y), z = y * y;
+  const float e = __builtin_amdgcn_exp2f(a * (-2.f * kLog2e));
+  const float far = copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), y);
+  const float near =
+      y * fmaf(fmaf(fmaf(fmaf(62.f / 2835, z, -17.f / 315), z, 2.f / 15), z, -1.f / 3), z, 1.f);
+  return a < 0.3f ? near : far;
+}
+
+// Scores in the log2 domain.  With neither cap nor bias: s * mul.
+template <bool CAP, bool BIAS>
+struct Scores {
+  float mul, cap2, slope2;   // scale log2e, or scale / cap; cap log2e; slope log2e
+  float p;                   // the row's position
+  __device__ __forceinline__ Scores() {}
+  __device__ __forceinline__ Scores(const Rule& u, const Seq& q, int i, int head) {
+    mul = CAP ? u.scale / u.cap : u.scale * kLog2e;
+    cap2 = u.cap * kLog2e;
+    slope2 = BIAS ? u.slopes[head] * kLog2e : 0.f;
+    p = (float)(q.len - q.n + i);
+  }
+  __device__ __forceinline__ float operator()(float s, float t) const {
+    float x = CAP ? cap2 * tanh_f(s * mul) : s * mul;
+    if (BIAS) x = fmaf(-slope2, fabsf(p - t), x);
+    return x;
+  }
+};
+
+// ------------------------------------------------------- division of work
+// Work is counted in (row tile, KV head, 64-key block) steps.  A tile whose keys
+// are more than 1/kTarget of all steps is split along the keys, so that a long
+// sequence among short ones, or few rows over a long cache, still fill the
+// device; the parts of a tile are joined by the last one to finish.  Every
+// workgroup finds its own part from the lengths on the device, so the host needs
+// none of them and a captured call stays right when they change.
+constexpr int kTarget = 512;                 // two workgroups per CU
+constexpr int kMaxParts = 2 * kTarget + 64;  // parts of split tiles (each has at most twice its share)
+constexpr int kMaxSplit = kTarget + 64;      // split tiles
+
+struct Part {
+  int s, tile;        // sequence (-1: no work), row tile
+  int split, n_split; // part and number of parts of the tile
+  int slot, counter;  // workspace slot of part 0, completion counter (n_split > 1)
+  Seq q;
+};
+
+// Blocks of 64 keys that the rows of a sequence see at most (documents aside).
+__device__ __forceinline__ int span_blocks(const Seq& q, int window, int cap) {
+  const int hi = min(q.len, cap), p0 = q.len - q.n;
+  const int lo = window > 0 && window <= p0 ? p0 - window + 1 : 0;
+  return hi > lo ? (hi + 63) / 64 - lo / 64 : 0;
+}
+
+// The part of unit `unit` (of the parts of all tiles of TR rows, one KV head),
+// found by one wave; every lane gets it.  min_blocks: fewest blocks of a part.
+template <int TR>
+__device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
+                                          const int32_t* seq_len, int n_seq, int rows, int G,
+                                          int h_kv, int window, int cap, int min_blocks) {
+  const int lane = __lane_id();
+  auto tiles_of = [&](const Seq& q) { return (int)(((int64_t)q.n * G + TR - 1) / TR); };
+  // all steps
+  float steps = 0.f;
+  Seq q0 = {0, 0, 0};
+  for (int base = 0; base < n_seq; base += 64) {
+    Seq q = {0, 0, 0};
+    if (base + lane < n_seq) q = sequence(seq_start, seq_len, base + lane, rows);
+    if (base == 0) q0 = q;
+    steps += wave_sum((float)tiles_of(q) * (float)span_blocks(q, window, cap));
+  }
+  const int per = max(min_blocks, (int)ceilf(steps * (float)h_kv / (float)kTarget));
+  // the sequence that holds the unit
+  Part r;
+  r.s = -1;
+  int unit0 = 0, slot0 = 0, cnt0 = 0;
+  for (int base = 0; base < n_seq; base += 64) {
+    Seq q = q0;
+    if (base) {
+      q = Seq{0, 0, 0};
+      if (base + lane < n_seq) q = sequence(seq_start, seq_len, base + lane, rows);
+    }
+    const int T = tiles_of(q), nb = span_blocks(q, window, cap);
+    const int ns = max(1, (nb + per - 1) / per);
+    const int units = T * ns;
+    const int incl = wave_incl_scan_i(units);
+    const int split_units = ns > 1 ? units : 0, split_tiles = ns > 1 ? T : 0;
+    const int si = wave_incl_scan_i(split_units), ti = wave_incl_scan_i(split_tiles);
+    const uint64_t hit = __ballot(unit >= unit0 + incl - units && unit < unit0 + incl);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      const int in = unit - unit0 - __builtin_amdgcn_readlane(incl - units, l);
+      const int n_tiles = __builtin_amdgcn_readlane(T, l);
+      r.n_split = __builtin_amdgcn_readlane(ns, l);
+      r.s = base + l;
+      r.tile = n_tiles - 1 - in / r.n_split;       // the longest first
+      r.split = in % r.n_split;
+      r.slot = slot0 + __builtin_amdgcn_readlane(si - split_units, l) + in - r.split;
+      r.counter = cnt0 + __builtin_amdgcn_readlane(ti - split_tiles, l) + in / r.n_split;
+      r.q.start = __builtin_amdgcn_readlane(q.start, l);
+      r.q.n = __builtin_amdgcn_readlane(q.n, l);
+      r.q.len = __builtin_amdgcn_readlane(q.len, l);
+      return r;
+    }
+    unit0 += __builtin_amdgcn_readlane(incl, 63);
+    slot0 += __builtin_amdgcn_readlane(si, 63);
+    cnt0 += __builtin_amdgcn_readlane(ti, 63);
+  }
+  return r;
+}
+
+// Workspace of the attention: completion counters (zero between calls, at the same
+// place for every size), then the parts' (m, l) and O.
+struct Workspace {
+  unsigned* counters;   // [kMaxSplit]
+  float* ml;            // [kMaxParts, TR, 2]
+  float* o;             // [kMaxParts, TR, d]
+};
+constexpr size_t kCounterBytes = (kMaxSplit * sizeof(unsigned) + 255) / 256 * 256;
+
+struct AttendArgs {
+  const uint16_t *q, *k, *v;
+  Pages pages;
+  const int32_t *seq_start, *seq_len;
+  int n_seq, rows, h_q, h_kv;
+  Rule rule;
+  uint16_t* out;
+  float* lse;
+  Workspace ws;
+};
+// ws as attend_few_workspace sizes it.
+hipError_t launch_attend_few(AttendArgs a, int dtype, int d, void* ws, hipStream_t s);
+size_t attend_few_workspace(int d);
+
+struct WeightArgs {
+  const uint16_t* q;
+  const float* lse;
+  const uint16_t* k;
+  Pages pages;
+  const int32_t *seq_start, *seq_len;
+  int n_seq, rows, h_q, h_kv;
+  Rule rule;
+  const float* acc;     // [n_seq, h_kv, cap] or NULL (0)
+  float decay;
+  float* acc_out;
+};
+hipError_t launch_weights(const WeightArgs& a, int dtype, int d, hipStream_t s);
+
+struct EvictArgs {
+  const float* acc;     // [n_seq, h_kv, cap]
+  const uint16_t *k, *v;
+  Pages pages;
+  const int32_t* seq_len;
+  int n_seq, h_kv, d, budget, n_sink, n_recent;
+  uint16_t *k_dst, *v_dst;
+  Pages dst;            // of the same page size
+  int32_t *idx, *new_len;
+  float* acc_out;       // [n_seq, h_kv, out_cap]
+  int out_cap;
+};
+hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
+
+constexpr int kMaxPairs = 128;        // rotary pairs of a head
+struct PairFreq {
+  double f[kMaxPairs];
+};
+struct RotaryArgs {
+  const uint16_t *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride, out_stride;   // elements from row to row
+  const int32_t* pos;
+  uint16_t *q_out, *k_pages, *v_pages;                // k_pages NULL: q alone
+  Pages pages;
+  const int32_t *seq_start, *seq_len;
+  int n_seq, rows, h_q, h_kv, d, rope_dim;
+  float amp;
+  bool inverse;
+  PairFreq freq;
+};
+hipError_t launch_rotary(const RotaryArgs& a, int dtype, bool interleaved, hipStream_t s);
+
+}  // namespace paged
+}  // namespace spot

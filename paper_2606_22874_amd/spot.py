@@ -43,6 +43,9 @@ SYMBOLS = ["spot_status_str", "spot_version", "spot_selector_score",
            "spot_sparse_prefill", "spot_decode_step_workspace_bytes", "spot_decode_step",
            "spot_decode_step_q", "spot_decode_step_static", "spot_decode_step_status",
            "spot_test_force_expiry",
+           "spot_rope_frequencies", "spot_rotary", "spot_rotary_append",
+           "spot_paged_workspace_bytes", "spot_paged_attend", "spot_paged_weights",
+           "spot_cache_evict",
            "spot_probe_stream_read", "spot_probe_sink_words"]
 
 
@@ -71,6 +74,7 @@ def load(path: Optional[str] = None):
                   "`python -m paper_2606_22874_amd.build`", file=sys.stderr)
         L = ctypes.CDLL(so)
         P, I, F, Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+        Q, D = ctypes.c_int64, ctypes.c_double
         L.spot_status_str.argtypes = [I]
         L.spot_status_str.restype = ctypes.c_char_p
         L.spot_version.restype = ctypes.c_char_p
@@ -101,6 +105,18 @@ def load(path: Optional[str] = None):
         L.spot_decode_step_status.argtypes = [P, Z, I, I, I, I, I, P]
         L.spot_test_force_expiry.argtypes = [I]
         L.spot_test_force_expiry.restype = None
+        L.spot_rope_frequencies.argtypes = [I, D, I, D, I, D, D, P]
+        L.spot_rotary.argtypes = [P, Q, P, I, I, I, I, P, F, I, I, P, Q, P]
+        L.spot_rotary_append.argtypes = [P, Q, P, Q, P, Q, I, P, P, I, I, I, P, P, I, I, I, I, I, I,
+                                         P, F, I, P, P, P, P]
+        L.spot_paged_workspace_bytes.argtypes = [I, I, I, I, I]
+        L.spot_paged_workspace_bytes.restype = Z
+        L.spot_paged_attend.argtypes = [P, I, P, P, P, I, I, I, P, P, I, I, I, I, I, F, F, P, I, P,
+                                        P, P, P, P, Z, P]
+        L.spot_paged_weights.argtypes = [P, P, I, P, P, I, I, I, P, P, I, I, I, I, I, F, F, P, I,
+                                         P, P, P, F, P, P]
+        L.spot_cache_evict.argtypes = [P, P, P, P, I, I, I, P, I, I, I, I, I, I, P, P, P, I, I, P,
+                                       P, P, I, P]
         L.spot_probe_stream_read.argtypes = [P, Z, P, P]
         L.spot_probe_stream_read.restype = ctypes.c_int32
         L.spot_probe_sink_words.restype = I
@@ -110,7 +126,9 @@ def load(path: Optional[str] = None):
                      "spot_selector_pool", "spot_select_blocks", "spot_sparse_decode",
                      "spot_sparse_decode_blk",
                      "spot_dense_decode", "spot_sparse_prefill", "spot_decode_step",
-                     "spot_decode_step_q", "spot_decode_step_static", "spot_decode_step_status"):
+                     "spot_decode_step_q", "spot_decode_step_static", "spot_decode_step_status",
+                     "spot_rope_frequencies", "spot_rotary", "spot_rotary_append",
+                     "spot_paged_attend", "spot_paged_weights", "spot_cache_evict"):
             getattr(L, name).restype = ctypes.c_int32
         if path is None:
             _load_native(L)
@@ -131,7 +149,8 @@ def _load_native(L):
                  L.spot_selector_project, L.spot_selector_project_pooled, L.spot_selector_pool,
                  L.spot_select_blocks, L.spot_sparse_decode_blk, L.spot_dense_decode,
                  L.spot_sparse_prefill, L.spot_decode_step, L.spot_decode_step_q,
-                 L.spot_decode_step_static)
+                 L.spot_decode_step_static, L.spot_rotary, L.spot_rotary_append,
+                 L.spot_paged_attend, L.spot_paged_weights, L.spot_cache_evict)
         _binding.init(tuple(ctypes.cast(f, ctypes.c_void_p).value for f in order),
                       torch.cuda.Stream)
         _native = _binding
@@ -175,6 +194,11 @@ BF16 = (torch.bfloat16, torch.int16)
 I32 = (torch.int32,)
 F32 = (torch.float32,)
 U8 = (torch.uint8,)
+
+
+PAGED_DTYPE = {torch.bfloat16: 0, torch.float16: 1}
+ROPE_SCALING = {"none": 0, "linear": 1, "ntk": 2, "parts": 3, "yarn": 3}
+ROPE_INTERLEAVED, ROPE_INVERSE = 1, 2
 
 
 def _check(fn: str, st: int):
@@ -558,6 +582,217 @@ def spot_test_force_expiry(on: bool):
     load().spot_test_force_expiry(1 if on else 0)
 
 
+# --------------------------------------------------- operators on a paged cache
+def _same_device(stream, *tensors):
+    """The device of every tensor given, and its stream: the stream passed, or the
+    device's current one."""
+    dev = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device}")
+    if isinstance(stream, torch.cuda.Stream) and stream.device != dev:
+        raise ValueError(f"a stream of {stream.device} for tensors on {dev}")
+    return dev, _stream(torch.cuda.current_stream(dev) if stream is None else stream)
+
+
+def _element(t, name):
+    """The SPOT_DTYPE of a tensor."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.dtype not in PAGED_DTYPE:
+        raise ValueError(f"{name}: dtype {t.dtype} not in {tuple(PAGED_DTYPE)}")
+    return PAGED_DTYPE[t.dtype]
+
+
+def _opt(t, name, dtypes, numel):
+    if t is not None:
+        _dev(t, name, dtypes, numel)
+
+
+def _row_tensor(t, name, dtype, rows, stride, row):
+    """Rows of `row` elements, `stride` apart, inside the tensor's storage."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype} is not {dtype}")
+    left = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+    if rows > 0 and (rows - 1) * stride + row > left:
+        raise ValueError(f"{name}: {left} elements, need {(rows - 1) * stride + row}")
+
+
+def _freq(freq, rope_dim):
+    if not isinstance(freq, torch.Tensor) or freq.device.type != "cpu" or \
+            freq.dtype != torch.float64 or not freq.is_contiguous():
+        raise ValueError("freq must be a contiguous float64 host tensor")
+    if freq.numel() < rope_dim // 2:
+        raise ValueError(f"freq: {freq.numel()} elements, need {rope_dim // 2}")
+
+
+def spot_rope_frequencies(rope_dim, rope_base, scaling, factor, orig_len, low, high, freq):
+    _freq(freq, rope_dim)
+    _check("spot_rope_frequencies", load().spot_rope_frequencies(
+        rope_dim, float(rope_base), scaling, float(factor), orig_len, float(low), float(high),
+        _ptr(freq)))
+
+
+def spot_rotary(x, x_stride, pos, rows, heads, d, rope_dim, freq, amp, flags, out, out_stride,
+                stream=None):
+    if _native is not None:
+        st = _native.rotary(x, x_stride, pos, rows, heads, d, rope_dim, freq, amp, flags, out,
+                            out_stride, stream)
+        if st is not None:
+            return _check("spot_rotary", st)
+    dt = _element(x, "x")
+    _row_tensor(x, "x", x.dtype, rows, x_stride, heads * d)
+    _dev(pos, "pos", I32, rows)
+    _freq(freq, rope_dim)
+    _row_tensor(out, "out", x.dtype, rows, out_stride, heads * d)
+    dev, s = _same_device(stream, x, pos, out)
+    with torch.cuda.device(dev):
+        _check("spot_rotary", load().spot_rotary(
+            _ptr(x), x_stride, _ptr(pos), rows, heads, d, rope_dim, _ptr(freq), float(amp), flags,
+            dt, _ptr(out), out_stride, s))
+
+
+def spot_rotary_append(q, q_stride, k, k_stride, v, v_stride, pos, page_table, n_pages, page_size,
+                       max_pages, seq_start, seq_len, n_seq, rows, h_q, h_kv, d, rope_dim, freq,
+                       amp, flags, q_out, k_pages, v_pages, stream=None):
+    if _native is not None:
+        st = _native.rotary_append(q, q_stride, k, k_stride, v, v_stride, pos, page_table, n_pages,
+                                   page_size, max_pages, seq_start, seq_len, n_seq, rows, h_q,
+                                   h_kv, d, rope_dim, freq, amp, flags, q_out, k_pages, v_pages,
+                                   stream)
+        if st is not None:
+            return _check("spot_rotary_append", st)
+    dt = _element(q, "q")
+    el = (q.dtype,)
+    _row_tensor(q, "q", q.dtype, rows, q_stride, h_q * d)
+    _row_tensor(k, "k", q.dtype, rows, k_stride, h_kv * d)
+    _row_tensor(v, "v", q.dtype, rows, v_stride, h_kv * d)
+    _opt(pos, "pos", I32, rows)
+    _dev(page_table, "page_table", I32, n_seq * max_pages)
+    _dev(seq_start, "seq_start", I32, n_seq + 1)
+    _dev(seq_len, "seq_len", I32, n_seq)
+    _freq(freq, rope_dim)
+    _dev(q_out, "q_out", el, rows * h_q * d)
+    _dev(k_pages, "k_pages", el, n_pages * h_kv * page_size * d)
+    _dev(v_pages, "v_pages", el, n_pages * h_kv * page_size * d)
+    dev, s = _same_device(stream, q, k, v, pos, page_table, seq_start, seq_len, q_out, k_pages,
+                          v_pages)
+    with torch.cuda.device(dev):
+        _check("spot_rotary_append", load().spot_rotary_append(
+            _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, dt, _ptr(pos),
+            _ptr(page_table), n_pages, page_size, max_pages, _ptr(seq_start), _ptr(seq_len),
+            n_seq, rows, h_q, h_kv, d, rope_dim, _ptr(freq), float(amp), flags, _ptr(q_out),
+            _ptr(k_pages), _ptr(v_pages), s))
+
+
+def spot_paged_workspace_bytes(n_seq, rows, h_q, h_kv, d) -> int:
+    return int(load().spot_paged_workspace_bytes(n_seq, rows, h_q, h_kv, d))
+
+
+def spot_paged_attend(q, k_pages, v_pages, page_table, n_pages, page_size, max_pages, seq_start,
+                      seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes, window,
+                      prefix, first, out, lse, ws, stream=None):
+    if _native is not None:
+        st = _native.paged_attend(q, k_pages, v_pages, page_table, n_pages, page_size, max_pages,
+                                  seq_start, seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap,
+                                  slopes, window, prefix, first, out, lse, ws, stream)
+        if st is not None:
+            return _check("spot_paged_attend", st)
+    dt = _element(q, "q")
+    el = (q.dtype,)
+    _dev(q, "q", el, rows * h_q * d)
+    _dev(k_pages, "k_pages", el, n_pages * h_kv * page_size * d)
+    _dev(v_pages, "v_pages", el, n_pages * h_kv * page_size * d)
+    _dev(page_table, "page_table", I32, n_seq * max_pages)
+    _dev(seq_start, "seq_start", I32, n_seq + 1)
+    _dev(seq_len, "seq_len", I32, n_seq)
+    _opt(slopes, "slopes", F32, h_q)
+    _opt(prefix, "prefix", I32, n_seq)
+    _opt(first, "first", I32, rows)
+    _dev(out, "out", el, rows * h_q * d)
+    _opt(lse, "lse", F32, rows * h_q)
+    _dev(ws, "ws", None)
+    dev, s = _same_device(stream, q, k_pages, v_pages, page_table, seq_start, seq_len, slopes,
+                          prefix, first, out, lse, ws)
+    with torch.cuda.device(dev):
+        _check("spot_paged_attend", load().spot_paged_attend(
+            _ptr(q), dt, _ptr(k_pages), _ptr(v_pages), _ptr(page_table), n_pages, page_size,
+            max_pages, _ptr(seq_start), _ptr(seq_len), n_seq, rows, h_q, h_kv, d, float(sm_scale),
+            float(softcap), _ptr(slopes), window, _ptr(prefix), _ptr(first), _ptr(out), _ptr(lse),
+            _ptr(ws), ws.numel() * ws.element_size(), s))
+
+
+def spot_paged_weights(q, lse, k_pages, page_table, n_pages, page_size, max_pages, seq_start,
+                       seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes, window,
+                       prefix, first, acc, decay, acc_out, stream=None):
+    if _native is not None:
+        st = _native.paged_weights(q, lse, k_pages, page_table, n_pages, page_size, max_pages,
+                                   seq_start, seq_len, n_seq, rows, h_q, h_kv, d, sm_scale,
+                                   softcap, slopes, window, prefix, first, acc, decay, acc_out,
+                                   stream)
+        if st is not None:
+            return _check("spot_paged_weights", st)
+    dt = _element(q, "q")
+    el = (q.dtype,)
+    _dev(q, "q", el, rows * h_q * d)
+    _dev(lse, "lse", F32, rows * h_q)
+    _dev(k_pages, "k_pages", el, n_pages * h_kv * page_size * d)
+    _dev(page_table, "page_table", I32, n_seq * max_pages)
+    _dev(seq_start, "seq_start", I32, n_seq + 1)
+    _dev(seq_len, "seq_len", I32, n_seq)
+    _opt(slopes, "slopes", F32, h_q)
+    _opt(prefix, "prefix", I32, n_seq)
+    _opt(first, "first", I32, rows)
+    _opt(acc, "acc", F32, n_seq * h_kv * max_pages * page_size)
+    _dev(acc_out, "acc_out", F32, n_seq * h_kv * max_pages * page_size)
+    dev, s = _same_device(stream, q, lse, k_pages, page_table, seq_start, seq_len, slopes, prefix,
+                          first, acc, acc_out)
+    with torch.cuda.device(dev):
+        _check("spot_paged_weights", load().spot_paged_weights(
+            _ptr(q), _ptr(lse), dt, _ptr(k_pages), _ptr(page_table), n_pages, page_size, max_pages,
+            _ptr(seq_start), _ptr(seq_len), n_seq, rows, h_q, h_kv, d, float(sm_scale),
+            float(softcap), _ptr(slopes), window, _ptr(prefix), _ptr(first), _ptr(acc),
+            float(decay), _ptr(acc_out), s))
+
+
+def spot_cache_evict(acc, k_pages, v_pages, page_table, n_pages, page_size, max_pages, seq_len,
+                     n_seq, h_kv, d, budget, n_sink, n_recent, k_dst, v_dst, dst_table,
+                     n_dst_pages, dst_max_pages, idx, new_len, acc_out, out_cap, stream=None):
+    if _native is not None:
+        st = _native.cache_evict(acc, k_pages, v_pages, page_table, n_pages, page_size, max_pages,
+                                 seq_len, n_seq, h_kv, d, budget, n_sink, n_recent, k_dst, v_dst,
+                                 dst_table, n_dst_pages, dst_max_pages, idx, new_len, acc_out,
+                                 out_cap, stream)
+        if st is not None:
+            return _check("spot_cache_evict", st)
+    _element(k_pages, "k_pages")
+    el = (k_pages.dtype,)
+    page = h_kv * page_size * d
+    _dev(acc, "acc", F32, n_seq * h_kv * max_pages * page_size)
+    _dev(k_pages, "k_pages", el, n_pages * page)
+    _dev(v_pages, "v_pages", el, n_pages * page)
+    _dev(page_table, "page_table", I32, n_seq * max_pages)
+    _dev(seq_len, "seq_len", I32, n_seq)
+    _dev(k_dst, "k_dst", el, n_dst_pages * page)
+    _dev(v_dst, "v_dst", el, n_dst_pages * page)
+    _dev(dst_table, "dst_table", I32, n_seq * dst_max_pages)
+    _dev(idx, "idx", I32, n_seq * h_kv * budget)
+    _dev(new_len, "new_len", I32, n_seq)
+    _dev(acc_out, "acc_out", F32, n_seq * h_kv * out_cap)
+    dev, s = _same_device(stream, acc, k_pages, v_pages, page_table, seq_len, k_dst, v_dst,
+                          dst_table, idx, new_len, acc_out)
+    with torch.cuda.device(dev):
+        _check("spot_cache_evict", load().spot_cache_evict(
+            _ptr(acc), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), n_pages, page_size,
+            max_pages, _ptr(seq_len), n_seq, h_kv, d, budget, n_sink, n_recent, _ptr(k_dst),
+            _ptr(v_dst), _ptr(dst_table), n_dst_pages, dst_max_pages, _ptr(idx), _ptr(new_len),
+            _ptr(acc_out), out_cap, s))
+
+
 def spot_probe_stream_read(buf, sink, stream=None):
     _dev(buf, "buf", None)
     _dev(sink, "sink", F32, int(load().spot_probe_sink_words()))
@@ -707,6 +942,124 @@ def decode_step(q_sel, w, k_sel, q, k, v, seq_len, rule, k_scale=None, kfmt="bf1
                      d, l_cap, sm_scale, scores, idx, count, mass, out, lse, ws, stream,
                      q_scale=q_scale, qfmt=qfmt)
     return scores, idx, count, mass, out, lse
+
+
+# ----------------------------------------------- paged cache, allocating wrappers
+def rope_frequencies(rope_dim, base=1.0e6, scaling="none", factor=1.0, orig_len=0, low=1.0,
+                     high=32.0):
+    """Rotary frequencies (float64 host tensor [rope_dim / 2], kept by the caller) and
+    the factor on sine and cosine.  scaling: "none", "linear", "ntk" (the base grows),
+    "parts" (by the turns of a pair over orig_len tokens, low and high), "yarn" (by
+    parts, with YaRN's factor 0.1 ln(factor) + 1)."""
+    if scaling not in ROPE_SCALING:
+        raise ValueError(f"scaling {scaling!r} not in {tuple(ROPE_SCALING)}")
+    freq = torch.empty(max(int(rope_dim), 0) // 2, dtype=torch.float64)
+    spot_rope_frequencies(rope_dim, base, ROPE_SCALING[scaling], factor, orig_len, low, high, freq)
+    return freq, 0.1 * math.log(factor) + 1.0 if scaling == "yarn" else 1.0
+
+
+def _strides(t, name):
+    """Row stride of [rows, heads, d] whose heads lie one after the other."""
+    rows, heads, d = t.shape
+    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}: the heads of a row must lie one after the other")
+    return t.stride(0) if rows > 1 else heads * d
+
+
+def rotary(x, pos, freq, amp=1.0, interleaved=False, inverse=False, out=None, stream=None):
+    """Rotary positions of x [rows, heads, d] (rows may be strided): the first
+    2 len(freq) elements of each head, pairs (i, i + len(freq)) or neighbours.
+    inverse: by the negative angles (also the gradient of the rotation)."""
+    rows, heads, d = x.shape
+    if out is None:
+        out = torch.empty((rows, heads, d), dtype=x.dtype, device=x.device)
+    spot_rotary(x, _strides(x, "x"), pos, rows, heads, d, 2 * freq.numel(), freq, amp,
+                (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_INVERSE if inverse else 0), out,
+                _strides(out, "out"), stream)
+    return out
+
+
+def rotary_append(q, k, v, k_pages, v_pages, page_table, seq_start, seq_len, freq, amp=1.0,
+                  interleaved=False, pos=None, q_out=None, stream=None):
+    """Rotates q [rows, h_q, d] into q_out and k [rows, h_kv, d] into the pages of a
+    paged cache (see spot_paged_attend), and stores v beside it; returns q_out."""
+    rows, h_q, d = q.shape
+    n_pages, h_kv, page, _ = k_pages.shape
+    if q_out is None:
+        q_out = torch.empty((rows, h_q, d), dtype=q.dtype, device=q.device)
+    spot_rotary_append(q, _strides(q, "q"), k, _strides(k, "k"), v, _strides(v, "v"), pos,
+                       page_table, n_pages, page, page_table.shape[1], seq_start, seq_len,
+                       seq_len.shape[0], rows, h_q, h_kv, d, 2 * freq.numel(), freq, amp,
+                       ROPE_INTERLEAVED if interleaved else 0, q_out, k_pages, v_pages, stream)
+    return q_out
+
+
+def paged_workspace(n_seq, rows, h_q, h_kv, d, device="cuda"):
+    """Zero-filled workspace of paged_attend (each call leaves it ready for the next)."""
+    n = spot_paged_workspace_bytes(n_seq, rows, h_q, h_kv, d)
+    return torch.zeros(max(n, 16), dtype=torch.uint8, device=device)
+
+
+def paged_attend(q, k_pages, v_pages, page_table, seq_start, seq_len, sm_scale=None, softcap=0.0,
+                 slopes=None, window=0, prefix=None, first=None, out=None, lse=None, ws=None,
+                 stream=None):
+    """Attention of the packed new tokens q [rows, h_q, d] of every sequence over its
+    pages; k_pages, v_pages [n_pages, h_kv, page_size, d], page_table [n_seq,
+    max_pages].  Returns (out [rows, h_q, d], lse [rows, h_q])."""
+    rows, h_q, d = q.shape
+    n_pages, h_kv, page, _ = k_pages.shape
+    n_seq, max_pages = page_table.shape
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(d)
+    if out is None:
+        out = torch.zeros((rows, h_q, d), dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.full((rows, h_q), -math.inf, dtype=torch.float32, device=q.device)
+    if ws is None:
+        ws = paged_workspace(n_seq, rows, h_q, h_kv, d, q.device)
+    spot_paged_attend(q, k_pages, v_pages, page_table, n_pages, page, max_pages, seq_start,
+                      seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes, window,
+                      prefix, first, out, lse, ws, stream)
+    return out, lse
+
+
+def paged_weights(q, lse, k_pages, page_table, seq_start, seq_len, sm_scale=None, softcap=0.0,
+                  slopes=None, window=0, prefix=None, first=None, acc=None, decay=1.0, out=None,
+                  stream=None):
+    """Attention weight each cached token received from q, summed per KV head, on top of
+    decay * acc: [n_seq, h_kv, max_pages * page_size] float32.  lse from paged_attend."""
+    rows, h_q, d = q.shape
+    n_pages, h_kv, page, _ = k_pages.shape
+    n_seq, max_pages = page_table.shape
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(d)
+    if out is None:
+        out = torch.empty((n_seq, h_kv, max_pages * page), dtype=torch.float32, device=q.device)
+    spot_paged_weights(q, lse, k_pages, page_table, n_pages, page, max_pages, seq_start, seq_len,
+                       n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes, window, prefix, first,
+                       acc, decay, out, stream)
+    return out
+
+
+def cache_evict(acc, k_pages, v_pages, page_table, seq_len, budget, n_sink, n_recent, k_dst, v_dst,
+                dst_table, idx=None, new_len=None, acc_out=None, stream=None):
+    """Keeps `budget` tokens of each sequence and KV head (sinks, recent ones and the
+    heaviest by acc) and copies them to the pages of dst_table; returns (idx [n_seq,
+    h_kv, budget], new_len [n_seq], acc_out [n_seq, h_kv, dst_max_pages * page_size])."""
+    n_pages, h_kv, page, d = k_pages.shape
+    n_seq, max_pages = page_table.shape
+    dev = k_pages.device
+    if idx is None:
+        idx = torch.empty((n_seq, h_kv, budget), dtype=torch.int32, device=dev)
+    if new_len is None:
+        new_len = torch.empty(n_seq, dtype=torch.int32, device=dev)
+    if acc_out is None:
+        acc_out = torch.empty((n_seq, h_kv, dst_table.shape[1] * page), dtype=torch.float32,
+                              device=dev)
+    spot_cache_evict(acc, k_pages, v_pages, page_table, n_pages, page, max_pages, seq_len, n_seq,
+                     h_kv, d, budget, n_sink, n_recent, k_dst, v_dst, dst_table, k_dst.shape[0],
+                     dst_table.shape[1], idx, new_len, acc_out, acc_out.shape[-1], stream)
+    return idx, new_len, acc_out
 
 
 # ------------------------------------------------------- host helpers
