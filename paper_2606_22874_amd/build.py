@@ -26,7 +26,8 @@ ARCH = "gfx950"
 
 SOURCES = ["api.hip", "api_paged.hip", "frontend.hip", "frontend_mfma.hip", "score.hip",
            "score_many.hip", "score_tokens.hip", "select.hip", "decode.hip", "step.hip",
-           "prefill.hip", "rotary.hip", "attend_few.hip", "weights.hip", "evict.hip", "probe.hip"]
+           "prefill.hip", "rotary.hip", "attend_few.hip", "attend_many.hip", "weights.hip",
+           "evict.hip", "probe.hip"]
 
 HIPCC_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",

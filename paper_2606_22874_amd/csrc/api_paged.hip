@@ -1,6 +1,7 @@
 // C ABI of the operators on a paged cache: argument validation, then kernel
 // launches.  Nothing is enqueued unless every argument check passes.
 #include <math.h>
+#include <stdlib.h>
 
 #include "paged_core.h"
 
@@ -43,6 +44,12 @@ spot_status check_rope(int d, int rope_dim, const double* freq, float amp, int f
   for (int i = 0; i < rope_dim / 2; ++i)
     if (!isfinite(freq[i])) return SPOT_ERR_UNSUPPORTED;
   return SPOT_OK;
+}
+
+// Which calls take tiles of 256 rows, and not of 16.
+bool attend_many_takes(int n_seq, int rows, int h_q, int h_kv) {
+  static const char* e = getenv("SPOT_MANY");
+  return (int64_t)rows * (h_q / h_kv) > (e ? atoi(e) : 64) * (int64_t)n_seq;
 }
 
 const uint16_t* in16(const void* p) { return static_cast<const uint16_t*>(p); }
@@ -161,7 +168,8 @@ spot_status spot_rotary_append(const void* q, int64_t q_stride, const void* k, i
 
 size_t spot_paged_workspace_bytes(int n_seq, int rows, int h_q, int h_kv, int d) {
   if (n_seq < 1 || rows < 1 || h_q < 1 || h_kv < 1 || d < 1) return 0;
-  return attend_few_workspace(d);
+  return attend_many_takes(n_seq, rows, h_q, h_kv) ? attend_many_workspace(d)
+                                                   : attend_few_workspace(d);
 }
 
 spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, const void* v_pages,
@@ -196,7 +204,9 @@ spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, con
   a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first};
   a.out = out16(out);
   a.lse = lse;
-  return from_hip(launch_attend_few(a, dtype, d, ws, static_cast<hipStream_t>(stream)));
+  return from_hip((attend_many_takes(n_seq, rows, h_q, h_kv) ? launch_attend_many
+                                                             : launch_attend_few)(
+      a, dtype, d, ws, static_cast<hipStream_t>(stream)));
 }
 
 spot_status spot_paged_weights(const void* q, const float* lse, int dtype, const void* k_pages,

@@ -231,9 +231,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
     };
     auto back = [&](int n, f32x4 s) {
       const int t0 = (c0 + n) * 64 + wave * 16;
+      const float ahead = (float)(sc.p - (t0 + 4 * kg));
       float x[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = sc(s[i], (float)(t0 + 4 * kg + i));
+      for (int i = 0; i < 4; ++i) x[i] = sc(s[i], ahead - (float)i);
       if (t0 < FLO || t0 + 16 > FHI || row_of(n) < 0) {
         const bool page = row_of(n) >= 0;
 #pragma unroll
@@ -414,13 +415,10 @@ void launch(const AttendArgs& a, dim3 grid, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_attend_few(AttendArgs a, int dtype, int d, void* ws, hipStream_t s) {
-  const int G = a.h_q / a.h_kv;
   a.ws.counters = static_cast<unsigned*>(ws);
   a.ws.ml = reinterpret_cast<float*>(static_cast<char*>(ws) + kCounterBytes);
   a.ws.o = a.ws.ml + (size_t)kMaxParts * kRows * 2;
-  // every tile in one part, and the parts that kTarget shares of the work add
-  const int64_t units = (int64_t)a.rows * G / kRows + a.n_seq + kTarget / a.h_kv + 2;
-  const dim3 grid((unsigned)(units * a.h_kv));
+  const dim3 grid(attend_grid<kRows>(a));
   if (dtype == SPOT_DTYPE_BF16)
     d == 128 ? launch<Bf16, 128>(a, grid, s) : launch<Bf16, 64>(a, grid, s);
   else

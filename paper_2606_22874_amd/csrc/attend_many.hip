@@ -1,0 +1,607 @@
+// Attention of many rows over a paged cache (gfx950): chunks and whole prompts.
+//
+// One workgroup of 8 waves takes one part of a tile of 256 rows (new tokens x the
+// query heads that share a KV head), 32 rows a wave; blocks of 64 keys pass through
+// LDS and are used by all waves.  The mathematics is that of attend_few.hip, with
+// S^T = K Q^T in 16x16x32 tiles (Q^T in registers for the whole key loop), the
+// softmax down the lanes' columns, and O^T += V^T P^T, P^T straight from the
+// accumulators (its keys permuted like those of the transposing LDS read of V).
+//
+// The matrix cores bound it, so the two waves of a SIMD alternate: waves 0-3 run
+// matrix instructions while waves 4-7 run their softmax, then the other way round,
+// separated by barriers; block t takes half periods 2t and 2t + 1:
+//   2t      waves 0-3: P V of block t-1, K Q of block t, then the copies of K(t+1) and
+//           V(t) into the other buffers;   waves 4-7: softmax of block t-1
+//   2t + 1  waves 0-3: softmax of block t; their copies land;   waves 4-7: P V, K Q
+// K and V go from memory to LDS 16 bytes a lane (1 KiB a wave instruction), rows
+// swizzled by 16-byte chunks against bank conflicts; each of the buffers is a
+// variable of its own and the loop is unrolled by two, so that the compiler can tell
+// the copies in flight from the reads.
+#include <type_traits>
+
+#include "decode_core.h"
+#include "paged_core.h"
+
+namespace spot {
+namespace paged {
+namespace {
+
+using dec::lanes_max_xor16;
+using dec::lanes_max_xor32;
+using dec::lanes_sum_xor16;
+using dec::lanes_sum_xor32;
+
+constexpr int kRows = 256;         // rows of a tile
+constexpr int kWaves = 8;
+constexpr int kMinBlocks = 4;      // fewest blocks of a part
+constexpr int kListBlocks = 512;   // blocks whose pages are looked up at once
+typedef __attribute__((address_space(3))) void lds_void;
+#define SPOT_INLINE __attribute__((always_inline))
+
+// Physical 16-byte chunk of logical chunk c of row r.  K is read one chunk of 16 rows
+// at a time, V 8 bytes of 8 rows at two neighbouring chunks.
+template <int D>
+__device__ __forceinline__ int swz_k(int r, int c) {
+  return c ^ (r & (D / 8 - 1));
+}
+template <int D>
+__device__ __forceinline__ int swz_v(int r, int c) {
+  return D == 128 ? c ^ ((r & 7) << 1) : c ^ (((r >> 1) & 3) << 1);
+}
+
+// Copies of a block of 64 rows by 4 waves: instruction u of wave w fills rows
+// R (4u + w) .. + R, R rows of 1 KiB, all of one group of 16 keys.
+template <int D, bool IS_K>
+struct Copy {
+  static constexpr int R = 1024 / (2 * D);       // 4 or 8 rows an instruction
+  static constexpr int N = 64 / R / 4;           // instructions of a wave
+  static constexpr int CH = D / 8;               // chunks of a row
+  static __device__ __forceinline__ int row(int u, int wave, int lane) {
+    return R * (4 * u + wave) + lane / CH;
+  }
+  static __device__ __forceinline__ void issue(const uint16_t* pool, const int* list,
+                                               unsigned char* dst, int wave, int lane) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int r = row(u, wave, lane), pc = lane % CH;
+      const int lc = IS_K ? swz_k<D>(r, pc) : swz_v<D>(r, pc);
+      const int group = R * (4 * u + wave) / 16;
+      const int at = __builtin_amdgcn_readfirstlane(list[group]);   // -1: a row of no use
+      const uint16_t* src = pool + (int64_t)(at < 0 ? 0 : at) * D;
+      const uint32_t off = (uint32_t)((r & 15) * D + lc * 8);
+      __builtin_amdgcn_global_load_lds(src + off, (lds_void*)(dst + (4 * u + wave) * 1024), 16, 0,
+                                       0);
+    }
+  }
+};
+
+__device__ __forceinline__ void wait_vm() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
+__device__ __forceinline__ float max4(f32x4 x) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x[0], x[1]),
+                                       __builtin_elementwise_maximum(x[2], x[3]));
+}
+
+template <class T, int D, bool CAP, bool BIAS>
+struct Wave {
+  static constexpr int RB = D * 2, KS = D / 32, DT = D / 16;
+  static constexpr bool PLAIN = !CAP && !BIAS;
+  u32x4 qf[KS][2];            // Q^T as the B operand [dims][16 rows]
+  f32x4 o[2][DT];
+  f32x4 s[2][4];              // scores, then probabilities, of the current block
+  u32x4 pb[2][2];             // the probabilities as the B operand
+  float m_run[2], l_run[2];
+  Scores<CAP, BIAS> sc[2];
+  int lo[2], hi[2];
+  int G, r16;
+
+  // S^T of one block; the K fragments of a step are read one step ahead.  The chunks'
+  // swizzle is an exclusive or: one address and immediates give all fragments (kept
+  // from the compiler's sight, which would hold one register for each).
+  __device__ __forceinline__ void qk(const unsigned char* Kt) {
+    u32x4 a[2][4];
+    int at = r16 * RB + (swz_k<D>(r16, G) << 4);
+    asm volatile("" : "+v"(at));
+    auto load = [&](int ks, int slot) {
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+        a[slot][kt] = *reinterpret_cast<const u32x4*>(Kt + (at ^ ks << 6) + kt * 16 * RB);
+    };
+    load(0, 0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int cur = ks & 1;
+      if (ks + 1 < KS) load(ks + 1, cur ^ 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int qt = 0; qt < 2; ++qt)
+          s[qt][kt] = T::mfma32(a[cur][kt], qf[ks][qt],
+                                ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[qt][kt]);
+    }
+  }
+
+  // O^T += V^T P^T of one block.  Lane (G, r16) of the transposing read addresses row
+  // 32 ks + 4 G + r16 / 4 (and 16 below), columns 4 (r16 % 4) .. +3 of the d tile, and
+  // gets column r16 of rows 4 G .. +3.
+  __device__ __forceinline__ void pv(const unsigned char* Vt) {
+    u32x4 a[2][DT];
+    const int r0 = 4 * G + (r16 >> 2);
+    int at = r0 * RB + (swz_v<D>(r0, (r16 & 3) >> 1) << 4) + (r16 & 1) * 8;
+    asm volatile("" : "+v"(at));
+    auto load = [&](int ks, int dt0) {
+#pragma unroll
+      for (int dt = dt0; dt < dt0 + 4; ++dt) {
+        const int off = (at ^ dt << 5) + 32 * ks * RB;
+        const u32x2 y0 = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                       (__attribute__((address_space(3))) s16x4*)(Vt + off)));
+        const u32x2 y1 = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                       (__attribute__((address_space(3))) s16x4*)(Vt + off + 16 * RB)));
+        a[ks][dt] = u32x4{y0[0], y0[1], y1[0], y1[1]};
+      }
+    };
+    auto mma = [&](int ks, int dt0) {
+#pragma unroll
+      for (int dt = dt0; dt < dt0 + 4; ++dt)
+#pragma unroll
+        for (int qt = 0; qt < 2; ++qt) o[qt][dt] = T::mfma32(a[ks][dt], pb[qt][ks], o[qt][dt]);
+    };
+    if constexpr (DT == 8) {
+      load(0, 0);
+      load(0, 4);
+      __builtin_amdgcn_sched_barrier(0);
+      mma(0, 0);
+      load(1, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      mma(0, 4);
+      load(1, 4);
+      __builtin_amdgcn_sched_barrier(0);
+      mma(1, 0);
+      mma(1, 4);
+    } else {
+      load(0, 0);
+      load(1, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      mma(0, 0);
+      mma(1, 0);
+    }
+  }
+
+  // Online softmax of the scores into pb.  MASK: some row does not see the whole block;
+  // pages: bit kt says that keys 16 kt .. are there.
+  template <bool MASK>
+  __device__ __forceinline__ void softmax(int t0, unsigned pages) {
+    asm volatile("s_nop 15"
+                 : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[0][2]), "+v"(s[0][3]), "+v"(s[1][0]),
+                   "+v"(s[1][1]), "+v"(s[1][2]), "+v"(s[1][3]));   // see settle()
+    const float c = PLAIN ? sc[0].mul : 1.f;    // positive
+    float mt[2];
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt) {
+      const float ahead = (float)(sc[qt].p - (t0 + 4 * G));
+      const int from = lo[qt] - (t0 + 4 * G), to = hi[qt] - (t0 + 4 * G);
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = s[qt][kt][i];
+          if (!PLAIN) x = sc[qt](x, ahead - (float)(16 * kt + i));
+          if (MASK && (!(pages >> kt & 1) || 16 * kt + i < from || 16 * kt + i >= to))
+            x = -INFINITY;
+          s[qt][kt][i] = x;
+        }
+      const float mx = __builtin_elementwise_maximum(
+          __builtin_elementwise_maximum(max4(s[qt][0]), max4(s[qt][1])),
+          __builtin_elementwise_maximum(max4(s[qt][2]), max4(s[qt][3])));
+      mt[qt] = lanes_max_xor16(lanes_max_xor32(mx)) * c - T::kShift;
+    }
+    // The reference maximum moves only when a column's grows by more than kLazy, so
+    // that most blocks leave O and l as they are.
+    if (__ballot(mt[0] > m_run[0] + T::kLazy || mt[1] > m_run[1] + T::kLazy)) {
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt) {
+        const float m_new = fmaxf(m_run[qt], mt[qt]);
+        const float alpha =
+            __builtin_amdgcn_exp2f(m_run[qt] - (m_new == -INFINITY ? 0.f : m_new));
+        m_run[qt] = m_new;
+        l_run[qt] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[qt][dt] *= alpha;
+      }
+    }
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt) {
+      const float mu = m_run[qt] == -INFINITY ? 0.f : m_run[qt];
+      float ps[4];
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          s[qt][kt][i] = __builtin_amdgcn_exp2f(PLAIN ? fmaf(s[qt][kt][i], c, -mu)
+                                                      : s[qt][kt][i] - mu);
+        ps[kt] = (s[qt][kt][0] + s[qt][kt][1]) + (s[qt][kt][2] + s[qt][kt][3]);
+      }
+      l_run[qt] += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+      // k entry 8 G + e is key 32 ks + 4 G + e for e < 4, and 16 further on from 4 on
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+        pb[qt][ks] = u32x4{T::pack2(s[qt][2 * ks][0], s[qt][2 * ks][1]),
+                           T::pack2(s[qt][2 * ks][2], s[qt][2 * ks][3]),
+                           T::pack2(s[qt][2 * ks + 1][0], s[qt][2 * ks + 1][1]),
+                           T::pack2(s[qt][2 * ks + 1][2], s[qt][2 * ks + 1][3])};
+    }
+  }
+};
+
+template <class T, int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) {
+  typedef Wave<T, D, CAP, BIAS> W;
+  typedef Copy<D, true> CopyK;
+  typedef Copy<D, false> CopyV;
+  constexpr int kTile = 64 * D * 2, DT = D / 16;
+  __shared__ __attribute__((aligned(16))) unsigned char sk0[kTile], sk1[kTile];
+  __shared__ __attribute__((aligned(16))) unsigned char sv0[kTile], sv1[kTile];
+  __shared__ int s_list[kListBlocks * 4];   // pool row of each 16-key group, -1 without a page
+  __shared__ int s_lim[kWaves][4];
+  __shared__ int s_missing, s_last, s_odd;
+  __shared__ float s_join[kRows][2];
+  __shared__ Part s_part;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int G = a.h_q / a.h_kv, g = blockIdx.x % a.h_kv;
+  const int cap = a.pages.cap();
+  if (wave == 0) {
+    const Part p = find_part<kRows>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len, a.n_seq, a.rows,
+                                    G, a.h_kv, a.rule.window, cap, kMinBlocks);
+    if (lane == 0) {
+      s_part = p;
+      s_odd = 0;
+    }
+  }
+  __syncthreads();
+  const Part pt = s_part;
+  if (pt.s < 0) return;
+
+  W w;
+  w.G = lane >> 4;
+  w.r16 = lane & 15;
+  const int64_t j0 = (int64_t)pt.tile * kRows, j_end = (int64_t)pt.q.n * G;
+  const int n_real = (int)min((int64_t)kRows, j_end - j0);
+  // row of q and out of the tile's row r
+  auto row_of = [&](int r) SPOT_INLINE {
+    const int64_t j = j0 + r;
+    return (size_t)(pt.q.start + (int)(j / G)) * a.h_q + g * G + (int)(j % G);
+  };
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt) {
+    const int r = wave * 32 + qt * 16 + w.r16;
+    const bool real = r < n_real;
+    const int64_t j = j0 + (real ? r : 0);
+    const int tok = (int)(j / G), head = g * G + (int)(j % G);
+    w.lo[qt] = w.hi[qt] = 0;
+    if (real) visible(a.rule, pt.q, pt.s, tok, cap, w.lo[qt], w.hi[qt]);
+    w.sc[qt] = Scores<CAP, BIAS>(a.rule, pt.q, tok, head);
+    const uint16_t* q = a.q + row_of(real ? r : 0) * D + 8 * w.G;
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) w.qf[ks][qt] = *reinterpret_cast<const u32x4*>(q + ks * 32);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) w.o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    w.m_run[qt] = -INFINITY;
+    w.l_run[qt] = 0.f;
+  }
+  // what some row of the wave sees and what all of them do, and of the workgroup
+  constexpr uint32_t kFar = 0x7fffffffu;
+  uint32_t lim[4] = {kFar, 0u, 0u, kFar};
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt) {
+    const bool any = w.hi[qt] > w.lo[qt], real = wave * 32 + qt * 16 + w.r16 < n_real;
+    lim[0] = min(lim[0], any ? (uint32_t)w.lo[qt] : kFar);
+    lim[1] = max(lim[1], (uint32_t)w.hi[qt]);
+    lim[2] = max(lim[2], real ? (any ? (uint32_t)w.lo[qt] : kFar) : 0u);
+    lim[3] = min(lim[3], real ? (uint32_t)w.hi[qt] : kFar);
+  }
+  const int w_lo = (int)wave_min_u(lim[0]), w_hi = (int)wave_max_u(lim[1]);
+  const int all_lo = (int)wave_max_u(lim[2]), all_hi = (int)wave_min_u(lim[3]);
+  if (lane == 0) {
+    s_lim[wave][0] = w_lo;
+    s_lim[wave][1] = w_hi;
+    s_lim[wave][2] = all_lo;
+    s_lim[wave][3] = all_hi;
+  }
+  __syncthreads();
+  int LO = (int)kFar, HI = 0, FLO = 0, FHI = (int)kFar;
+  for (int u = 0; u < kWaves; ++u) {
+    LO = min(LO, s_lim[u][0]);
+    HI = max(HI, s_lim[u][1]);
+    FLO = max(FLO, s_lim[u][2]);
+    FHI = min(FHI, s_lim[u][3]);
+  }
+  LO = __builtin_amdgcn_readfirstlane(LO);
+  HI = __builtin_amdgcn_readfirstlane(HI);
+  FLO = __builtin_amdgcn_readfirstlane(FLO);
+  FHI = __builtin_amdgcn_readfirstlane(FHI);
+  const int b0 = LO < HI ? LO / 64 : 0, b1 = LO < HI ? (HI + 63) / 64 : 0;
+  const int share = (b1 - b0 + pt.n_split - 1) / pt.n_split;
+  const int e0 = min(b0 + pt.split * share, b1), e1 = min(e0 + share, b1);
+  const bool second = wave >= kWaves / 2;
+
+  for (int c0 = e0; c0 < e1; c0 += kListBlocks) {
+    const int nb = min(kListBlocks, e1 - c0);
+    __syncthreads();                   // the list and the buffers are done with
+    if (tid == 0) s_missing = 0;
+    __syncthreads();
+    for (int i = tid; i < 4 * nb; i += 64 * kWaves) {
+      const int t = c0 * 64 + i * kGroupKeys;
+      const int r = t < cap ? a.pages.row(pt.s, t, g, a.h_kv) : -1;
+      s_list[i] = r;
+      if (r < 0) s_missing = 1;
+    }
+    __syncthreads();
+    const bool missing = __builtin_amdgcn_readfirstlane(s_missing) != 0;
+    auto pages_of = [&](int t) SPOT_INLINE -> unsigned {     // bit kt: the keys 16 kt .. are there
+      if (!missing) return 15u;
+      unsigned m = 0;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) m |= s_list[4 * t + kt] >= 0 ? 1u << kt : 0u;
+      return __builtin_amdgcn_readfirstlane(m);
+    };
+    // Blocks that some row of the workgroup sees in part only.
+    auto edge = [&](int t) SPOT_INLINE {
+      const int t0 = (c0 + t) * 64;
+      return t0 < FLO || t0 + 64 > FHI || pages_of(t) != 15u;
+    };
+    auto active = [&](int t) SPOT_INLINE {
+      const int t0 = (c0 + t) * 64;
+      return t0 < w_hi && t0 + 64 > w_lo;
+    };
+    auto vector_phase = [&](int t) SPOT_INLINE {
+      const int t0 = (c0 + t) * 64;
+      const unsigned pages = pages_of(t);
+      if (t0 < all_lo || t0 + 64 > all_hi || pages != 15u)
+        w.template softmax<true>(t0, pages);
+      else
+        w.template softmax<false>(t0, 15u);
+    };
+    // Values that no row sees become zero (they may be infinite or NaN, and meet the
+    // probability 0).  So do infinite and NaN elements of the others, which not every
+    // row sees: those that see them get theirs after the loop.  Each lane looks at
+    // what it copied itself.
+    auto mend = [&](int t, unsigned char* v) SPOT_INLINE {
+      const int t0 = (c0 + t) * 64;
+      const unsigned pages = pages_of(t);
+#pragma unroll
+      for (int u = 0; u < CopyV::N; ++u) {
+        const int r = CopyV::row(u, wave, lane), tok = t0 + r;
+        u32x4* at = reinterpret_cast<u32x4*>(v + (4 * u + wave) * 1024 + lane * 16);
+        if (tok < LO || tok >= HI || !(pages >> (r >> 4) & 1)) {
+          *at = u32x4{0u, 0u, 0u, 0u};
+        } else {
+          u32x4 x = *at;
+          if (odd2<T>(x[0]) || odd2<T>(x[1]) || odd2<T>(x[2]) || odd2<T>(x[3])) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = clean2<T>(x[e]);
+            *at = x;
+            s_odd = 1;
+          }
+        }
+      }
+    };
+    auto matrix_phase = [&](int t, const unsigned char* k, const unsigned char* v) SPOT_INLINE {
+      if (t >= 1 && active(t - 1)) w.pv(v);
+      if (t < nb && active(t)) w.qk(k);
+    };
+    if (!second) CopyK::issue(a.k, s_list, sk0, wave, lane);
+    wait_vm();
+    __syncthreads();
+    auto period = [&](auto parity, int t) SPOT_INLINE {
+      constexpr int P = decltype(parity)::value;
+      unsigned char* kcur = P ? sk1 : sk0;
+      unsigned char* knext = P ? sk0 : sk1;
+      unsigned char* vcur = P ? sv1 : sv0;
+      unsigned char* vprev = P ? sv0 : sv1;
+      if (!second) {
+        __builtin_amdgcn_s_setprio(3);
+        matrix_phase(t, kcur, vprev);
+        __builtin_amdgcn_s_setprio(0);
+        if (t + 1 < nb) CopyK::issue(a.k, s_list + 4 * (t + 1), knext, wave, lane);
+        if (t < nb) CopyV::issue(a.v, s_list + 4 * t, vcur, wave, lane);
+        __builtin_amdgcn_s_barrier();     // the phases change; no data changes hands
+        if (t < nb && active(t)) vector_phase(t);
+        wait_vm();
+        if (t < nb && edge(t)) mend(t, vcur);
+        __syncthreads();
+      } else {
+        if (t >= 1 && active(t - 1)) vector_phase(t - 1);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_s_setprio(3);
+        matrix_phase(t, kcur, vprev);
+        __builtin_amdgcn_s_setprio(0);
+        __syncthreads();
+      }
+    };
+    for (int t = 0;; t += 2) {
+      period(std::integral_constant<int, 0>(), t);
+      if (t + 1 > nb) break;
+      period(std::integral_constant<int, 1>(), t + 1);
+      if (t + 2 > nb) break;
+    }
+  }
+
+  // lane (G, r16) holds O^T[16 dt + 4 G + i][row r16]
+  settle(w.o[0]);
+  settle(w.o[1]);
+  __syncthreads();
+  if (s_odd) {
+    // The infinite and NaN elements that mend() left out, for the rows that see their
+    // tokens: p v of each, p from the row's score once more.  Rare, and slow.
+#pragma unroll 1
+    for (int tok = max(e0 * 64, LO); tok < min(e1 * 64, HI); ++tok) {
+      const int t0 = tok & ~63;
+      bool edge = t0 < FLO || t0 + 64 > FHI;
+      for (int t = t0; t < t0 + 64; t += kGroupKeys)
+        edge = edge || t >= cap || a.pages.row(pt.s, t, g, a.h_kv) < 0;
+      const int at = a.pages.row(pt.s, tok & ~(kGroupKeys - 1), g, a.h_kv);
+      if (!edge || at < 0) continue;
+      const size_t row = ((size_t)at + (tok & (kGroupKeys - 1))) * D;
+      u32x2 y[DT];
+      bool odd = false;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        y[dt] = *reinterpret_cast<const u32x2*>(a.v + row + dt * 16 + 4 * w.G);
+        odd = odd || odd2<T>(y[dt][0]) || odd2<T>(y[dt][1]);
+      }
+      if (!__ballot(odd)) continue;
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt) {
+        if (tok < w.lo[qt] || tok >= w.hi[qt]) continue;
+        float dot = 0.f;
+#pragma unroll 1
+        for (int d = 0; d < D; ++d)
+          dot = fmaf(T::one(a.q[row_of(wave * 32 + qt * 16 + w.r16) * D + d]), T::one(a.k[row + d]),
+                     dot);
+        const float p = __builtin_amdgcn_exp2f(w.sc[qt](dot, (float)(w.sc[qt].p - tok)) - w.m_run[qt]);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t h = i & 1 ? y[dt][i >> 1] >> 16 : y[dt][i >> 1] & 0xffffu;
+            if ((~h & T::kExponent) == 0u)
+              w.o[qt][dt][i] = fmaf(p, T::one((uint16_t)h), w.o[qt][dt][i]);
+          }
+      }
+    }
+  }
+  const size_t slot0 = (size_t)pt.slot * a.h_kv + (size_t)g * pt.n_split;
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt) {
+    const float L = lanes_sum_xor16(lanes_sum_xor32(w.l_run[qt])), M = w.m_run[qt];
+    const int r = wave * 32 + qt * 16 + w.r16;
+    if (r >= n_real) continue;
+    if (pt.n_split > 1) {
+      const size_t at = (slot0 + pt.split) * kRows + r;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        float* o = a.ws.o + at * D + dt * 16 + 4 * w.G;
+        dec::store_coherent(o, make_float2(w.o[qt][dt][0], w.o[qt][dt][1]));
+        dec::store_coherent(o + 2, make_float2(w.o[qt][dt][2], w.o[qt][dt][3]));
+      }
+      if (w.G == 0) dec::store_coherent(a.ws.ml + at * 2, make_float2(M, L));
+    } else {
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      const size_t row = row_of(r);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        *reinterpret_cast<u32x2*>(a.out + row * D + dt * 16 + 4 * w.G) =
+            u32x2{T::pack2(w.o[qt][dt][0] * inv, w.o[qt][dt][1] * inv),
+                  T::pack2(w.o[qt][dt][2] * inv, w.o[qt][dt][3] * inv)};
+      if (a.lse && w.G == 0)
+        a.lse[row] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
+    }
+  }
+  if (pt.n_split == 1) return;
+
+  dec::wait_stores();
+  __syncthreads();
+  unsigned* const counter = a.ws.counters + (size_t)pt.counter * a.h_kv + g;
+  if (tid == 0)
+    s_last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+             (unsigned)(pt.n_split - 1);
+  __syncthreads();
+  if (!s_last) return;
+
+  // the last part joins them: each row's M and 1 / L, then its output 4 dims a lane
+  const int n = pt.n_split;
+  const float* const ml = a.ws.ml + slot0 * kRows * 2;
+  if (tid < n_real) {
+    float M = -INFINITY, L = 0.f;
+    for (int u = 0; u < n; ++u) {
+      const float2 t = dec::load_coherent(ml + ((size_t)u * kRows + tid) * 2);
+      if (t.y != 0.f) {
+        const float m = fmaxf(M, t.x);
+        L = L * (M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - m)) +
+            t.y * __builtin_amdgcn_exp2f(t.x - m);
+        M = m;
+      }
+    }
+    s_join[tid][0] = M;
+    s_join[tid][1] = L == 0.f ? 0.f : 1.f / L;
+    if (a.lse) a.lse[row_of(tid)] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
+  }
+  __syncthreads();
+  constexpr int Q = D / 4, U = 4;      // quads of a row; rows of a lane in flight
+  constexpr int step = 64 * kWaves / Q;
+  for (int r0 = tid / Q; r0 < n_real; r0 += step * U) {
+    const int c = tid % Q;
+    f32x4 acc[U];
+    float M[U], inv[U];
+#pragma unroll
+    for (int e = 0; e < U; ++e) {
+      acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const int r = min(r0 + e * step, n_real - 1);
+      M[e] = s_join[r][0];
+      inv[e] = s_join[r][1];
+    }
+    for (int u = 0; u < n; ++u) {
+      float2 t[U], x[U], y[U];
+#pragma unroll
+      for (int e = 0; e < U; ++e) {
+        const size_t at = (size_t)u * kRows + min(r0 + e * step, n_real - 1);
+        t[e] = dec::load_coherent(ml + at * 2);
+        const float* o = a.ws.o + (slot0 * kRows + at) * D + 4 * c;
+        x[e] = dec::load_coherent(o);
+        y[e] = dec::load_coherent(o + 2);
+      }
+#pragma unroll
+      for (int e = 0; e < U; ++e) {
+        if (t[e].y == 0.f) continue;
+        const float wt = __builtin_amdgcn_exp2f(t[e].x - M[e]);
+        acc[e][0] = fmaf(x[e].x, wt, acc[e][0]);
+        acc[e][1] = fmaf(x[e].y, wt, acc[e][1]);
+        acc[e][2] = fmaf(y[e].x, wt, acc[e][2]);
+        acc[e][3] = fmaf(y[e].y, wt, acc[e][3]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < U; ++e) {
+      const int r = r0 + e * step;
+      if (r < n_real)
+        *reinterpret_cast<u32x2*>(a.out + row_of(r) * D + 4 * c) =
+            u32x2{T::pack2(acc[e][0] * inv[e], acc[e][1] * inv[e]),
+                  T::pack2(acc[e][2] * inv[e], acc[e][3] * inv[e])};
+    }
+  }
+  if (tid == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <class T, int D>
+void launch(const AttendArgs& a, dim3 grid, hipStream_t s) {
+  // the plain form needs a positive scale (it takes maxima before it scales)
+  const bool cap = a.rule.cap > 0.f, bias = a.rule.slopes || (!cap && !(a.rule.scale > 0.f));
+  auto f = cap ? (bias ? attend_many_kernel<T, D, true, true> : attend_many_kernel<T, D, true, false>)
+               : (bias ? attend_many_kernel<T, D, false, true>
+                       : attend_many_kernel<T, D, false, false>);
+  hipLaunchKernelGGL(f, grid, dim3(64 * kWaves), 0, s, a);
+}
+
+}  // namespace
+
+hipError_t launch_attend_many(AttendArgs a, int dtype, int d, void* ws, hipStream_t s) {
+  a.ws.counters = static_cast<unsigned*>(ws);
+  a.ws.ml = reinterpret_cast<float*>(static_cast<char*>(ws) + kCounterBytes);
+  a.ws.o = a.ws.ml + (size_t)kMaxParts * kRows * 2;
+  const dim3 grid(attend_grid<kRows>(a));
+  if (dtype == SPOT_DTYPE_BF16)
+    d == 128 ? launch<Bf16, 128>(a, grid, s) : launch<Bf16, 64>(a, grid, s);
+  else
+    d == 128 ? launch<Fp16, 128>(a, grid, s) : launch<Fp16, 64>(a, grid, s);
+  return hipGetLastError();
+}
+
+size_t attend_many_workspace(int d) {
+  return kCounterBytes + (size_t)kMaxParts * kRows * (2 + d) * sizeof(float);
+}
+
+}  // namespace paged
+}  // namespace spot

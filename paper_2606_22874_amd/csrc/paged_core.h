@@ -113,21 +113,22 @@ __device__ __forceinline__ float tanh_f(float y) {
   return a < 0.3f ? near : far;
 }
 
-// Scores in the log2 domain.  With neither cap nor bias: s * mul.
+// Scores in the log2 domain.  `ahead`: the row's position less the key's, in FP32 from
+// their difference as integers (positions themselves may need more than 24 bits).
 template <bool CAP, bool BIAS>
 struct Scores {
   float mul, cap2, slope2;   // scale log2e, or scale / cap; cap log2e; slope log2e
-  float p;                   // the row's position
+  int p;                     // the row's position
   __device__ __forceinline__ Scores() {}
   __device__ __forceinline__ Scores(const Rule& u, const Seq& q, int i, int head) {
     mul = CAP ? u.scale / u.cap : u.scale * kLog2e;
     cap2 = u.cap * kLog2e;
-    slope2 = BIAS ? u.slopes[head] * kLog2e : 0.f;
-    p = (float)(q.len - q.n + i);
+    slope2 = BIAS && u.slopes ? u.slopes[head] * kLog2e : 0.f;
+    p = q.len - q.n + i;
   }
-  __device__ __forceinline__ float operator()(float s, float t) const {
+  __device__ __forceinline__ float operator()(float s, float ahead) const {
     float x = CAP ? cap2 * tanh_f(s * mul) : s * mul;
-    if (BIAS) x = fmaf(-slope2, fabsf(p - t), x);
+    if (BIAS) x = fmaf(-slope2, fabsf(ahead), x);
     return x;
   }
 };
@@ -139,7 +140,7 @@ struct Scores {
 // device; the parts of a tile are joined by the last one to finish.  Every
 // workgroup finds its own part from the lengths on the device, so the host needs
 // none of them and a captured call stays right when they change.
-constexpr int kTarget = 512;                 // two workgroups per CU
+constexpr int kTarget = 512;
 constexpr int kMaxParts = 2 * kTarget + 64;  // parts of split tiles (each has at most twice its share)
 constexpr int kMaxSplit = kTarget + 64;      // split tiles
 
@@ -233,9 +234,19 @@ struct AttendArgs {
   float* lse;
   Workspace ws;
 };
-// ws as attend_few_workspace sizes it.
+// ws as the kernel's *_workspace sizes it.
 hipError_t launch_attend_few(AttendArgs a, int dtype, int d, void* ws, hipStream_t s);
 size_t attend_few_workspace(int d);
+hipError_t launch_attend_many(AttendArgs a, int dtype, int d, void* ws, hipStream_t s);
+size_t attend_many_workspace(int d);
+
+// Workgroups of a launch over tiles of TR rows: every tile in one part, and the parts
+// that kTarget shares of the work add.
+template <int TR>
+inline unsigned attend_grid(const AttendArgs& a) {
+  const int64_t rows = (int64_t)a.rows * (a.h_q / a.h_kv);
+  return (unsigned)((rows / TR + a.n_seq + kTarget / a.h_kv + 2) * a.h_kv);
+}
 
 struct WeightArgs {
   const uint16_t* q;
