@@ -10,9 +10,12 @@
 // The matrix cores bound it, so the two waves of a SIMD alternate: waves 0-3 run
 // matrix instructions while waves 4-7 run their softmax, then the other way round,
 // separated by barriers; block t takes half periods 2t and 2t + 1:
-//   2t      waves 0-3: P V of block t-1, K Q of block t, then the copies of K(t+1) and
-//           V(t) into the other buffers;   waves 4-7: softmax of block t-1
-//   2t + 1  waves 0-3: softmax of block t; their copies land;   waves 4-7: P V, K Q
+//   2t      waves 0-3: P V of block t-1, K Q of block t;   waves 4-7: start the copies of
+//           K(t+1) and V(t) into the buffers not in use, softmax of block t-1, wait for
+//           the copies
+//   2t + 1  waves 0-3: softmax of block t;   waves 4-7: P V of block t-1, K Q of block t
+// The copies fly behind a softmax and are down before the wave's next matrix phase: the
+// compiler orders the LDS reads of a wave with a copy in flight one by one.
 // K and V go from memory to LDS 16 bytes a lane (1 KiB a wave instruction), rows
 // swizzled by 16-byte chunks against bank conflicts; each of the buffers is a
 // variable of its own and the loop is unrolled by two, so that the compiler can tell
@@ -49,6 +52,14 @@ __device__ __forceinline__ int swz_v(int r, int c) {
   return D == 128 ? c ^ ((r & 7) << 1) : c ^ (((r >> 1) & 3) << 1);
 }
 
+// The lane's number, made anew where it is used: held or kept in scratch memory, what
+// follows from it costs registers or waits for every copy in flight.
+__device__ __forceinline__ int fresh_lane() {
+  int lane;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+  return lane;
+}
+
 // Copies of a block of 64 rows by 4 waves: instruction u of wave w fills rows
 // R (4u + w) .. + R, R rows of 1 KiB, all of one group of 16 keys.
 template <int D, bool IS_K>
@@ -60,7 +71,8 @@ struct Copy {
     return R * (4 * u + wave) + lane / CH;
   }
   static __device__ __forceinline__ void issue(const uint16_t* pool, const int* list,
-                                               unsigned char* dst, int wave, int lane) {
+                                               unsigned char* dst, int wave) {
+    const int lane = fresh_lane();
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int r = row(u, wave, lane), pc = lane % CH;
@@ -75,12 +87,27 @@ struct Copy {
   }
 };
 
-__device__ __forceinline__ void wait_vm() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+__device__ __forceinline__ void wait_vm() { __builtin_amdgcn_s_waitcnt(0x0F70); }   // vmcnt(0)
+
+// Barrier over the waves' LDS accesses.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_s_waitcnt(0xC07F);      // lgkmcnt(0)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
 __device__ __forceinline__ float max4(f32x4 x) {
   return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x[0], x[1]),
                                        __builtin_elementwise_maximum(x[2], x[3]));
 }
+
+// What a row of the tile sees, and what its scores need: read from LDS where a block
+// calls for it (registers are short).
+struct RowRule {
+  int lo, hi, p;
+  float slope2;
+};
 
 template <class T, int D, bool CAP, bool BIAS>
 struct Wave {
@@ -91,17 +118,16 @@ struct Wave {
   f32x4 s[2][4];              // scores, then probabilities, of the current block
   u32x4 pb[2][2];             // the probabilities as the B operand
   float m_run[2], l_run[2];
-  Scores<CAP, BIAS> sc[2];
-  int lo[2], hi[2];
+  const RowRule* rows;        // the wave's 32
+  float mul, cap2;            // see Scores
   int G, r16;
 
   // S^T of one block; the K fragments of a step are read one step ahead.  The chunks'
-  // swizzle is an exclusive or: one address and immediates give all fragments (kept
-  // from the compiler's sight, which would hold one register for each).
+  // swizzle is an exclusive or: one address and immediates give all fragments.
   __device__ __forceinline__ void qk(const unsigned char* Kt) {
     u32x4 a[2][4];
-    int at = r16 * RB + (swz_k<D>(r16, G) << 4);
-    asm volatile("" : "+v"(at));
+    const int lane = fresh_lane(), r16 = lane & 15, G = lane >> 4;
+    const int at = r16 * RB + (swz_k<D>(r16, G) << 4);
     auto load = [&](int ks, int slot) {
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt)
@@ -127,9 +153,9 @@ struct Wave {
   // gets column r16 of rows 4 G .. +3.
   __device__ __forceinline__ void pv(const unsigned char* Vt) {
     u32x4 a[2][DT];
+    const int lane = fresh_lane(), r16 = lane & 15, G = lane >> 4;
     const int r0 = 4 * G + (r16 >> 2);
-    int at = r0 * RB + (swz_v<D>(r0, (r16 & 3) >> 1) << 4) + (r16 & 1) * 8;
-    asm volatile("" : "+v"(at));
+    const int at = r0 * RB + (swz_v<D>(r0, (r16 & 3) >> 1) << 4) + (r16 & 1) * 8;
     auto load = [&](int ks, int dt0) {
 #pragma unroll
       for (int dt = dt0; dt < dt0 + 4; ++dt) {
@@ -170,29 +196,53 @@ struct Wave {
     }
   }
 
-  // Online softmax of the scores into pb.  MASK: some row does not see the whole block;
-  // pages: bit kt says that keys 16 kt .. are there.
-  template <bool MASK>
-  __device__ __forceinline__ void softmax(int t0, unsigned pages) {
+  // Online softmax of the scores into pb.  masked: some row does not see the whole
+  // block; pages: bit kt says that keys 16 kt .. are there.
+  __device__ __forceinline__ void softmax(int t0, bool masked, unsigned pages) {
     asm volatile("s_nop 15"
                  : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[0][2]), "+v"(s[0][3]), "+v"(s[1][0]),
                    "+v"(s[1][1]), "+v"(s[1][2]), "+v"(s[1][3]));   // see settle()
-    const float c = PLAIN ? sc[0].mul : 1.f;    // positive
+    const float c = PLAIN ? mul : 1.f;    // positive
+    if (!PLAIN) {
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt) {
+        const int lane = fresh_lane();
+        Scores<CAP, BIAS> sc;
+        sc.mul = mul;
+        sc.cap2 = cap2;
+        sc.slope2 = 0.f;
+        float ahead = 0.f;
+        if (BIAS) {
+          const RowRule u = rows[16 * qt + (lane & 15)];
+          sc.slope2 = u.slope2;
+          ahead = (float)(u.p - (t0 + 4 * (lane >> 4)));
+        }
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            s[qt][kt][i] = sc(s[qt][kt][i], ahead - (float)(16 * kt + i));
+      }
+    }
+    if (masked) {
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt) {
+        const int lane = fresh_lane(), at = t0 + 4 * (lane >> 4);
+        const RowRule u = rows[16 * qt + (lane & 15)];
+        const int from = u.lo - at, to = u.hi - at;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            s[qt][kt][i] = ((16 * kt + i < from) | (16 * kt + i >= to)) ? -INFINITY : s[qt][kt][i];
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+          if (!(pages >> kt & 1)) s[qt][kt] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      }
+    }
     float mt[2];
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
-      const float ahead = (float)(sc[qt].p - (t0 + 4 * G));
-      const int from = lo[qt] - (t0 + 4 * G), to = hi[qt] - (t0 + 4 * G);
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = s[qt][kt][i];
-          if (!PLAIN) x = sc[qt](x, ahead - (float)(16 * kt + i));
-          if (MASK && (!(pages >> kt & 1) || 16 * kt + i < from || 16 * kt + i >= to))
-            x = -INFINITY;
-          s[qt][kt][i] = x;
-        }
       const float mx = __builtin_elementwise_maximum(
           __builtin_elementwise_maximum(max4(s[qt][0]), max4(s[qt][1])),
           __builtin_elementwise_maximum(max4(s[qt][2]), max4(s[qt][3])));
@@ -248,6 +298,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
   __shared__ int s_lim[kWaves][4];
   __shared__ int s_missing, s_last, s_odd;
   __shared__ float s_join[kRows][2];
+  __shared__ RowRule s_rule[kRows];
   __shared__ Part s_part;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int G = a.h_q / a.h_kv, g = blockIdx.x % a.h_kv;
@@ -274,15 +325,20 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
     const int64_t j = j0 + r;
     return (size_t)(pt.q.start + (int)(j / G)) * a.h_q + g * G + (int)(j % G);
   };
+  w.rows = s_rule + wave * 32;
+  int lo[2], hi[2];
 #pragma unroll
   for (int qt = 0; qt < 2; ++qt) {
     const int r = wave * 32 + qt * 16 + w.r16;
     const bool real = r < n_real;
     const int64_t j = j0 + (real ? r : 0);
     const int tok = (int)(j / G), head = g * G + (int)(j % G);
-    w.lo[qt] = w.hi[qt] = 0;
-    if (real) visible(a.rule, pt.q, pt.s, tok, cap, w.lo[qt], w.hi[qt]);
-    w.sc[qt] = Scores<CAP, BIAS>(a.rule, pt.q, tok, head);
+    lo[qt] = hi[qt] = 0;
+    if (real) visible(a.rule, pt.q, pt.s, tok, cap, lo[qt], hi[qt]);
+    const Scores<CAP, BIAS> sc(a.rule, pt.q, tok, head);
+    w.mul = sc.mul;
+    w.cap2 = sc.cap2;
+    if (w.G == 0) s_rule[r] = RowRule{lo[qt], hi[qt], sc.p, sc.slope2};
     const uint16_t* q = a.q + row_of(real ? r : 0) * D + 8 * w.G;
 #pragma unroll
     for (int ks = 0; ks < D / 32; ++ks) w.qf[ks][qt] = *reinterpret_cast<const u32x4*>(q + ks * 32);
@@ -296,11 +352,11 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
   uint32_t lim[4] = {kFar, 0u, 0u, kFar};
 #pragma unroll
   for (int qt = 0; qt < 2; ++qt) {
-    const bool any = w.hi[qt] > w.lo[qt], real = wave * 32 + qt * 16 + w.r16 < n_real;
-    lim[0] = min(lim[0], any ? (uint32_t)w.lo[qt] : kFar);
-    lim[1] = max(lim[1], (uint32_t)w.hi[qt]);
-    lim[2] = max(lim[2], real ? (any ? (uint32_t)w.lo[qt] : kFar) : 0u);
-    lim[3] = min(lim[3], real ? (uint32_t)w.hi[qt] : kFar);
+    const bool any = hi[qt] > lo[qt], real = wave * 32 + qt * 16 + w.r16 < n_real;
+    lim[0] = min(lim[0], any ? (uint32_t)lo[qt] : kFar);
+    lim[1] = max(lim[1], (uint32_t)hi[qt]);
+    lim[2] = max(lim[2], real ? (any ? (uint32_t)lo[qt] : kFar) : 0u);
+    lim[3] = min(lim[3], real ? (uint32_t)hi[qt] : kFar);
   }
   const int w_lo = (int)wave_min_u(lim[0]), w_hi = (int)wave_max_u(lim[1]);
   const int all_lo = (int)wave_max_u(lim[2]), all_hi = (int)wave_min_u(lim[3]);
@@ -359,10 +415,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
     auto vector_phase = [&](int t) SPOT_INLINE {
       const int t0 = (c0 + t) * 64;
       const unsigned pages = pages_of(t);
-      if (t0 < all_lo || t0 + 64 > all_hi || pages != 15u)
-        w.template softmax<true>(t0, pages);
-      else
-        w.template softmax<false>(t0, 15u);
+      w.softmax(t0, t0 < all_lo || t0 + 64 > all_hi || pages != 15u, pages);
     };
     // Values that no row sees become zero (they may be infinite or NaN, and meet the
     // probability 0).  So do infinite and NaN elements of the others, which not every
@@ -371,10 +424,11 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
     auto mend = [&](int t, unsigned char* v) SPOT_INLINE {
       const int t0 = (c0 + t) * 64;
       const unsigned pages = pages_of(t);
-#pragma unroll
+      const int lane = fresh_lane();
+#pragma unroll 1
       for (int u = 0; u < CopyV::N; ++u) {
-        const int r = CopyV::row(u, wave, lane), tok = t0 + r;
-        u32x4* at = reinterpret_cast<u32x4*>(v + (4 * u + wave) * 1024 + lane * 16);
+        const int wv = wave - kWaves / 2, r = CopyV::row(u, wv, lane), tok = t0 + r;
+        u32x4* at = reinterpret_cast<u32x4*>(v + (4 * u + wv) * 1024 + lane * 16);
         if (tok < LO || tok >= HI || !(pages >> (r >> 4) & 1)) {
           *at = u32x4{0u, 0u, 0u, 0u};
         } else {
@@ -392,33 +446,35 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
       if (t >= 1 && active(t - 1)) w.pv(v);
       if (t < nb && active(t)) w.qk(k);
     };
-    if (!second) CopyK::issue(a.k, s_list, sk0, wave, lane);
-    wait_vm();
-    __syncthreads();
+    if (second) {
+      CopyK::issue(a.k, s_list, sk0, wave - kWaves / 2);
+      wait_vm();
+    }
+    lds_barrier();
     auto period = [&](auto parity, int t) SPOT_INLINE {
-      constexpr int P = decltype(parity)::value;
-      unsigned char* kcur = P ? sk1 : sk0;
-      unsigned char* knext = P ? sk0 : sk1;
-      unsigned char* vcur = P ? sv1 : sv0;
-      unsigned char* vprev = P ? sv0 : sv1;
+      constexpr int P = decltype(parity)::value;     // t % 2
+      unsigned char* const kcur = P ? sk1 : sk0;
+      unsigned char* const knext = P ? sk0 : sk1;
+      unsigned char* const vcur = P ? sv1 : sv0;
+      unsigned char* const vprev = P ? sv0 : sv1;
       if (!second) {
         __builtin_amdgcn_s_setprio(3);
         matrix_phase(t, kcur, vprev);
         __builtin_amdgcn_s_setprio(0);
-        if (t + 1 < nb) CopyK::issue(a.k, s_list + 4 * (t + 1), knext, wave, lane);
-        if (t < nb) CopyV::issue(a.v, s_list + 4 * t, vcur, wave, lane);
-        __builtin_amdgcn_s_barrier();     // the phases change; no data changes hands
+        lds_barrier();
         if (t < nb && active(t)) vector_phase(t);
+        lds_barrier();
+      } else {
+        if (t + 1 < nb) CopyK::issue(a.k, s_list + 4 * (t + 1), knext, wave - kWaves / 2);
+        if (t < nb) CopyV::issue(a.v, s_list + 4 * t, vcur, wave - kWaves / 2);
+        if (t >= 1 && active(t - 1)) vector_phase(t - 1);
         wait_vm();
         if (t < nb && edge(t)) mend(t, vcur);
-        __syncthreads();
-      } else {
-        if (t >= 1 && active(t - 1)) vector_phase(t - 1);
-        __builtin_amdgcn_s_barrier();
+        lds_barrier();
         __builtin_amdgcn_s_setprio(3);
         matrix_phase(t, kcur, vprev);
         __builtin_amdgcn_s_setprio(0);
-        __syncthreads();
+        lds_barrier();
       }
     };
     for (int t = 0;; t += 2) {
@@ -455,13 +511,18 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
       if (!__ballot(odd)) continue;
 #pragma unroll
       for (int qt = 0; qt < 2; ++qt) {
-        if (tok < w.lo[qt] || tok >= w.hi[qt]) continue;
+        const RowRule u = w.rows[16 * qt + w.r16];
+        if (tok < u.lo || tok >= u.hi) continue;
+        Scores<CAP, BIAS> sc;
+        sc.mul = w.mul;
+        sc.cap2 = w.cap2;
+        sc.slope2 = u.slope2;
         float dot = 0.f;
 #pragma unroll 1
         for (int d = 0; d < D; ++d)
           dot = fmaf(T::one(a.q[row_of(wave * 32 + qt * 16 + w.r16) * D + d]), T::one(a.k[row + d]),
                      dot);
-        const float p = __builtin_amdgcn_exp2f(w.sc[qt](dot, (float)(w.sc[qt].p - tok)) - w.m_run[qt]);
+        const float p = __builtin_amdgcn_exp2f(sc(dot, (float)(u.p - tok)) - w.m_run[qt]);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
