@@ -10,10 +10,10 @@
 // The matrix cores bound it, so the two waves of a SIMD alternate: waves 0-3 run
 // matrix instructions while waves 4-7 run their softmax, then the other way round,
 // separated by barriers; block t takes half periods 2t and 2t + 1:
-//   2t      waves 0-3: P V of block t-1, K Q of block t;   waves 4-7: start the copies of
-//           K(t+1) and V(t) into the buffers not in use, softmax of block t-1, wait for
-//           the copies
-//   2t + 1  waves 0-3: softmax of block t;   waves 4-7: P V of block t-1, K Q of block t
+//   2t      waves 0-3: P V of block t-1, K Q of block t;   waves 4-7: start the copy of
+//           K(t+1) into the buffer not in use, softmax of block t-1, wait for the copy
+//   2t + 1  waves 0-3: start the copy of V(t), softmax of block t, wait for the copy;
+//           waves 4-7: P V of block t-1, K Q of block t
 // The copies fly behind a softmax and are down before the wave's next matrix phase: the
 // compiler orders the LDS reads of a wave with a copy in flight one by one.
 // K and V go from memory to LDS 16 bytes a lane (1 KiB a wave instruction), rows
@@ -95,11 +95,6 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-}
-
-__device__ __forceinline__ float max4(f32x4 x) {
-  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x[0], x[1]),
-                                       __builtin_elementwise_maximum(x[2], x[3]));
 }
 
 // What a row of the tile sees, and what its scores need: read from LDS where a block
@@ -243,9 +238,15 @@ struct Wave {
     float mt[2];
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
-      const float mx = __builtin_elementwise_maximum(
-          __builtin_elementwise_maximum(max4(s[qt][0]), max4(s[qt][1])),
-          __builtin_elementwise_maximum(max4(s[qt][2]), max4(s[qt][3])));
+      // (a NaN may be passed over here: its probability makes l NaN)
+      float mx = fmaxf(fmaxf(s[qt][0][0], s[qt][0][1]), s[qt][0][2]);
+      mx = fmaxf(fmaxf(mx, s[qt][0][3]), s[qt][1][0]);
+      mx = fmaxf(fmaxf(mx, s[qt][1][1]), s[qt][1][2]);
+      mx = fmaxf(fmaxf(mx, s[qt][1][3]), s[qt][2][0]);
+      mx = fmaxf(fmaxf(mx, s[qt][2][1]), s[qt][2][2]);
+      mx = fmaxf(fmaxf(mx, s[qt][2][3]), s[qt][3][0]);
+      mx = fmaxf(fmaxf(mx, s[qt][3][1]), s[qt][3][2]);
+      mx = fmaxf(mx, s[qt][3][3]);
       mt[qt] = lanes_max_xor16(lanes_max_xor32(mx)) * c - T::kShift;
     }
     // The reference maximum moves only when a column's grows by more than kLazy, so
@@ -427,8 +428,8 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
       const int lane = fresh_lane();
 #pragma unroll 1
       for (int u = 0; u < CopyV::N; ++u) {
-        const int wv = wave - kWaves / 2, r = CopyV::row(u, wv, lane), tok = t0 + r;
-        u32x4* at = reinterpret_cast<u32x4*>(v + (4 * u + wv) * 1024 + lane * 16);
+        const int r = CopyV::row(u, wave, lane), tok = t0 + r;
+        u32x4* at = reinterpret_cast<u32x4*>(v + (4 * u + wave) * 1024 + lane * 16);
         if (tok < LO || tok >= HI || !(pages >> (r >> 4) & 1)) {
           *at = u32x4{0u, 0u, 0u, 0u};
         } else {
@@ -458,22 +459,19 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
       unsigned char* const vcur = P ? sv1 : sv0;
       unsigned char* const vprev = P ? sv0 : sv1;
       if (!second) {
-        __builtin_amdgcn_s_setprio(3);
         matrix_phase(t, kcur, vprev);
-        __builtin_amdgcn_s_setprio(0);
         lds_barrier();
+        if (t < nb) CopyV::issue(a.v, s_list + 4 * t, vcur, wave);
         if (t < nb && active(t)) vector_phase(t);
-        lds_barrier();
-      } else {
-        if (t + 1 < nb) CopyK::issue(a.k, s_list + 4 * (t + 1), knext, wave - kWaves / 2);
-        if (t < nb) CopyV::issue(a.v, s_list + 4 * t, vcur, wave - kWaves / 2);
-        if (t >= 1 && active(t - 1)) vector_phase(t - 1);
         wait_vm();
         if (t < nb && edge(t)) mend(t, vcur);
         lds_barrier();
-        __builtin_amdgcn_s_setprio(3);
+      } else {
+        if (t + 1 < nb) CopyK::issue(a.k, s_list + 4 * (t + 1), knext, wave - kWaves / 2);
+        if (t >= 1 && active(t - 1)) vector_phase(t - 1);
+        wait_vm();
+        lds_barrier();
         matrix_phase(t, kcur, vprev);
-        __builtin_amdgcn_s_setprio(0);
         lds_barrier();
       }
     };
