@@ -1,7 +1,6 @@
 // C ABI of the operators on a paged cache: argument validation, then kernel
 // launches.  Nothing is enqueued unless every argument check passes.
 #include <math.h>
-#include <stdlib.h>
 
 #include "paged_core.h"
 
@@ -46,11 +45,16 @@ spot_status check_rope(int d, int rope_dim, const double* freq, float amp, int f
   return SPOT_OK;
 }
 
-// Which calls take tiles of 256 rows, and not of 16.
-bool attend_many_takes(int n_seq, int rows, int h_q, int h_kv) {
-  static const char* e = getenv("SPOT_MANY");
-  return (int64_t)rows * (h_q / h_kv) > (e ? atoi(e) : 64) * (int64_t)n_seq;
+// Rows (new tokens x heads of a group) of a sequence up to which it goes to the kernel of
+// 16-row tiles, beyond them to that of 256.  The lengths are on the device, so the
+// host knows their mean alone: where that is within 16, the first kernel takes all
+// of them (a call has one launch in a decode step), and with one sequence either one
+// does; otherwise both are launched, and each passes over the other's sequences.
+constexpr int kFewRows = 64;
+bool launch_many(int n_seq, int rows, int G) {
+  return (int64_t)rows * G > (n_seq == 1 ? kFewRows : 16 * (int64_t)n_seq);
 }
+bool launch_few(int n_seq, int rows, int G) { return n_seq > 1 || !launch_many(n_seq, rows, G); }
 
 const uint16_t* in16(const void* p) { return static_cast<const uint16_t*>(p); }
 uint16_t* out16(void* p) { return static_cast<uint16_t*>(p); }
@@ -168,8 +172,7 @@ spot_status spot_rotary_append(const void* q, int64_t q_stride, const void* k, i
 
 size_t spot_paged_workspace_bytes(int n_seq, int rows, int h_q, int h_kv, int d) {
   if (n_seq < 1 || rows < 1 || h_q < 1 || h_kv < 1 || d < 1) return 0;
-  return attend_many_takes(n_seq, rows, h_q, h_kv) ? attend_many_workspace(d)
-                                                   : attend_few_workspace(d);
+  return launch_many(n_seq, rows, h_q / h_kv) ? attend_many_workspace(d) : attend_few_workspace(d);
 }
 
 spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, const void* v_pages,
@@ -204,9 +207,21 @@ spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, con
   a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first};
   a.out = out16(out);
   a.lse = lse;
-  return from_hip((attend_many_takes(n_seq, rows, h_q, h_kv) ? launch_attend_many
-                                                             : launch_attend_few)(
-      a, dtype, d, ws, static_cast<hipStream_t>(stream)));
+  const int G = h_q / h_kv;
+  const bool many = launch_many(n_seq, rows, G), few = launch_few(n_seq, rows, G);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e = hipSuccess;
+  if (many) {
+    a.from = few ? kFewRows : 0;
+    a.to = 0x7fffffff;
+    e = launch_attend_many(a, dtype, d, ws, s);
+  }
+  if (few && e == hipSuccess) {
+    a.from = 0;
+    a.to = many ? kFewRows : 0x7fffffff;
+    e = launch_attend_few(a, dtype, d, ws, s);
+  }
+  return from_hip(e);
 }
 
 spot_status spot_paged_weights(const void* q, const float* lse, int dtype, const void* k_pages,

@@ -130,8 +130,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
   const int G = a.h_q / a.h_kv, g = blockIdx.x % a.h_kv;
   const int cap = a.pages.cap();
   if (wave == 0) {
-    const Part p = find_part<kRows>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len, a.n_seq, a.rows,
-                                    G, a.h_kv, a.rule.window, cap, kMinBlocks);
+    const Part p = find_part<kRows, kMinBlocks>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len,
+                                                a.n_seq, a.rows, G, a.h_kv, a.rule.window, cap,
+                                                a.from, a.to);
     if (lane == 0) sm.part = p;
   }
   __syncthreads();
@@ -231,10 +232,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
     };
     auto back = [&](int n, f32x4 s) {
       const int t0 = (c0 + n) * 64 + wave * 16;
-      const float ahead = (float)(sc.p - (t0 + 4 * kg));
-      float x[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = sc(s[i], ahead - (float)i);
+      f32x4 quad[1] = {s};
+      sc(quad, (float)(sc.p - (t0 + 4 * kg)));
+      float x[4] = {quad[0][0], quad[0][1], quad[0][2], quad[0][3]};
       if (t0 < FLO || t0 + 16 > FHI || row_of(n) < 0) {
         const bool page = row_of(n) >= 0;
 #pragma unroll

@@ -37,6 +37,7 @@ using dec::lanes_sum_xor32;
 constexpr int kRows = 256;         // rows of a tile
 constexpr int kWaves = 8;
 constexpr int kMinBlocks = 4;      // fewest blocks of a part
+constexpr int kRound = 256;        // workgroups at once: one a CU
 constexpr int kListBlocks = 512;   // blocks whose pages are looked up at once
 typedef __attribute__((address_space(3))) void lds_void;
 #define SPOT_INLINE __attribute__((always_inline))
@@ -212,11 +213,7 @@ struct Wave {
           sc.slope2 = u.slope2;
           ahead = (float)(u.p - (t0 + 4 * (lane >> 4)));
         }
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            s[qt][kt][i] = sc(s[qt][kt][i], ahead - (float)(16 * kt + i));
+        sc(s[qt], ahead);
       }
     }
     if (masked) {
@@ -305,8 +302,9 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
   const int G = a.h_q / a.h_kv, g = blockIdx.x % a.h_kv;
   const int cap = a.pages.cap();
   if (wave == 0) {
-    const Part p = find_part<kRows>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len, a.n_seq, a.rows,
-                                    G, a.h_kv, a.rule.window, cap, kMinBlocks);
+    const Part p = find_part<kRows, kMinBlocks, kRound>(blockIdx.x / a.h_kv, a.seq_start,
+                                                        a.seq_len, a.n_seq, a.rows, G, a.h_kv,
+                                                        a.rule.window, cap, a.from, a.to);
     if (lane == 0) {
       s_part = p;
       s_odd = 0;
@@ -520,7 +518,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
         for (int d = 0; d < D; ++d)
           dot = fmaf(T::one(a.q[row_of(wave * 32 + qt * 16 + w.r16) * D + d]), T::one(a.k[row + d]),
                      dot);
-        const float p = __builtin_amdgcn_exp2f(sc(dot, (float)(u.p - tok)) - w.m_run[qt]);
+        const float p = __builtin_amdgcn_exp2f(sc.one(dot, (float)(u.p - tok)) - w.m_run[qt]);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll

@@ -102,15 +102,21 @@ __device__ __forceinline__ uint32_t clean2(uint32_t x) {
   return x;
 }
 
-// tanh to 2e-7 relative: e^(-2|y|) beyond 0.3, where 1 - e keeps its bits, and the
-// Taylor polynomial below (its first dropped term is 5e-8 there).
-__device__ __forceinline__ float tanh_f(float y) {
-  const float a = fabsf(y), z = y * y;
-  const float e = __builtin_amdgcn_exp2f(a * (-2.f * kLog2e));
+// tanh to 2e-7 relative: its Taylor polynomial up to 0.5 (the first dropped term is
+// 9e-8 there), and beyond it e^(-2|y|), where 1 - e keeps its bits.
+__device__ __forceinline__ float tanh_near(float y) {
+  const float z = y * y;
+  float t = fmaf(21844.f / 6081075, z, -1382.f / 155925);
+  t = fmaf(t, z, 62.f / 2835);
+  t = fmaf(t, z, -17.f / 315);
+  t = fmaf(t, z, 2.f / 15);
+  t = fmaf(t, z, -1.f / 3);
+  return y * fmaf(t, z, 1.f);
+}
+__device__ __forceinline__ float tanh_any(float y) {
+  const float a = fabsf(y), e = __builtin_amdgcn_exp2f(a * (-2.f * kLog2e));
   const float far = copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), y);
-  const float near =
-      y * fmaf(fmaf(fmaf(fmaf(62.f / 2835, z, -17.f / 315), z, 2.f / 15), z, -1.f / 3), z, 1.f);
-  return a < 0.3f ? near : far;
+  return a < 0.5f ? tanh_near(y) : far;
 }
 
 // Scores in the log2 domain.  `ahead`: the row's position less the key's, in FP32 from
@@ -126,10 +132,39 @@ struct Scores {
     slope2 = BIAS && u.slopes ? u.slopes[head] * kLog2e : 0.f;
     p = q.len - q.n + i;
   }
-  __device__ __forceinline__ float operator()(float s, float ahead) const {
-    float x = CAP ? cap2 * tanh_f(s * mul) : s * mul;
-    if (BIAS) x = fmaf(-slope2, fabsf(ahead), x);
-    return x;
+  // Four scores of a lane, `ahead` of the first; NEAR: all of the wave's lie where
+  // tanh_near does (most calls have a cap well above their scores).
+  template <bool NEAR>
+  __device__ __forceinline__ f32x4 scaled(f32x4 s, float ahead) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float y = s[i] * mul;
+      float x = CAP ? cap2 * (NEAR ? tanh_near(y) : tanh_any(y)) : y;
+      if (BIAS) x = fmaf(-slope2, fabsf(ahead - (float)i), x);
+      s[i] = x;
+    }
+    return s;
+  }
+  // N such quads, 16 keys from one to the next.
+  template <int N>
+  __device__ __forceinline__ void operator()(f32x4 (&s)[N], float ahead) const {
+    if constexpr (CAP) {
+      float top = 0.f;
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(s[e][i]));
+      if (!__ballot(top * fabsf(mul) > 0.5f)) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) s[e] = scaled<true>(s[e], ahead - 16.f * e);
+        return;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) s[e] = scaled<false>(s[e], ahead - 16.f * e);
+  }
+  __device__ __forceinline__ float one(float s, float ahead) const {
+    return scaled<false>(f32x4{s, s, s, s}, ahead)[0];
   }
 };
 
@@ -158,14 +193,21 @@ __device__ __forceinline__ int span_blocks(const Seq& q, int window, int cap) {
   return hi > lo ? (hi + 63) / 64 - lo / 64 : 0;
 }
 
-// The part of unit `unit` (of the parts of all tiles of TR rows, one KV head),
-// found by one wave; every lane gets it.  min_blocks: fewest blocks of a part.
-template <int TR>
+// The part of unit `unit` (of the parts of all tiles of TR rows, one KV head), found by
+// one wave; every lane gets it.  Sequences of from < rows <= to (new tokens x heads)
+// take part.  MIN_BLOCKS: fewest blocks of a part.  ROUND: workgroups that the device
+// holds at once, each as long as its blocks; the blocks of a part then grow from
+// their least number, up to twice as many, to what ends first: rounds of workgroups
+// x blocks of a part (and what a workgroup costs beside them, about 3).
+template <int TR, int MIN_BLOCKS, int ROUND = 0>
 __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
                                           const int32_t* seq_len, int n_seq, int rows, int G,
-                                          int h_kv, int window, int cap, int min_blocks) {
+                                          int h_kv, int window, int cap, int from, int to) {
   const int lane = __lane_id();
-  auto tiles_of = [&](const Seq& q) { return (int)(((int64_t)q.n * G + TR - 1) / TR); };
+  auto tiles_of = [&](const Seq& q) {
+    const int64_t n = (int64_t)q.n * G;
+    return n > from && n <= to ? (int)((n + TR - 1) / TR) : 0;
+  };
   // all steps
   float steps = 0.f;
   Seq q0 = {0, 0, 0};
@@ -175,7 +217,25 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
     if (base == 0) q0 = q;
     steps += wave_sum((float)tiles_of(q) * (float)span_blocks(q, window, cap));
   }
-  const int per = max(min_blocks, (int)ceilf(steps * (float)h_kv / (float)kTarget));
+  int per = max(MIN_BLOCKS, (int)ceilf(steps * (float)h_kv / (float)kTarget));
+  if (ROUND && n_seq <= 64) {
+    const int T = tiles_of(q0), nb = T ? span_blocks(q0, window, cap) : 0;
+    if (__ballot(nb > per)) {
+      int best = 0x7fffffff, at = per;
+      for (int e = 8; e <= 16; ++e) {
+        const int p = (per * e + 7) / 8, ns = max(1, (nb + p - 1) / p);
+        const int units = wave_sum_i(T * ns) * h_kv;
+        // the longest part of any tile
+        const int most = (int)wave_max_u((uint32_t)((nb + ns - 1) / ns));
+        const int cost = (units + ROUND - 1) / ROUND * (most + 3);
+        if (cost < best) {
+          best = cost;
+          at = p;
+        }
+      }
+      per = at;
+    }
+  }
   // the sequence that holds the unit
   Part r;
   r.s = -1;
@@ -233,6 +293,7 @@ struct AttendArgs {
   uint16_t* out;
   float* lse;
   Workspace ws;
+  int from, to;      // sequences of from < rows (new tokens x heads of a group) <= to
 };
 // ws as the kernel's *_workspace sizes it.
 hipError_t launch_attend_few(AttendArgs a, int dtype, int d, void* ws, hipStream_t s);
@@ -245,7 +306,10 @@ size_t attend_many_workspace(int d);
 template <int TR>
 inline unsigned attend_grid(const AttendArgs& a) {
   const int64_t rows = (int64_t)a.rows * (a.h_q / a.h_kv);
-  return (unsigned)((rows / TR + a.n_seq + kTarget / a.h_kv + 2) * a.h_kv);
+  int64_t tiles = rows / TR + a.n_seq;
+  const int64_t most = (int64_t)a.n_seq * ((a.to - 1) / TR + 1);   // of sequences up to a.to
+  if (tiles > most) tiles = most;
+  return (unsigned)((tiles + kTarget / a.h_kv + 2) * a.h_kv);
 }
 
 struct WeightArgs {

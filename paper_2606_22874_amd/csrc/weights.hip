@@ -68,14 +68,13 @@ __global__ __launch_bounds__(64 * kWaves) void weights_kernel(WeightArgs a) {
         for (int kt = 0; kt < 4; ++kt) x[kt] = T::mfma32(kf[kt][kc], qf, x[kt]);
       }
       settle(x);
-      const float ahead = (float)(sc.p - (t0 + 4 * kg));
+      sc(x, (float)(sc.p - (t0 + 4 * kg)));
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int t = t0 + 16 * kt + 4 * kg + i;
-          const float w =
-              __builtin_amdgcn_exp2f(sc(x[kt][i], ahead - (float)(16 * kt + i)) - lse * kLog2e);
+          const float w = __builtin_amdgcn_exp2f(x[kt][i] - lse * kLog2e);
           sum[kt][i] += page[kt] && t >= lo && t < hi && lse != -INFINITY ? w : 0.f;
         }
     }
