@@ -108,7 +108,6 @@ struct RowRule {
 template <class T, int D, bool CAP, bool BIAS>
 struct Wave {
   static constexpr int RB = D * 2, KS = D / 32, DT = D / 16;
-  static constexpr bool PLAIN = !CAP && !BIAS;
   u32x4 qf[KS][2];            // Q^T as the B operand [dims][16 rows]
   f32x4 o[2][DT];
   f32x4 s[2][4];              // scores, then probabilities, of the current block
@@ -192,14 +191,17 @@ struct Wave {
     }
   }
 
-  // Online softmax of the scores into pb.  masked: some row does not see the whole
-  // block; pages: bit kt says that keys 16 kt .. are there.
-  __device__ __forceinline__ void softmax(int t0, bool masked, unsigned pages) {
+  // Online softmax of the scores into pb.  below, above: some row does not see the
+  // first or last keys of the block; pages: bit kt says that keys 16 kt .. are there.
+  __device__ __forceinline__ void softmax(int t0, bool below, bool above, unsigned pages) {
     asm volatile("s_nop 15"
                  : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[0][2]), "+v"(s[0][3]), "+v"(s[1][0]),
                    "+v"(s[1][1]), "+v"(s[1][2]), "+v"(s[1][3]));   // see settle()
-    const float c = PLAIN ? mul : 1.f;    // positive
-    if (!PLAIN) {
+    // Without a cap a positive scale waits until the exponent (and the bias is taken in
+    // its units): an operation less for each score.
+    const bool late = !CAP && mul > 1e-6f;
+    const float c = late ? mul : 1.f;
+    if (CAP || BIAS) {
 #pragma unroll
       for (int qt = 0; qt < 2; ++qt) {
         const int lane = fresh_lane();
@@ -213,20 +215,38 @@ struct Wave {
           sc.slope2 = u.slope2;
           ahead = (float)(u.p - (t0 + 4 * (lane >> 4)));
         }
-        sc(s[qt], ahead);
+        if (BIAS && late) {
+          const float m = -sc.slope2 * (1.f / mul);
+#pragma unroll
+          for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              s[qt][kt][i] = fmaf(m, fabsf(ahead - (float)(16 * kt + i)), s[qt][kt][i]);
+        } else {
+          sc(s[qt], ahead);
+        }
       }
     }
-    if (masked) {
+    if (below | above | (pages != 15u)) {
 #pragma unroll
       for (int qt = 0; qt < 2; ++qt) {
         const int lane = fresh_lane(), at = t0 + 4 * (lane >> 4);
         const RowRule u = rows[16 * qt + (lane & 15)];
         const int from = u.lo - at, to = u.hi - at;
+        if (below) {
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
+          for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            s[qt][kt][i] = ((16 * kt + i < from) | (16 * kt + i >= to)) ? -INFINITY : s[qt][kt][i];
+            for (int i = 0; i < 4; ++i)
+              s[qt][kt][i] = 16 * kt + i < from ? -INFINITY : s[qt][kt][i];
+        }
+        if (above) {
+#pragma unroll
+          for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              s[qt][kt][i] = 16 * kt + i >= to ? -INFINITY : s[qt][kt][i];
+        }
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt)
           if (!(pages >> kt & 1)) s[qt][kt] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -268,8 +288,8 @@ struct Wave {
       for (int kt = 0; kt < 4; ++kt) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          s[qt][kt][i] = __builtin_amdgcn_exp2f(PLAIN ? fmaf(s[qt][kt][i], c, -mu)
-                                                      : s[qt][kt][i] - mu);
+          s[qt][kt][i] = __builtin_amdgcn_exp2f(CAP ? s[qt][kt][i] - mu
+                                                    : fmaf(s[qt][kt][i], c, -mu));
         ps[kt] = (s[qt][kt][0] + s[qt][kt][1]) + (s[qt][kt][2] + s[qt][kt][3]);
       }
       l_run[qt] += (ps[0] + ps[1]) + (ps[2] + ps[3]);
@@ -414,7 +434,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
     auto vector_phase = [&](int t) SPOT_INLINE {
       const int t0 = (c0 + t) * 64;
       const unsigned pages = pages_of(t);
-      w.softmax(t0, t0 < all_lo || t0 + 64 > all_hi || pages != 15u, pages);
+      w.softmax(t0, t0 < all_lo, t0 + 64 > all_hi, pages);
     };
     // Values that no row sees become zero (they may be infinite or NaN, and meet the
     // probability 0).  So do infinite and NaN elements of the others, which not every
@@ -600,24 +620,26 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
       M[e] = s_join[r][0];
       inv[e] = s_join[r][1];
     }
-    for (int u = 0; u < n; ++u) {
-      float2 t[U], x[U], y[U];
+    for (int u0 = 0; u0 < n; u0 += 2) {
+      float2 t[2 * U], x[2 * U], y[2 * U];
 #pragma unroll
-      for (int e = 0; e < U; ++e) {
-        const size_t at = (size_t)u * kRows + min(r0 + e * step, n_real - 1);
-        t[e] = dec::load_coherent(ml + at * 2);
+      for (int h = 0; h < 2 * U; ++h) {
+        const size_t at =
+            (size_t)min(u0 + h / U, n - 1) * kRows + min(r0 + h % U * step, n_real - 1);
+        t[h] = dec::load_coherent(ml + at * 2);
         const float* o = a.ws.o + (slot0 * kRows + at) * D + 4 * c;
-        x[e] = dec::load_coherent(o);
-        y[e] = dec::load_coherent(o + 2);
+        x[h] = dec::load_coherent(o);
+        y[h] = dec::load_coherent(o + 2);
       }
 #pragma unroll
-      for (int e = 0; e < U; ++e) {
-        if (t[e].y == 0.f) continue;
-        const float wt = __builtin_amdgcn_exp2f(t[e].x - M[e]);
-        acc[e][0] = fmaf(x[e].x, wt, acc[e][0]);
-        acc[e][1] = fmaf(x[e].y, wt, acc[e][1]);
-        acc[e][2] = fmaf(y[e].x, wt, acc[e][2]);
-        acc[e][3] = fmaf(y[e].y, wt, acc[e][3]);
+      for (int h = 0; h < 2 * U; ++h) {
+        const int e = h % U;
+        if (t[h].y == 0.f || u0 + h / U >= n) continue;
+        const float wt = __builtin_amdgcn_exp2f(t[h].x - M[e]);
+        acc[e][0] = fmaf(x[h].x, wt, acc[e][0]);
+        acc[e][1] = fmaf(x[h].y, wt, acc[e][1]);
+        acc[e][2] = fmaf(y[h].x, wt, acc[e][2]);
+        acc[e][3] = fmaf(y[h].y, wt, acc[e][3]);
       }
     }
 #pragma unroll
@@ -634,8 +656,9 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
 
 template <class T, int D>
 void launch(const AttendArgs& a, dim3 grid, hipStream_t s) {
-  // the plain form needs a positive scale (it takes maxima before it scales)
-  const bool cap = a.rule.cap > 0.f, bias = a.rule.slopes || (!cap && !(a.rule.scale > 0.f));
+  // the plain form takes maxima before it scales: it needs a positive scale
+  const bool cap = a.rule.cap > 0.f;
+  const bool bias = a.rule.slopes || (!cap && !(a.rule.scale * kLog2e > 1e-6f));
   auto f = cap ? (bias ? attend_many_kernel<T, D, true, true> : attend_many_kernel<T, D, true, false>)
                : (bias ? attend_many_kernel<T, D, false, true>
                        : attend_many_kernel<T, D, false, false>);

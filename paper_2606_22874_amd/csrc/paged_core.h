@@ -197,8 +197,8 @@ __device__ __forceinline__ int span_blocks(const Seq& q, int window, int cap) {
 // one wave; every lane gets it.  Sequences of from < rows <= to (new tokens x heads)
 // take part.  MIN_BLOCKS: fewest blocks of a part.  ROUND: workgroups that the device
 // holds at once, each as long as its blocks; the blocks of a part then grow from
-// their least number, up to twice as many, to what ends first: rounds of workgroups
-// x blocks of a part (and what a workgroup costs beside them, about 3).
+// their least number, up to three times as many, to what ends first: rounds of
+// workgroups x (blocks of a part + 8, about what a part costs beside them).
 template <int TR, int MIN_BLOCKS, int ROUND = 0>
 __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
                                           const int32_t* seq_len, int n_seq, int rows, int G,
@@ -222,12 +222,12 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
     const int T = tiles_of(q0), nb = T ? span_blocks(q0, window, cap) : 0;
     if (__ballot(nb > per)) {
       int best = 0x7fffffff, at = per;
-      for (int e = 8; e <= 16; ++e) {
+      for (int e = 8; e <= 24; e += e < 12 ? 1 : 2) {
         const int p = (per * e + 7) / 8, ns = max(1, (nb + p - 1) / p);
         const int units = wave_sum_i(T * ns) * h_kv;
         // the longest part of any tile
         const int most = (int)wave_max_u((uint32_t)((nb + ns - 1) / ns));
-        const int cost = (units + ROUND - 1) / ROUND * (most + 3);
+        const int cost = (units + ROUND - 1) / ROUND * (most + 8);
         if (cost < best) {
           best = cost;
           at = p;
