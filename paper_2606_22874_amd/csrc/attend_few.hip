@@ -140,9 +140,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
   if (pt.s < 0) return;
 
   // this lane's column: row j of the sequence's matrix
-  const int64_t j = (int64_t)pt.tile * kRows + r16;
-  const bool real = j < (int64_t)pt.q.n * G;
-  const int tok = real ? (int)(j / G) : 0, head = g * G + (real ? (int)(j % G) : 0);
+  const unsigned j = pt.tile * kRows + r16, n_rows = pt.q.n * G;
+  const bool real = j < n_rows;
+  const int tok = real ? j / G : 0, head = g * G + (real ? j - tok * G : 0);
   int lo = 0, hi = 0;
   if (real) visible(a.rule, pt.q, pt.s, tok, cap, lo, hi);
   const Scores<CAP, BIAS> sc(a.rule, pt.q, tok, head);
@@ -347,7 +347,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
   for (int dt = 0; dt < D / 16; ++dt)
     *reinterpret_cast<f32x4*>(&sm.merge.o[wave][r16][16 * dt + 4 * kg]) = o[dt];
   __syncthreads();
-  const int n_real = (int)min((int64_t)kRows, (int64_t)pt.q.n * G - (int64_t)pt.tile * kRows);
+  const int n_real = min((unsigned)kRows, n_rows - pt.tile * kRows);
+  auto row_of = [&](int c) __attribute__((always_inline)) {   // row of the tile in out
+    const unsigned jc = pt.tile * kRows + c, tc = jc / (unsigned)G;
+    return (size_t)(pt.q.start + tc) * a.h_q + g * G + (jc - tc * G);
+  };
   const size_t slot0 = ((size_t)pt.slot * a.h_kv + (size_t)g * pt.n_split);
   float* const wml = a.ws.ml + (slot0 + pt.split) * kRows * 2;
   float* const wo = a.ws.o + (slot0 + pt.split) * kRows * D;
@@ -373,8 +377,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
         __hip_atomic_store(wo + c * D + lane, acc[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (lane == 0) dec::store_coherent(wml + c * 2, make_float2(M, L));
     } else {
-      const int64_t jc = (int64_t)pt.tile * kRows + c;
-      const size_t row = (size_t)(pt.q.start + (int)(jc / G)) * a.h_q + g * G + (int)(jc % G);
+      const size_t row = row_of(c);
       const float inv = L == 0.f ? 0.f : 1.f / L;
       if constexpr (PL == 2)
         reinterpret_cast<uint32_t*>(a.out + row * D)[lane] = T::pack2(acc[0] * inv, acc[1] * inv);
@@ -395,8 +398,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
   __syncthreads();
   if (!sm.last) return;
   for (int c = wave; c < n_real; c += kWaves) {
-    const int64_t jc = (int64_t)pt.tile * kRows + c;
-    const size_t row = (size_t)(pt.q.start + (int)(jc / G)) * a.h_q + g * G + (int)(jc % G);
+    const size_t row = row_of(c);
     join_row<T, D>(a.ws.ml + slot0 * kRows * 2 + c * 2, a.ws.o + slot0 * kRows * D + c * D,
                    pt.n_split, a.out + row * D, a.lse ? a.lse + row : nullptr, lane);
   }

@@ -337,12 +337,12 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
   W w;
   w.G = lane >> 4;
   w.r16 = lane & 15;
-  const int64_t j0 = (int64_t)pt.tile * kRows, j_end = (int64_t)pt.q.n * G;
-  const int n_real = (int)min((int64_t)kRows, j_end - j0);
+  const unsigned j0 = pt.tile * kRows;
+  const int n_real = min((unsigned)kRows, (unsigned)(pt.q.n * G) - j0);
   // row of q and out of the tile's row r
   auto row_of = [&](int r) SPOT_INLINE {
-    const int64_t j = j0 + r;
-    return (size_t)(pt.q.start + (int)(j / G)) * a.h_q + g * G + (int)(j % G);
+    const unsigned j = j0 + r, tok = j / (unsigned)G;
+    return (size_t)(pt.q.start + tok) * a.h_q + g * G + (j - tok * G);
   };
   w.rows = s_rule + wave * 32;
   int lo[2], hi[2];
@@ -350,8 +350,8 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
   for (int qt = 0; qt < 2; ++qt) {
     const int r = wave * 32 + qt * 16 + w.r16;
     const bool real = r < n_real;
-    const int64_t j = j0 + (real ? r : 0);
-    const int tok = (int)(j / G), head = g * G + (int)(j % G);
+    const unsigned j = j0 + (real ? r : 0);
+    const int tok = j / (unsigned)G, head = g * G + (j - tok * G);
     lo[qt] = hi[qt] = 0;
     if (real) visible(a.rule, pt.q, pt.s, tok, cap, lo[qt], hi[qt]);
     const Scores<CAP, BIAS> sc(a.rule, pt.q, tok, head);

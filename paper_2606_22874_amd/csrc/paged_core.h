@@ -205,8 +205,8 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
                                           int h_kv, int window, int cap, int from, int to) {
   const int lane = __lane_id();
   auto tiles_of = [&](const Seq& q) {
-    const int64_t n = (int64_t)q.n * G;
-    return n > from && n <= to ? (int)((n + TR - 1) / TR) : 0;
+    const int n = q.n * G;
+    return n > from && n <= to ? (int)((unsigned)(n + TR - 1) / TR) : 0;
   };
   // all steps
   float steps = 0.f;

@@ -2,10 +2,13 @@
 // (gfx950): acc_out[s, g, t] = decay acc[s, g, t] + sum over the rows (new tokens x
 // the heads of KV head g) of e^(x - lse), with the scores x and lse of the attention.
 //
-// One workgroup of 4 waves per 256 keys of a KV head, 64 keys a wave, held in
-// registers as the A operand of S^T = K Q^T; the rows pass by 16 at a time as the B
-// operand.  A key belongs to one wave, so there are no atomics and the order of the
-// sums is fixed.
+// A wave holds 64 keys of a KV head in registers as the A operand of S^T = K Q^T, and
+// the rows pass by 16 at a time as the B operand, the next 16 on their way from memory
+// meanwhile.  The keys come by way of LDS, so that their loads are coalesced.  Few
+// rows (a decode step, bound by the keys' bytes): the 4 waves of a workgroup take 256
+// keys.  Many rows (bound by exponentials and matrix instructions): they take the
+// same 64 keys and a quarter of the rows each.  A key belongs to one workgroup, so
+// there are no atomics and the order of the sums is fixed.
 #include "decode_core.h"
 #include "paged_core.h"
 
@@ -13,33 +16,45 @@ namespace spot {
 namespace paged {
 namespace {
 
-constexpr int kKeys = 256;      // of a workgroup
 constexpr int kWaves = 4;
+typedef __attribute__((address_space(3))) void lds_void;
 
-template <class T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(64 * kWaves) void weights_kernel(WeightArgs a) {
+template <class T, int D, bool CAP, bool BIAS, bool ROWS>
+__global__ __launch_bounds__(64 * kWaves, 2) void weights_kernel(WeightArgs a) {
+  constexpr int RB = D * 2, CH = D / 8;        // bytes and 16-byte chunks of a row
+  constexpr int R = 1024 / RB;                 // rows of a copy instruction
+  constexpr int kTile = 64 * RB;
+  __shared__ __attribute__((aligned(16))) unsigned char s_k[(ROWS ? 1 : kWaves) * kTile];
+  __shared__ float s_sum[ROWS ? kWaves : 1][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int r16 = lane & 15, kg = lane >> 4;
   const int G = a.h_q / a.h_kv, cap = a.pages.cap();
   const int g = blockIdx.x % a.h_kv, s = blockIdx.y;
-  const int t0 = (blockIdx.x / a.h_kv) * kKeys + wave * 64;
-  if (t0 >= cap) return;
+  const int t0 = ROWS ? (blockIdx.x / a.h_kv) * 64 : ((blockIdx.x / a.h_kv) * kWaves + wave) * 64;
   const Seq q = sequence(a.seq_start, a.seq_len, s, a.rows);
   const int end = min(q.len, cap);
 
   float sum[4][4] = {};
   if (t0 < end && q.n > 0) {
-    u32x4 kf[4][D / 32];
-    bool page[4];
+    // the keys; bit kt of pages: those from 16 kt on are there
+    unsigned char* const ks = s_k + (ROWS ? 0 : wave * kTile);
+    unsigned pages = 0;
+    int at[4];
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
       const int t = t0 + 16 * kt;
-      const int row = t < cap ? a.pages.row(s, t, g, a.h_kv) : -1;
-      page[kt] = row >= 0;
-      const uint16_t* p = a.k + ((int64_t)max(row, 0) + r16) * D + 8 * kg;
+      at[kt] = t < cap ? a.pages.row(s, t, g, a.h_kv) : -1;
+      pages |= at[kt] >= 0 ? 1u << kt : 0u;
+    }
 #pragma unroll
-      for (int kc = 0; kc < D / 32; ++kc)
-        kf[kt][kc] = *reinterpret_cast<const u32x4*>(p + 32 * kc);
+    for (int u = 0; u < 64 / R / (ROWS ? kWaves : 1); ++u) {
+      const int i = ROWS ? kWaves * u + wave : u;        // rows R i ..
+      const int r = R * i + lane / CH, c = (lane % CH) ^ (r & (CH - 1));
+      const int kt = R * i / 16;
+      const int from = kt == 0 ? at[0] : kt == 1 ? at[1] : kt == 2 ? at[2] : at[3];
+      const uint16_t* src = a.k + (int64_t)__builtin_amdgcn_readfirstlane(max(from, 0)) * D;
+      __builtin_amdgcn_global_load_lds(src + (uint32_t)((r & 15) * D + c * 8),
+                                       (lds_void*)(ks + i * 1024), 16, 0, 0);
     }
     // the new tokens that see some of these keys
     const int p0 = q.len - q.n;
@@ -47,36 +62,82 @@ __global__ __launch_bounds__(64 * kWaves) void weights_kernel(WeightArgs a) {
     if (a.rule.prefix && a.rule.prefix[s] > t0) i0 = 0;
     if (a.rule.window > 0)
       i1 = (int)min((int64_t)i1, max((int64_t)t0 + 63 + a.rule.window - p0, (int64_t)0));
-    const int64_t j1 = (int64_t)i1 * G;
-    for (int64_t j0 = (int64_t)i0 * G; j0 < j1; j0 += 16) {
-      const int64_t j = j0 + r16;
-      const bool real = j < j1;
-      const int tok = real ? (int)(j / G) : 0, head = g * G + (real ? (int)(j % G) : 0);
-      const size_t row = (size_t)(q.start + tok) * a.h_q + head;
-      int lo = 0, hi = 0;
-      if (real) visible(a.rule, q, s, tok, cap, lo, hi);
-      const float lse = real ? a.lse[row] : -INFINITY;
-      const Scores<CAP, BIAS> sc(a.rule, q, tok, head);
+    const int end_row = i1 * G;
+    // Rows of a step: this lane's is j = i0 G + 16 (step of the wave) + r16; token and
+    // head advance without a division.
+    constexpr int kStride = 16 * (ROWS ? kWaves : 1);
+    const int dt = kStride / G, dh = kStride % G;
+    int j = i0 * G + (ROWS ? 16 * wave : 0) + r16;
+    int tok = (int)((unsigned)j / (unsigned)G), hd = j - tok * G;
+    struct Step {
+      u32x4 q[D / 32];
+      float lse;
+      int lo, hi, tok, hd;
+    };
+    auto load = [&](Step& e) __attribute__((always_inline)) {
+      const bool real = j < end_row;
+      e.tok = real ? tok : i0;
+      e.hd = real ? hd : 0;
+      e.lo = e.hi = 0;
+      if (real) visible(a.rule, q, s, e.tok, cap, e.lo, e.hi);
+      const size_t row = (size_t)(q.start + min(e.tok, q.n - 1)) * a.h_q + g * G + e.hd;
+      e.lse = a.lse[row] * kLog2e;
+#pragma unroll
+      for (int kc = 0; kc < D / 32; ++kc)
+        e.q[kc] = *reinterpret_cast<const u32x4*>(a.q + row * D + 32 * kc + 8 * kg);
+      j += kStride;
+      tok += dt;
+      hd += dh;
+      if (hd >= G) {
+        hd -= G;
+        ++tok;
+      }
+    };
+    const int first = i0 * G + (ROWS ? 16 * wave : 0);
+    const int steps = end_row > first ? (end_row - first + kStride - 1) / kStride : 0;
+    Step cur, nxt;
+    if (steps > 0) load(cur);
+    __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0): the copies
+    if (ROWS) __syncthreads();
+    u32x4 kf[4][D / 32];
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int kc = 0; kc < D / 32; ++kc)
+        kf[kt][kc] = *reinterpret_cast<const u32x4*>(
+            ks + (16 * kt + r16) * RB + (((4 * kc + kg) ^ (r16 & (CH - 1))) << 4));
+    for (int n = 0; n < steps; ++n) {
+      if (n + 1 < steps) load(nxt);
       f32x4 x[4];
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) x[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int kc = 0; kc < D / 32; ++kc) {
-        const u32x4 qf =
-            *reinterpret_cast<const u32x4*>(a.q + row * D + 32 * kc + 8 * kg);
+      for (int kc = 0; kc < D / 32; ++kc)
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) x[kt] = T::mfma32(kf[kt][kc], qf, x[kt]);
-      }
+        for (int kt = 0; kt < 4; ++kt) x[kt] = T::mfma32(kf[kt][kc], cur.q[kc], x[kt]);
       settle(x);
-      sc(x, (float)(sc.p - (t0 + 4 * kg)));
+      const Scores<CAP, BIAS> sc(a.rule, q, cur.tok, g * G + cur.hd);
+      if (CAP || BIAS) sc(x, (float)(sc.p - (t0 + 4 * kg)));
+      const float mul = CAP || BIAS ? 1.f : sc.mul;
+      const bool counts = cur.lse != -INFINITY;
+      if (__ballot(cur.lo > t0 || cur.hi < t0 + 64 || !counts) || pages != 15u) {
+        const int from = counts ? cur.lo - (t0 + 4 * kg) : 64;
+        const int to = counts ? cur.hi - (t0 + 4 * kg) : 0;
 #pragma unroll
-      for (int kt = 0; kt < 4; ++kt)
+        for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int t = t0 + 16 * kt + 4 * kg + i;
-          const float w = __builtin_amdgcn_exp2f(x[kt][i] - lse * kLog2e);
-          sum[kt][i] += page[kt] && t >= lo && t < hi && lse != -INFINITY ? w : 0.f;
-        }
+          for (int i = 0; i < 4; ++i) {
+            const float w = __builtin_amdgcn_exp2f(fmaf(x[kt][i], mul, -cur.lse));
+            sum[kt][i] += (pages >> kt & 1) && 16 * kt + i >= from && 16 * kt + i < to ? w : 0.f;
+          }
+      } else {
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            sum[kt][i] += __builtin_amdgcn_exp2f(fmaf(x[kt][i], mul, -cur.lse));
+      }
+      cur = nxt;
     }
   }
   // the 16 columns of a key
@@ -91,37 +152,53 @@ __global__ __launch_bounds__(64 * kWaves) void weights_kernel(WeightArgs a) {
       v += dpp_f<kDppMirror>(v);
       sum[kt][i] = v;
     }
-  if (r16 == 0) {
-    const int64_t base = ((int64_t)s * a.h_kv + g) * cap;
+  const int64_t base = ((int64_t)s * a.h_kv + g) * cap;
+  auto put = [&](int t, float v) __attribute__((always_inline)) {
+    a.acc_out[base + t] = a.acc ? fmaf(a.decay, a.acc[base + t], v) : v;
+  };
+  // lane (kg, r16) has the sums of keys 16 kt + 4 kg + i: it keeps that of kt = r16 / 4,
+  // i = r16 % 4, which makes one key a lane
+  float mine = 0.f;
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt)
+  for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = t0 + 16 * kt + 4 * kg + i;
-        if (t < cap)
-          a.acc_out[base + t] = a.acc ? fmaf(a.decay, a.acc[base + t], sum[kt][i]) : sum[kt][i];
-      }
+    for (int i = 0; i < 4; ++i) mine = r16 == 4 * kt + i ? sum[kt][i] : mine;
+  const int key = 16 * (r16 >> 2) + 4 * kg + (r16 & 3);
+  if (ROWS) {
+    s_sum[wave][key] = mine;
+    __syncthreads();
+    if (tid < 64 && t0 + tid < cap)
+      put(t0 + tid, (s_sum[0][tid] + s_sum[1][tid]) + (s_sum[2][tid] + s_sum[3][tid]));
+  } else if (t0 + key < cap) {
+    put(t0 + key, mine);
   }
 }
 
-template <class T, int D>
+template <class T, int D, bool ROWS>
 void launch(const WeightArgs& a, dim3 grid, hipStream_t s) {
   const bool cap = a.rule.cap > 0.f, bias = a.rule.slopes != nullptr;
-  auto f = cap ? (bias ? weights_kernel<T, D, true, true> : weights_kernel<T, D, true, false>)
-               : (bias ? weights_kernel<T, D, false, true> : weights_kernel<T, D, false, false>);
+  auto f = cap ? (bias ? weights_kernel<T, D, true, true, ROWS>
+                       : weights_kernel<T, D, true, false, ROWS>)
+               : (bias ? weights_kernel<T, D, false, true, ROWS>
+                       : weights_kernel<T, D, false, false, ROWS>);
   hipLaunchKernelGGL(f, grid, dim3(64 * kWaves), 0, s, a);
+}
+template <bool ROWS>
+void launch(const WeightArgs& a, int dtype, int d, hipStream_t s) {
+  const int keys = ROWS ? 64 : 64 * kWaves, cap = a.pages.cap();
+  const dim3 grid((unsigned)((cap + keys - 1) / keys) * (unsigned)a.h_kv, (unsigned)a.n_seq);
+  if (dtype == SPOT_DTYPE_BF16)
+    d == 128 ? launch<Bf16, 128, ROWS>(a, grid, s) : launch<Bf16, 64, ROWS>(a, grid, s);
+  else
+    d == 128 ? launch<Fp16, 128, ROWS>(a, grid, s) : launch<Fp16, 64, ROWS>(a, grid, s);
 }
 
 }  // namespace
 
 hipError_t launch_weights(const WeightArgs& a, int dtype, int d, hipStream_t s) {
-  const int cap = a.pages.cap();
-  if (cap == 0) return hipSuccess;
-  const dim3 grid((unsigned)((cap + kKeys - 1) / kKeys) * (unsigned)a.h_kv, (unsigned)a.n_seq);
-  if (dtype == SPOT_DTYPE_BF16)
-    d == 128 ? launch<Bf16, 128>(a, grid, s) : launch<Bf16, 64>(a, grid, s);
-  else
-    d == 128 ? launch<Fp16, 128>(a, grid, s) : launch<Fp16, 64>(a, grid, s);
+  if (a.pages.cap() == 0) return hipSuccess;
+  const bool many = (int64_t)a.rows * (a.h_q / a.h_kv) >= 64 * (int64_t)a.n_seq;
+  many ? launch<true>(a, dtype, d, s) : launch<false>(a, dtype, d, s);
   return hipGetLastError();
 }
 
