@@ -206,7 +206,7 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
   const int lane = __lane_id();
   auto tiles_of = [&](const Seq& q) {
     const int n = q.n * G;
-    return n > from && n <= to ? (int)((unsigned)(n + TR - 1) / TR) : 0;
+    return n > from && n <= to ? (int)(((unsigned)n + TR - 1) / TR) : 0;
   };
   // all steps
   float steps = 0.f;

@@ -2,12 +2,12 @@
 // (gfx950): acc_out[s, g, t] = decay acc[s, g, t] + sum over the rows (new tokens x
 // the heads of KV head g) of e^(x - lse), with the scores x and lse of the attention.
 //
-// A wave holds 64 keys of a KV head in registers as the A operand of S^T = K Q^T, and
-// the rows pass by 16 at a time as the B operand, the next 16 on their way from memory
+// A wave holds 64 or 128 keys of a KV head in registers as the A operand of
+// S^T = K Q^T, and the rows pass by 16 at a time as the B operand, the next 16 on their way from memory
 // meanwhile.  The keys come by way of LDS, so that their loads are coalesced.  Few
 // rows (a decode step, bound by the keys' bytes): the 4 waves of a workgroup take 256
 // keys.  Many rows (bound by exponentials and matrix instructions): they take the
-// same 64 keys and a quarter of the rows each.  A key belongs to one workgroup, so
+// same 128 keys and a quarter of the rows each.  A key belongs to one workgroup, so
 // there are no atomics and the order of the sums is fixed.
 #include "decode_core.h"
 #include "paged_core.h"
@@ -23,45 +23,47 @@ template <class T, int D, bool CAP, bool BIAS, bool ROWS>
 __global__ __launch_bounds__(64 * kWaves, 2) void weights_kernel(WeightArgs a) {
   constexpr int RB = D * 2, CH = D / 8;        // bytes and 16-byte chunks of a row
   constexpr int R = 1024 / RB;                 // rows of a copy instruction
-  constexpr int kTile = 64 * RB;
+  constexpr int NK = ROWS ? 8 : 4, kKeys = 16 * NK;   // groups of 16 keys of a wave
+  constexpr int kTile = kKeys * RB;
   __shared__ __attribute__((aligned(16))) unsigned char s_k[(ROWS ? 1 : kWaves) * kTile];
-  __shared__ float s_sum[ROWS ? kWaves : 1][64];
+  __shared__ float s_sum[ROWS ? kWaves : 1][kKeys];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int r16 = lane & 15, kg = lane >> 4;
   const int G = a.h_q / a.h_kv, cap = a.pages.cap();
   const int g = blockIdx.x % a.h_kv, s = blockIdx.y;
-  const int t0 = ROWS ? (blockIdx.x / a.h_kv) * 64 : ((blockIdx.x / a.h_kv) * kWaves + wave) * 64;
+  const int t0 = (ROWS ? blockIdx.x / a.h_kv : (blockIdx.x / a.h_kv) * kWaves + wave) * kKeys;
   const Seq q = sequence(a.seq_start, a.seq_len, s, a.rows);
   const int end = min(q.len, cap);
 
-  float sum[4][4] = {};
+  float sum[NK][4] = {};
   if (t0 < end && q.n > 0) {
     // the keys; bit kt of pages: those from 16 kt on are there
     unsigned char* const ks = s_k + (ROWS ? 0 : wave * kTile);
     unsigned pages = 0;
-    int at[4];
+    int at[NK];
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt) {
+    for (int kt = 0; kt < NK; ++kt) {
       const int t = t0 + 16 * kt;
       at[kt] = t < cap ? a.pages.row(s, t, g, a.h_kv) : -1;
       pages |= at[kt] >= 0 ? 1u << kt : 0u;
     }
 #pragma unroll
-    for (int u = 0; u < 64 / R / (ROWS ? kWaves : 1); ++u) {
+    for (int u = 0; u < kKeys / R / (ROWS ? kWaves : 1); ++u) {
       const int i = ROWS ? kWaves * u + wave : u;        // rows R i ..
       const int r = R * i + lane / CH, c = (lane % CH) ^ (r & (CH - 1));
-      const int kt = R * i / 16;
-      const int from = kt == 0 ? at[0] : kt == 1 ? at[1] : kt == 2 ? at[2] : at[3];
+      int from = at[0];
+#pragma unroll
+      for (int kt = 1; kt < NK; ++kt) from = R * i / 16 == kt ? at[kt] : from;
       const uint16_t* src = a.k + (int64_t)__builtin_amdgcn_readfirstlane(max(from, 0)) * D;
       __builtin_amdgcn_global_load_lds(src + (uint32_t)((r & 15) * D + c * 8),
                                        (lds_void*)(ks + i * 1024), 16, 0, 0);
     }
     // the new tokens that see some of these keys
     const int p0 = q.len - q.n;
-    int i0 = max(0, t0 - p0), i1 = q.n;
+    int i0 = min(max(0, t0 - p0), q.n), i1 = q.n;
     if (a.rule.prefix && a.rule.prefix[s] > t0) i0 = 0;
     if (a.rule.window > 0)
-      i1 = (int)min((int64_t)i1, max((int64_t)t0 + 63 + a.rule.window - p0, (int64_t)0));
+      i1 = (int)min((int64_t)i1, max((int64_t)t0 + kKeys - 1 + a.rule.window - p0, (int64_t)0));
     const int end_row = i1 * G;
     // Rows of a step: this lane's is j = i0 G + 16 (step of the wave) + r16; token and
     // head advance without a division.
@@ -99,50 +101,56 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weights_kernel(WeightArgs a) {
     if (steps > 0) load(cur);
     __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0): the copies
     if (ROWS) __syncthreads();
-    u32x4 kf[4][D / 32];
+    u32x4 kf[NK][D / 32];
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt)
+    for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
       for (int kc = 0; kc < D / 32; ++kc)
         kf[kt][kc] = *reinterpret_cast<const u32x4*>(
             ks + (16 * kt + r16) * RB + (((4 * kc + kg) ^ (r16 & (CH - 1))) << 4));
     for (int n = 0; n < steps; ++n) {
       if (n + 1 < steps) load(nxt);
-      f32x4 x[4];
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt) x[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kc = 0; kc < D / 32; ++kc)
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt) x[kt] = T::mfma32(kf[kt][kc], cur.q[kc], x[kt]);
-      settle(x);
       const Scores<CAP, BIAS> sc(a.rule, q, cur.tok, g * G + cur.hd);
-      if (CAP || BIAS) sc(x, (float)(sc.p - (t0 + 4 * kg)));
       const float mul = CAP || BIAS ? 1.f : sc.mul;
       const bool counts = cur.lse != -INFINITY;
-      if (__ballot(cur.lo > t0 || cur.hi < t0 + 64 || !counts) || pages != 15u) {
-        const int from = counts ? cur.lo - (t0 + 4 * kg) : 64;
-        const int to = counts ? cur.hi - (t0 + 4 * kg) : 0;
+      const bool part = __ballot(cur.lo > t0 || cur.hi < t0 + kKeys || !counts) != 0ull ||
+                        pages != (1u << NK) - 1u;
+      const int from = counts ? cur.lo - (t0 + 4 * kg) : kKeys;
+      const int to = counts ? cur.hi - (t0 + 4 * kg) : 0;
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
+      for (int k0 = 0; k0 < NK; k0 += 4) {     // 64 keys at a time
+        f32x4 x[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float w = __builtin_amdgcn_exp2f(fmaf(x[kt][i], mul, -cur.lse));
-            sum[kt][i] += (pages >> kt & 1) && 16 * kt + i >= from && 16 * kt + i < to ? w : 0.f;
-          }
-      } else {
+        for (int kt = 0; kt < 4; ++kt) x[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
+        for (int kc = 0; kc < D / 32; ++kc)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            sum[kt][i] += __builtin_amdgcn_exp2f(fmaf(x[kt][i], mul, -cur.lse));
+          for (int kt = 0; kt < 4; ++kt) x[kt] = T::mfma32(kf[k0 + kt][kc], cur.q[kc], x[kt]);
+        settle(x);
+        if (CAP || BIAS) sc(x, (float)(sc.p - (t0 + 16 * k0 + 4 * kg)));
+        if (part) {
+#pragma unroll
+          for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int key = 16 * (k0 + kt) + i;
+              const float w = __builtin_amdgcn_exp2f(fmaf(x[kt][i], mul, -cur.lse));
+              sum[k0 + kt][i] += (pages >> (k0 + kt) & 1) && key >= from && key < to ? w : 0.f;
+            }
+        } else {
+#pragma unroll
+          for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              sum[k0 + kt][i] += __builtin_amdgcn_exp2f(fmaf(x[kt][i], mul, -cur.lse));
+        }
       }
       cur = nxt;
     }
   }
   // the 16 columns of a key
 #pragma unroll
-  for (int kt = 0; kt < 4; ++kt)
+  for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float v = sum[kt][i];
@@ -156,21 +164,25 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weights_kernel(WeightArgs a) {
   auto put = [&](int t, float v) __attribute__((always_inline)) {
     a.acc_out[base + t] = a.acc ? fmaf(a.decay, a.acc[base + t], v) : v;
   };
-  // lane (kg, r16) has the sums of keys 16 kt + 4 kg + i: it keeps that of kt = r16 / 4,
-  // i = r16 % 4, which makes one key a lane
-  float mine = 0.f;
+  // lane (kg, r16) has the sums of keys 16 kt + 4 kg + i: it keeps those of
+  // 4 (kt % 4) + i = r16, one key a lane and 64
 #pragma unroll
-  for (int kt = 0; kt < 4; ++kt)
+  for (int e = 0; e < NK / 4; ++e) {
+    float mine = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) mine = r16 == 4 * kt + i ? sum[kt][i] : mine;
-  const int key = 16 * (r16 >> 2) + 4 * kg + (r16 & 3);
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mine = r16 == 4 * kt + i ? sum[4 * e + kt][i] : mine;
+    const int key = 64 * e + 16 * (r16 >> 2) + 4 * kg + (r16 & 3);
+    if (ROWS)
+      s_sum[wave][key] = mine;
+    else if (t0 + key < cap)
+      put(t0 + key, mine);
+  }
   if (ROWS) {
-    s_sum[wave][key] = mine;
     __syncthreads();
-    if (tid < 64 && t0 + tid < cap)
+    if (tid < kKeys && t0 + tid < cap)
       put(t0 + tid, (s_sum[0][tid] + s_sum[1][tid]) + (s_sum[2][tid] + s_sum[3][tid]));
-  } else if (t0 + key < cap) {
-    put(t0 + key, mine);
   }
 }
 
@@ -185,7 +197,7 @@ void launch(const WeightArgs& a, dim3 grid, hipStream_t s) {
 }
 template <bool ROWS>
 void launch(const WeightArgs& a, int dtype, int d, hipStream_t s) {
-  const int keys = ROWS ? 64 : 64 * kWaves, cap = a.pages.cap();
+  const int keys = ROWS ? 128 : 64 * kWaves, cap = a.pages.cap();
   const dim3 grid((unsigned)((cap + keys - 1) / keys) * (unsigned)a.h_kv, (unsigned)a.n_seq);
   if (dtype == SPOT_DTYPE_BF16)
     d == 128 ? launch<Bf16, 128, ROWS>(a, grid, s) : launch<Bf16, 64, ROWS>(a, grid, s);
