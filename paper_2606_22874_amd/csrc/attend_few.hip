@@ -28,7 +28,6 @@ using dec::wave_lds_sync;
 
 constexpr int kRows = 16;          // rows of a tile
 constexpr int kWaves = 4;
-constexpr int kMinBlocks = 2;      // fewest blocks of a part
 constexpr int kListBlocks = 512;   // blocks whose pages are looked up at once
 
 template <int D>
@@ -130,9 +129,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
   const int G = a.h_q / a.h_kv, g = blockIdx.x % a.h_kv;
   const int cap = a.pages.cap();
   if (wave == 0) {
-    const Part p = find_part<kRows, kMinBlocks>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len,
-                                                a.n_seq, a.rows, G, a.h_kv, a.rule.window, cap,
-                                                a.from, a.to);
+    const Part p = find_part<kRows, 0>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len, a.n_seq,
+                                       a.rows, G, a.h_kv, a.rule.window, cap, a.from, a.to);
     if (lane == 0) sm.part = p;
   }
   __syncthreads();

@@ -36,7 +36,6 @@ using dec::lanes_sum_xor32;
 
 constexpr int kRows = 256;         // rows of a tile
 constexpr int kWaves = 8;
-constexpr int kMinBlocks = 4;      // fewest blocks of a part
 constexpr int kRound = 256;        // workgroups at once: one a CU
 constexpr int kListBlocks = 512;   // blocks whose pages are looked up at once
 typedef __attribute__((address_space(3))) void lds_void;
@@ -322,9 +321,8 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
   const int G = a.h_q / a.h_kv, g = blockIdx.x % a.h_kv;
   const int cap = a.pages.cap();
   if (wave == 0) {
-    const Part p = find_part<kRows, kMinBlocks, kRound>(blockIdx.x / a.h_kv, a.seq_start,
-                                                        a.seq_len, a.n_seq, a.rows, G, a.h_kv,
-                                                        a.rule.window, cap, a.from, a.to);
+    const Part p = find_part<kRows, kRound>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len, a.n_seq,
+                                            a.rows, G, a.h_kv, a.rule.window, cap, a.from, a.to);
     if (lane == 0) {
       s_part = p;
       s_odd = 0;

@@ -194,12 +194,19 @@ __device__ __forceinline__ int span_blocks(const Seq& q, int window, int cap) {
 }
 
 // The part of unit `unit` (of the parts of all tiles of TR rows, one KV head), found by
-// one wave; every lane gets it.  Sequences of from < rows <= to (new tokens x heads)
-// take part.  MIN_BLOCKS: fewest blocks of a part.  ROUND: workgroups that the device
-// holds at once, each as long as its blocks; the blocks of a part then grow from
-// their least number, up to three times as many, to what ends first: rounds of
-// workgroups x (blocks of a part + 8, about what a part costs beside them).
-template <int TR, int MIN_BLOCKS, int ROUND = 0>
+// one wave; every lane gets it.  Sequences of from < rows (new tokens x heads) <= to
+// take part.  A tile has at most kMaxJoin parts: the one that joins them reads them
+// all.
+// ROUND 0 (many workgroups at once, bound by the keys' bytes): parts of at least 2, 4
+// or 8 blocks by the number of tiles, as splitting costs a join (us, decode, 2 / 4 / 8:
+// one sequence of 700 tokens, 8 tiles, 9.8 / 11.3 / 12.9; 8 of 700, 64 tiles, 13.2 /
+// 12.4 / 13.6; 16 of 300, 128 tiles, 13.2 / 11.9 / 11.0).
+// ROUND > 0: that many workgroups run at once, each as long as its blocks; the blocks
+// of a part then grow from their least number, up to three times as many, to what
+// ends first: rounds of workgroups x (blocks of a part + 8, about what a part costs
+// beside them).
+constexpr int kMaxJoin = 64;
+template <int TR, int ROUND>
 __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
                                           const int32_t* seq_len, int n_seq, int rows, int G,
                                           int h_kv, int window, int cap, int from, int to) {
@@ -210,24 +217,28 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
   };
   // all steps
   float steps = 0.f;
+  int tiles = 0;
   Seq q0 = {0, 0, 0};
   for (int base = 0; base < n_seq; base += 64) {
     Seq q = {0, 0, 0};
     if (base + lane < n_seq) q = sequence(seq_start, seq_len, base + lane, rows);
     if (base == 0) q0 = q;
-    steps += wave_sum((float)tiles_of(q) * (float)span_blocks(q, window, cap));
+    const int T = tiles_of(q);
+    steps += wave_sum((float)T * (float)span_blocks(q, window, cap));
+    if (!ROUND) tiles += wave_sum_i(T);
   }
-  int per = max(MIN_BLOCKS, (int)ceilf(steps * (float)h_kv / (float)kTarget));
+  const int least = ROUND ? 4 : tiles * h_kv <= 16 ? 2 : tiles * h_kv <= 96 ? 4 : 8;
+  int per = max(least, (int)ceilf(steps * (float)h_kv / (float)kTarget));
   if (ROUND && n_seq <= 64) {
     const int T = tiles_of(q0), nb = T ? span_blocks(q0, window, cap) : 0;
     if (__ballot(nb > per)) {
       int best = 0x7fffffff, at = per;
       for (int e = 8; e <= 24; e += e < 12 ? 1 : 2) {
-        const int p = (per * e + 7) / 8, ns = max(1, (nb + p - 1) / p);
+        const int p = (per * e + 7) / 8, ns = min(max(1, (nb + p - 1) / p), kMaxJoin);
         const int units = wave_sum_i(T * ns) * h_kv;
         // the longest part of any tile
         const int most = (int)wave_max_u((uint32_t)((nb + ns - 1) / ns));
-        const int cost = (units + ROUND - 1) / ROUND * (most + 8);
+        const int cost = (units + ROUND - 1) / max(ROUND, 1) * (most + 8);
         if (cost < best) {
           best = cost;
           at = p;
@@ -247,7 +258,7 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
       if (base + lane < n_seq) q = sequence(seq_start, seq_len, base + lane, rows);
     }
     const int T = tiles_of(q), nb = span_blocks(q, window, cap);
-    const int ns = max(1, (nb + per - 1) / per);
+    const int ns = min(max(1, (nb + per - 1) / per), kMaxJoin);
     const int units = T * ns;
     const int incl = wave_incl_scan_i(units);
     const int split_units = ns > 1 ? units : 0, split_tiles = ns > 1 ? T : 0;
