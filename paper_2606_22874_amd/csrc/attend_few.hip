@@ -36,9 +36,13 @@ struct Smem {
     float ml[kWaves][kRows][2];
     alignas(16) float o[kWaves][kRows][D];
   };
+  struct Join {
+    float weight[kMaxJoin][kRows];  // of part and row: 2^(m - M) / L
+  };
   union {
     alignas(16) unsigned char kv[kWaves][2 * 16 * D * 2];   // a wave's V rows, then its K rows
     Merge merge;
+    Join join;
   };
   int list[kListBlocks * 4];       // pool row of each 16-key group, -1 without a page
   Part part;
@@ -54,66 +58,6 @@ __device__ __forceinline__ int swz_k(int r, int c) {
 template <int D>
 __device__ __forceinline__ int swz_v(int r, int c) {
   return D == 128 ? c ^ ((r & 7) << 1) : c ^ (((r >> 1) & 3) << 1);
-}
-
-// Joins the n parts of one row: part u's (m, l) at ml + u * 2 * kRows, its O at
-// o + u * D * kRows; lane = dims lane * D/64 ...  One order, so deterministic.
-template <class T, int D>
-__device__ __forceinline__ void join_row(const float* ml, const float* o, int n, uint16_t* out,
-                                         float* lse, int lane) {
-  constexpr int PL = D / 64;
-  float M = -INFINITY;
-  bool bad = false;
-  for (int u = lane; u < n; u += 64) {
-    const float2 t = dec::load_coherent(ml + (size_t)u * 2 * kRows);
-    bad = bad || t.y != t.y;
-    if (t.y > 0.f) M = fmaxf(M, t.x);
-  }
-  M = wave_max(M);
-  float L = 0.f, acc[PL] = {};
-  if (M > -INFINITY) {
-    for (int base = 0; base < n; base += 64) {
-      float w = 0.f, lw = 0.f;
-      if (base + lane < n) {
-        const float2 t = dec::load_coherent(ml + (size_t)(base + lane) * 2 * kRows);
-        if (t.y > 0.f) {
-          w = __builtin_amdgcn_exp2f(t.x - M);
-          lw = t.y * w;
-        }
-      }
-      L += wave_sum(lw);
-      const int nn = min(64, n - base);
-      for (int u0 = 0; u0 < nn; u0 += 8) {   // 8 loads in flight
-        float v[8][PL];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const float* src = o + (size_t)(base + min(u0 + u, nn - 1)) * D * kRows + lane * PL;
-          if constexpr (PL == 2) {
-            const float2 t = dec::load_coherent(src);
-            v[u][0] = t.x;
-            v[u][1] = t.y;
-          } else {
-            v[u][0] = __hip_atomic_load(src, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          }
-        }
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-          if (u0 + u < nn) {
-            const float wt = readlane_f(w, u0 + u);
-#pragma unroll
-            for (int e = 0; e < PL; ++e)
-              if (wt > 0.f) acc[e] = fmaf(v[u][e], wt, acc[e]);
-          }
-      }
-    }
-  }
-  if (__ballot(bad)) L = NAN;
-  const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : NAN);
-  if constexpr (PL == 2)
-    reinterpret_cast<uint32_t*>(out)[lane] = T::pack2(acc[0] * inv, acc[1] * inv);
-  else
-    out[lane] = T::round(acc[0] * inv);
-  if (lse && lane == 0) *lse = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
 }
 
 template <class T, int D, bool CAP, bool BIAS>
@@ -395,10 +339,73 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
               (unsigned)(pt.n_split - 1);
   __syncthreads();
   if (!sm.last) return;
-  for (int c = wave; c < n_real; c += kWaves) {
+  // Row c of 16 threads: each has the (m, l) of every 16th part, then D / 16 dims.  The
+  // first parts' O is on its way while the weights are made.
+  constexpr int E = D / 32, U = 4;           // float pairs of a thread; parts in flight
+  const int c = min(tid >> 4, n_real - 1), k = tid & 15, n = pt.n_split;
+  const float* const ml = a.ws.ml + (slot0 * kRows + c) * 2;
+  const float* const po = a.ws.o + (slot0 * kRows + c) * D + k * 2 * E;
+  float2 v[U][E];
+  auto load = [&](int u0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        v[u][e] = dec::load_coherent(po + (size_t)min(u0 + u, n - 1) * kRows * D + 2 * e);
+  };
+  load(0);
+  constexpr int P = kMaxJoin / 16;
+  float2 t[P];
+  float M = -INFINITY, L = 0.f;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    t[i] = make_float2(-INFINITY, 0.f);
+    if (k + 16 * i < n) t[i] = dec::load_coherent(ml + (size_t)(k + 16 * i) * kRows * 2);
+  }
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+    if (t[i].y != 0.f) M = fmaxf(M, t[i].x);
+  M = fmaxf(M, dpp_f<kDppQuadXor1>(M));
+  M = fmaxf(M, dpp_f<kDppQuadXor2>(M));
+  M = fmaxf(M, dpp_f<kDppHalfMirror>(M));
+  M = fmaxf(M, dpp_f<kDppMirror>(M));
+  float wt[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    wt[i] = t[i].y != 0.f ? __builtin_amdgcn_exp2f(t[i].x - M) : 0.f;
+    if (t[i].y != 0.f) L = fmaf(t[i].y, wt[i], L);
+  }
+  L += dpp_f<kDppQuadXor1>(L);
+  L += dpp_f<kDppQuadXor2>(L);
+  L += dpp_f<kDppHalfMirror>(L);
+  L += dpp_f<kDppMirror>(L);
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+    if (k + 16 * i < n) sm.join.weight[k + 16 * i][tid >> 4] = wt[i] * inv;
+  wave_lds_sync();               // a row's threads lie in one wave
+  float2 acc[E] = {};
+  for (int u0 = 0; u0 < n; u0 += U) {
+    if (u0) load(u0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u0 + u >= n) continue;
+      const float w = sm.join.weight[u0 + u][tid >> 4];
+      if (w == 0.f) continue;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        acc[e].x = fmaf(v[u][e].x, w, acc[e].x);
+        acc[e].y = fmaf(v[u][e].y, w, acc[e].y);
+      }
+    }
+  }
+  if (tid >> 4 < n_real) {
     const size_t row = row_of(c);
-    join_row<T, D>(a.ws.ml + slot0 * kRows * 2 + c * 2, a.ws.o + slot0 * kRows * D + c * D,
-                   pt.n_split, a.out + row * D, a.lse ? a.lse + row : nullptr, lane);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      reinterpret_cast<uint32_t*>(a.out + row * D)[k * E + e] = T::pack2(acc[e].x, acc[e].y);
+    if (a.lse && k == 0)
+      a.lse[row] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
   }
   if (tid == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }

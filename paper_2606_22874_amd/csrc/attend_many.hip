@@ -591,14 +591,20 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
   const float* const ml = a.ws.ml + slot0 * kRows * 2;
   if (tid < n_real) {
     float M = -INFINITY, L = 0.f;
-    for (int u = 0; u < n; ++u) {
-      const float2 t = dec::load_coherent(ml + ((size_t)u * kRows + tid) * 2);
-      if (t.y != 0.f) {
-        const float m = fmaxf(M, t.x);
-        L = L * (M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - m)) +
-            t.y * __builtin_amdgcn_exp2f(t.x - m);
-        M = m;
-      }
+    for (int u0 = 0; u0 < n; u0 += 8) {
+      float2 t[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        t[u] = dec::load_coherent(ml + ((size_t)min(u0 + u, n - 1) * kRows + tid) * 2);
+      float m = M;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (t[u].y != 0.f) m = fmaxf(m, t[u].x);
+      L *= M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - m);
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (t[u].y != 0.f && u0 + u < n) L = fmaf(t[u].y, __builtin_amdgcn_exp2f(t[u].x - m), L);
+      M = m;
     }
     s_join[tid][0] = M;
     s_join[tid][1] = L == 0.f ? 0.f : 1.f / L;

@@ -202,9 +202,9 @@ __device__ __forceinline__ int span_blocks(const Seq& q, int window, int cap) {
 // one sequence of 700 tokens, 8 tiles, 9.8 / 11.3 / 12.9; 8 of 700, 64 tiles, 13.2 /
 // 12.4 / 13.6; 16 of 300, 128 tiles, 13.2 / 11.9 / 11.0).
 // ROUND > 0: that many workgroups run at once, each as long as its blocks; the blocks
-// of a part then grow from their least number, up to three times as many, to what
-// ends first: rounds of workgroups x (blocks of a part + 8, about what a part costs
-// beside them).
+// of a part then grow from their least number, up to four times as many, to what ends
+// first: rounds of workgroups x (blocks of a part + 8, about what a part costs beside
+// them), and a join, about a block for each part.
 constexpr int kMaxJoin = 64;
 template <int TR, int ROUND>
 __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
@@ -233,12 +233,13 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
     const int T = tiles_of(q0), nb = T ? span_blocks(q0, window, cap) : 0;
     if (__ballot(nb > per)) {
       int best = 0x7fffffff, at = per;
-      for (int e = 8; e <= 24; e += e < 12 ? 1 : 2) {
+      for (int e = 8; e <= 32; e += e < 12 ? 1 : e < 20 ? 2 : 4) {
         const int p = (per * e + 7) / 8, ns = min(max(1, (nb + p - 1) / p), kMaxJoin);
         const int units = wave_sum_i(T * ns) * h_kv;
         // the longest part of any tile
         const int most = (int)wave_max_u((uint32_t)((nb + ns - 1) / ns));
-        const int cost = (units + ROUND - 1) / max(ROUND, 1) * (most + 8);
+        const int cost = (units + ROUND - 1) / max(ROUND, 1) * (most + 8) +
+                         (int)wave_max_u((uint32_t)ns);
         if (cost < best) {
           best = cost;
           at = p;
