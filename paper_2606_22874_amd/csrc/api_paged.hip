@@ -46,15 +46,22 @@ spot_status check_rope(int d, int rope_dim, const double* freq, float amp, int f
 }
 
 // Rows (new tokens x heads of a group) of a sequence up to which it goes to the kernel of
-// 16-row tiles, beyond them to that of 256.  The lengths are on the device, so the
-// host knows their mean alone: where that is within 16, the first kernel takes all
-// of them (a call has one launch in a decode step), and with one sequence either one
-// does; otherwise both are launched, and each passes over the other's sequences.
-constexpr int kFewRows = 64;
-bool launch_many(int n_seq, int rows, int G) {
-  return (int64_t)rows * G > (n_seq == 1 ? kFewRows : 16 * (int64_t)n_seq);
+// 16-row tiles, beyond them to that of 256.  The first reads the keys once for every 16
+// rows, the second computes 256 however many there are, on fewer workgroups.  8 KV
+// heads, 16 / 64 / 128 / 256 rows, us, first and second kernel: 32768 tokens 48, 70,
+// 105, 169 and 64, 70, 93, 139; 4096 tokens 19, 26, 26, 32 and 30, 33, 41, 60; eight
+// sequences of 4096 34, 62, 90 and 34, 57, 65.
+// The lengths are on the device, so the host knows the mean of the rows and the table's
+// size alone: where the mean is within 16, the first kernel takes all of them (a call
+// has one launch in a decode step), and with one sequence either one does; otherwise
+// both are launched, and each passes over the other's sequences.
+constexpr int kFewRows = 64, kFewRowsShort = 256, kShortCache = 8192;
+int few_rows(int n_seq, int64_t cap) {
+  return n_seq == 1 && cap <= kShortCache ? kFewRowsShort : kFewRows;
 }
-bool launch_few(int n_seq, int rows, int G) { return n_seq > 1 || !launch_many(n_seq, rows, G); }
+bool launch_many(int n_seq, int rows, int G, int64_t cap) {
+  return (int64_t)rows * G > (n_seq == 1 ? few_rows(n_seq, cap) : 16 * (int64_t)n_seq);
+}
 
 const uint16_t* in16(const void* p) { return static_cast<const uint16_t*>(p); }
 uint16_t* out16(void* p) { return static_cast<uint16_t*>(p); }
@@ -172,7 +179,9 @@ spot_status spot_rotary_append(const void* q, int64_t q_stride, const void* k, i
 
 size_t spot_paged_workspace_bytes(int n_seq, int rows, int h_q, int h_kv, int d) {
   if (n_seq < 1 || rows < 1 || h_q < 1 || h_kv < 1 || d < 1) return 0;
-  return launch_many(n_seq, rows, h_q / h_kv) ? attend_many_workspace(d) : attend_few_workspace(d);
+  // A call with a short cache may go to the first kernel, one with a long to the second.
+  return launch_many(n_seq, rows, h_q / h_kv, kShortCache + 1) ? attend_many_workspace(d)
+                                                               : attend_few_workspace(d);
 }
 
 spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, const void* v_pages,
@@ -208,7 +217,8 @@ spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, con
   a.out = out16(out);
   a.lse = lse;
   const int G = h_q / h_kv;
-  const bool many = launch_many(n_seq, rows, G), few = launch_few(n_seq, rows, G);
+  const int64_t cap = (int64_t)max_pages * page_size;
+  const bool many = launch_many(n_seq, rows, G, cap), few = n_seq > 1 || !many;
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e = hipSuccess;
   if (many) {

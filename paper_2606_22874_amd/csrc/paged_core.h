@@ -200,7 +200,10 @@ __device__ __forceinline__ int span_blocks(const Seq& q, int window, int cap) {
 // ROUND 0 (many workgroups at once, bound by the keys' bytes): parts of at least 2, 4
 // or 8 blocks by the number of tiles, as splitting costs a join (us, decode, 2 / 4 / 8:
 // one sequence of 700 tokens, 8 tiles, 9.8 / 11.3 / 12.9; 8 of 700, 64 tiles, 13.2 /
-// 12.4 / 13.6; 16 of 300, 128 tiles, 13.2 / 11.9 / 11.0).
+// 12.4 / 13.6; 16 of 300, 128 tiles, 13.2 / 11.9 / 11.0), and at most twice the root of
+// a tile's blocks, where blocks of a part and parts of a join add least (one sequence
+// of 4000 tokens 17.8 us without that bound, 15.1 with it, 16.3 with 2.5 times the
+// root; two of them 21.2 at 2.5, 16.8).
 // ROUND > 0: that many workgroups run at once, each as long as its blocks; the blocks
 // of a part then grow from their least number, up to four times as many, to what ends
 // first: rounds of workgroups x (blocks of a part + 8, about what a part costs beside
@@ -211,6 +214,9 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
                                           const int32_t* seq_len, int n_seq, int rows, int G,
                                           int h_kv, int window, int cap, int from, int to) {
   const int lane = __lane_id();
+  auto most_parts = [](int nb) {
+    return ROUND ? kMaxJoin : min(kMaxJoin, (int)ceilf(2.f * sqrtf((float)nb)));
+  };
   auto tiles_of = [&](const Seq& q) {
     const int n = q.n * G;
     return n > from && n <= to ? (int)(((unsigned)n + TR - 1) / TR) : 0;
@@ -259,7 +265,7 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
       if (base + lane < n_seq) q = sequence(seq_start, seq_len, base + lane, rows);
     }
     const int T = tiles_of(q), nb = span_blocks(q, window, cap);
-    const int ns = min(max(1, (nb + per - 1) / per), kMaxJoin);
+    const int ns = max(1, min((nb + per - 1) / per, most_parts(nb)));
     const int units = T * ns;
     const int incl = wave_incl_scan_i(units);
     const int split_units = ns > 1 ? units : 0, split_tiles = ns > 1 ? T : 0;
