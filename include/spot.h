@@ -828,11 +828,12 @@ spot_status spot_paged_weights(const void *q, const float *lse, int dtype, const
  *             padded with -1
  *  new_len    device int32 [n_seq] (output): min(len, budget); not seq_len itself
  *  acc_out    device float [n_seq, h_kv, out_cap] (output): their weights, then zeros;
- *             not acc itself.  out_cap >= budget
+ *             not acc itself
  *
- * Supported: d a multiple of 8, 8 <= d <= 1024; n_seq, h_kv <= 65535.  Errors:
- * SPOT_ERR_RULE where budget < 1, n_sink or n_recent < 0 or n_sink + n_recent >
- * budget; SPOT_ERR_SHAPE where budget exceeds dst_max_pages * page_size or out_cap.
+ * Supported: d a multiple of 8, 8 <= d <= 1024; n_seq, h_kv <= 65535; budget, out_cap
+ * <= 2^30.  Errors: SPOT_ERR_RULE where budget < 1, n_sink or n_recent < 0 or n_sink +
+ * n_recent > budget; SPOT_ERR_SHAPE where min(budget, max_pages * page_size), the most
+ * that can stay, exceeds dst_max_pages * page_size or out_cap.
  */
 spot_status spot_cache_evict(const float *acc, const void *k_pages, const void *v_pages,
                              const int32_t *page_table, int n_pages, int page_size,

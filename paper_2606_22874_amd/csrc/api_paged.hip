@@ -1,5 +1,6 @@
 // C ABI of the operators on a paged cache: argument validation, then kernel
 // launches.  Nothing is enqueued unless every argument check passes.
+#include <algorithm>
 #include <math.h>
 
 #include "paged_core.h"
@@ -284,7 +285,9 @@ spot_status spot_cache_evict(const float* acc, const void* k_pages, const void* 
   if (budget < 1 || n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > budget)
     return SPOT_ERR_RULE;
   if (d < 8 || d % 8 || d > 1024 || n_seq > 65535 || h_kv > 65535) return SPOT_ERR_UNSUPPORTED;
-  if (budget > (int64_t)dst_max_pages * page_size || budget > out_cap) return SPOT_ERR_SHAPE;
+  if (budget > 1 << 30 || out_cap > 1 << 30) return SPOT_ERR_UNSUPPORTED;
+  const int64_t kept = std::min((int64_t)budget, (int64_t)max_pages * page_size);   // at most
+  if (kept > (int64_t)dst_max_pages * page_size || kept > out_cap) return SPOT_ERR_SHAPE;
   if (!aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(k_dst, 16) || !aligned(v_dst, 16))
     return SPOT_ERR_SHAPE;
   if (acc_out == acc || new_len == seq_len) return SPOT_ERR_SHAPE;

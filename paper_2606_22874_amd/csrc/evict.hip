@@ -229,7 +229,7 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
                      dim3(kThreads), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t work = (int64_t)a.budget * (a.d / 8);
+  const int64_t work = (int64_t)min(a.budget, a.pages.cap()) * (a.d / 8);   // most that stays
   hipLaunchKernelGGL(evict_move_kernel,
                      dim3((unsigned)((work + 255) / 256), (unsigned)a.h_kv, (unsigned)a.n_seq),
                      dim3(256), 0, s, a);

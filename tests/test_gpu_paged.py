@@ -143,6 +143,84 @@ def test_attend_many_sequences():
     check_attend(c, **rule_of(c, "all"))
 
 
+def test_attend_many_sequences_of_many_rows():
+    """More sequences than lanes, with few and with many rows, split and whole."""
+    n = [90 if i % 9 == 4 else (i * 5) % 3 for i in range(140)]
+    length = [max(a, (67 * i) % 800 + (3000 if i % 27 == 4 else 0)) for i, a in enumerate(n)]
+    c = Cache(15, n, length, 4, 2, 64, 16, BF)
+    check_attend(c)
+    check_attend(c, **rule_of(c, "all"))
+
+
+@pytest.mark.parametrize("d,dtype", [(64, FP), (128, BF)])
+def test_attend_rule_edges_of_many_rows(d, dtype):
+    """Scales of every sign; NaN at the tokens just outside each row's rule."""
+    c = Cache(21, [150, 90], [400, 700], 4, 2, d, 16, dtype)
+    for scale in (0.0, -0.3):
+        check_attend(c, sm_scale=scale)
+    big = Cache(22, [150, 90], [400, 700], 4, 2, d, 16, dtype, scale=30.0)
+    check_attend(big)
+    check_attend(big, softcap=50.0)
+    # sequence 0, window 70: row i sees [250 + i - 69, 250 + i]; token 300 is seen by rows
+    # 50 .. 119, and token 0 by none
+    for bad in (math.nan, math.inf):
+        v = c.v.clone()
+        for t in (300, 0):
+            v[c.table[0, t // 16], :, t % 16, 7] = bad
+        out, _ = spot.paged_attend(c.q, c.k, v, c.table, c.starts, c.len, window=70)
+        o, _, tol, _ = ref.attend(c.q, c.k, c.v, c.table, c.starts, c.len, 1 / math.sqrt(d),
+                                  window=70)
+        clean = torch.ones(out.shape, dtype=torch.bool, device=DEV)
+        clean[50:120, :, 7] = False
+        assert torch.all(((out.double() - o).abs() <= tol)[clean])
+        assert not torch.any(torch.isfinite(out[50:120, :, 7]))
+    # documents of 64 tokens: token 310 is seen from its own place to the end of its document
+    first = (torch.arange(250, 400, device=DEV) // 64 * 64).to(torch.int32)
+    first = torch.cat((first, torch.zeros(90, dtype=torch.int32, device=DEV)))
+    k = c.k.clone()
+    k[c.table[0, 310 // 16], :, 310 % 16, 1] = math.nan
+    out, lse = spot.paged_attend(c.q, k, c.v, c.table, c.starts, c.len, first=first)
+    seen = torch.zeros(240, dtype=torch.bool, device=DEV)
+    seen[310 - 250:320 - 250] = True
+    assert torch.all(torch.isnan(lse[seen])) and torch.all(torch.isfinite(lse[~seen]))
+    assert torch.all(torch.isnan(out[seen])) and torch.all(torch.isfinite(out[~seen]))
+
+
+def test_attend_mixed_batch_replayed():
+    """Long chunks and single tokens in one captured call, over lengths that change
+    between the replays, with eager calls in the same workspace between them."""
+    c = Cache(31, [200, 1, 1, 40], [900, 5000, 33, 70], 8, 2, 128, 16, BF)
+    ws = spot.paged_workspace(4, 242, 8, 2, 128, DEV)
+    out, lse = torch.empty_like(c.q), torch.empty((242, 8), device=DEV)
+
+    def step(o, l, w):
+        spot.paged_attend(c.q, c.k, c.v, c.table, c.starts, c.len, softcap=30.0, out=o, lse=l,
+                          ws=w)
+
+    step(out, lse, ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(out, lse, ws)
+    want, wl = torch.empty_like(out), torch.empty_like(lse)
+    for start, length in (([0, 200, 201, 202, 242], [900, 5000, 33, 70]),
+                          ([0, 1, 2, 122, 242], [900, 4000, 400, 120]),
+                          ([0, 10, 10, 11, 242], [10, 5000, 1, 231]),
+                          ([0, 200, 201, 202, 242], [800, 1, 2, 40])):
+        c.starts.copy_(i32(start))
+        c.len.copy_(i32(length))
+        for _ in range(2):
+            want.fill_(3)
+            wl.fill_(3)
+            step(want, wl, ws)
+            out.fill_(3)
+            lse.fill_(3)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+            assert torch.equal(lse.view(torch.int32), wl.view(torch.int32))
+
+
 def test_attend_scales_and_large_scores():
     c = Cache(11, [4, 20], [100, 400], 4, 2, 128, 16, BF, scale=30.0)
     check_attend(c)
@@ -435,6 +513,26 @@ def test_evict_special_weights():
     check_evict(c, acc, 60, 50, 9)
     c.len = i32([2 ** 31 - 1, -4])
     check_evict(c, acc, 60, 50, 9)
+
+
+def test_evict_budget_beyond_the_cache():
+    """Nothing is dropped; destination and weights hold the cache, not the budget."""
+    c = Cache(3, [0, 0], [90, 33], 2, 2, 64, 16, BF, spare=0)
+    room = c.table.shape[1] * 16
+    acc = torch.rand((2, 2, room), device=DEV)
+    kd, vd = torch.zeros_like(c.k), torch.zeros_like(c.v)
+    dst = torch.arange(c.table.numel(), dtype=torch.int32, device=DEV).reshape(c.table.shape)
+    out = torch.full_like(acc, 5.0)
+    idx, new, _ = spot.cache_evict(acc, c.k, c.v, c.table, c.len, 5000, 3, 9, kd, vd, dst,
+                                   acc_out=out)
+    assert new.tolist() == [90, 33] and idx.shape == (2, 2, 5000)
+    for s, n in enumerate((90, 33)):
+        t = torch.arange(n, device=DEV)
+        assert torch.equal(idx[s, :, :n], t.int().expand(2, n)) and torch.all(idx[s, :, n:] == -1)
+        assert torch.equal(out[s, :, :n], acc[s, :, :n]) and torch.all(out[s, :, n:] == 0)
+        for a, b in ((c.k, kd), (c.v, vd)):
+            assert torch.equal(a[c.table[s].long()[t // 16], :, t % 16],
+                               b[dst[s].long()[t // 16], :, t % 16])
 
 
 def test_evict_missing_destination():

@@ -125,7 +125,12 @@ def test_evict_refusals(lib):
     for bad in (dict(budget=0), dict(sink=-1), dict(recent=-1), dict(sink=29), dict(recent=31),
                 dict(sink=2 ** 31 - 1, recent=2 ** 31 - 1)):
         assert call(f, base, **bad) == 4, bad
+    for bad in (dict(budget=2 ** 30 + 1), dict(out_cap=2 ** 30 + 1)):
+        assert call(f, base, **bad) == 3, bad
     assert call(f, base, n_seq=0) == 0
+    # a budget beyond the cache: what can stay has to fit
+    assert call(f, base, n_seq=0, budget=1000, max_pages=2) == 0
+    assert call(f, base, n_seq=0, budget=1000, max_pages=3) == 2
 
 
 def test_frequencies(lib):
