@@ -7,13 +7,19 @@
 // softmax down the lanes' columns, and O^T += V^T P^T, P^T straight from the
 // accumulators (its keys permuted like those of the transposing LDS read of V).
 //
-// The matrix cores bound it, so the two waves of a SIMD alternate: waves 0-3 run
-// matrix instructions while waves 4-7 run their softmax, then the other way round,
-// separated by barriers; block t takes half periods 2t and 2t + 1:
-//   2t      waves 0-3: P V of block t-1, K Q of block t;   waves 4-7: start the copy of
-//           K(t+1) into the buffer not in use, softmax of block t-1, wait for the copy
-//   2t + 1  waves 0-3: start the copy of V(t), softmax of block t, wait for the copy;
-//           waves 4-7: P V of block t-1, K Q of block t
+// The two waves of a SIMD share its matrix core and its vector unit, so they go through
+// a block in opposite order; period t is
+//   waves 0-3: P V of block t-1, K Q of block t; start the copy of V(t); softmax of
+//              block t; wait for the copy
+//   waves 4-7: start the copy of K(t+1); softmax of block t-1; wait for the copy;
+//              P V of block t-1, K Q of block t
+// with one barrier behind it: what a period writes, V(t) and K(t+1), lies in the buffers
+// that the period before it read last.  (A second barrier between the halves, so that
+// matrix phases and softmaxes meet exactly, costs the longer of both twice: a prompt of
+// 8192 tokens, 64 heads of 64, capped, 1653 us with it and 1341 without; plain, d = 128,
+// 1198 and 1071.)  A softmax goes at a higher priority than matrix instructions, which
+// wait for their own results anyway (16000 tokens, d = 128: 3891 to 3815 us; d = 64,
+// 8192 tokens: 963 to 811; the other way round 3848 and 945).
 // The copies fly behind a softmax and are down before the wave's next matrix phase: the
 // compiler orders the LDS reads of a wave with a copy in flight one by one.
 // K and V go from memory to LDS 16 bytes a lane (1 KiB a wave instruction), rows
@@ -460,8 +466,10 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
       }
     };
     auto matrix_phase = [&](int t, const unsigned char* k, const unsigned char* v) SPOT_INLINE {
+      __builtin_amdgcn_s_setprio(0);
       if (t >= 1 && active(t - 1)) w.pv(v);
       if (t < nb && active(t)) w.qk(k);
+      __builtin_amdgcn_s_setprio(1);      // the softmax first, where both could go on
     };
     if (second) {
       CopyK::issue(a.k, s_list, sk0, wave - kWaves / 2);
@@ -476,7 +484,6 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
       unsigned char* const vprev = P ? sv0 : sv1;
       if (!second) {
         matrix_phase(t, kcur, vprev);
-        lds_barrier();
         if (t < nb) CopyV::issue(a.v, s_list + 4 * t, vcur, wave);
         if (t < nb && active(t)) vector_phase(t);
         wait_vm();
@@ -486,7 +493,6 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
         if (t + 1 < nb) CopyK::issue(a.k, s_list + 4 * (t + 1), knext, wave - kWaves / 2);
         if (t >= 1 && active(t - 1)) vector_phase(t - 1);
         wait_vm();
-        lds_barrier();
         matrix_phase(t, kcur, vprev);
         lds_barrier();
       }
