@@ -80,6 +80,9 @@ struct Fp16 {
 // result lands in other registers than its addend, and then scores came back without
 // the chain's last product; 13 were enough, here are 16 more.
 __device__ __forceinline__ void settle(f32x4& a) { asm volatile("s_nop 15" : "+v"(a)); }
+__device__ __forceinline__ void settle(f32x4 (&a)[2]) {
+  asm volatile("s_nop 15" : "+v"(a[0]), "+v"(a[1]));
+}
 __device__ __forceinline__ void settle(f32x4 (&a)[4]) {
   asm volatile("s_nop 15" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]));
 }

@@ -2,13 +2,15 @@
 // (gfx950): acc_out[s, g, t] = decay acc[s, g, t] + sum over the rows (new tokens x
 // the heads of KV head g) of e^(x - lse), with the scores x and lse of the attention.
 //
-// A wave holds 64 or 128 keys of a KV head in registers as the A operand of
-// S^T = K Q^T, and the rows pass by 16 at a time as the B operand, the next 16 on their way from memory
-// meanwhile.  The keys come by way of LDS, so that their loads are coalesced.  Few
-// rows (a decode step, bound by the keys' bytes): the 4 waves of a workgroup take 256
-// keys.  Many rows (bound by exponentials and matrix instructions): they take the
-// same 128 keys and a quarter of the rows each.  A key belongs to one workgroup, so
-// there are no atomics and the order of the sums is fixed.
+// A wave holds 32 or 128 keys of a KV head in registers as the A operand of
+// S^T = K Q^T, and the rows pass by 16 at a time as the B operand, the next 16 on their
+// way from memory meanwhile.  The keys come by way of LDS, so that their loads are
+// coalesced.  Few rows (a decode step, bound by the keys' bytes): the 4 waves of a
+// workgroup take 128 keys between them (4.9 TB/s over four sequences of 20000 .. 32768
+// keys, 41 us).  Many rows (bound by exponentials and matrix instructions): they take
+// the same 128 keys and a quarter of the rows each (64 tokens of 64 heads over 32768
+// keys: 59 us, 580 TFLOP/s).  A key belongs to one workgroup, so there are no atomics
+// and the order of the sums is fixed.
 #include "decode_core.h"
 #include "paged_core.h"
 
@@ -17,13 +19,16 @@ namespace paged {
 namespace {
 
 constexpr int kWaves = 4;
+constexpr int kFewKeys = 32;       // keys of a wave, few rows (four sequences of 20000 ..
+                                   // 32768 keys, 41.0 us; with 64 keys, half the
+                                   // workgroups on a CU, 45.7)
 typedef __attribute__((address_space(3))) void lds_void;
 
 template <class T, int D, bool CAP, bool BIAS, bool ROWS>
 __global__ __launch_bounds__(64 * kWaves, 2) void weights_kernel(WeightArgs a) {
   constexpr int RB = D * 2, CH = D / 8;        // bytes and 16-byte chunks of a row
   constexpr int R = 1024 / RB;                 // rows of a copy instruction
-  constexpr int NK = ROWS ? 8 : 4, kKeys = 16 * NK;   // groups of 16 keys of a wave
+  constexpr int NK = ROWS ? 8 : kFewKeys / 16, kKeys = 16 * NK;   // groups of 16 keys of a wave
   constexpr int kTile = kKeys * RB;
   __shared__ __attribute__((aligned(16))) unsigned char s_k[(ROWS ? 1 : kWaves) * kTile];
   __shared__ float s_sum[ROWS ? kWaves : 1][kKeys];
@@ -34,6 +39,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weights_kernel(WeightArgs a) {
   const int t0 = (ROWS ? blockIdx.x / a.h_kv : (blockIdx.x / a.h_kv) * kWaves + wave) * kKeys;
   const Seq q = sequence(a.seq_start, a.seq_len, s, a.rows);
   const int end = min(q.len, cap);
+
+  // lane (kg, r16) ends with the sums of keys 16 kt + 4 kg + i: it keeps those of
+  // 4 (kt % 4) + i = r16, one key a lane and 64 (or 32: r16 < 8)
+  constexpr int NX = NK < 4 ? NK : 4;
+  const int mine_key = 16 * (r16 >> 2) + 4 * kg + (r16 & 3);
+  const int64_t base = ((int64_t)s * a.h_kv + g) * cap;
+  const bool mine_real = !ROWS && mine_key < kKeys && t0 + mine_key < cap;
+  // what the key has already, on its way beside the keys (in place it is this lane's)
+  const float had = a.acc && mine_real ? a.acc[base + t0 + mine_key] : 0.f;
 
   float sum[NK][4] = {};
   if (t0 < end && q.n > 0) {
@@ -118,19 +132,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weights_kernel(WeightArgs a) {
       const int from = counts ? cur.lo - (t0 + 4 * kg) : kKeys;
       const int to = counts ? cur.hi - (t0 + 4 * kg) : 0;
 #pragma unroll
-      for (int k0 = 0; k0 < NK; k0 += 4) {     // 64 keys at a time
-        f32x4 x[4];
+      for (int k0 = 0; k0 < NK; k0 += NX) {    // 64 keys at a time
+        f32x4 x[NX];
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) x[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int kt = 0; kt < NX; ++kt) x[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kc = 0; kc < D / 32; ++kc)
 #pragma unroll
-          for (int kt = 0; kt < 4; ++kt) x[kt] = T::mfma32(kf[k0 + kt][kc], cur.q[kc], x[kt]);
+          for (int kt = 0; kt < NX; ++kt) x[kt] = T::mfma32(kf[k0 + kt][kc], cur.q[kc], x[kt]);
         settle(x);
         if (CAP || BIAS) sc(x, (float)(sc.p - (t0 + 16 * k0 + 4 * kg)));
         if (part) {
 #pragma unroll
-          for (int kt = 0; kt < 4; ++kt)
+          for (int kt = 0; kt < NX; ++kt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int key = 16 * (k0 + kt) + i;
@@ -139,7 +153,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weights_kernel(WeightArgs a) {
             }
         } else {
 #pragma unroll
-          for (int kt = 0; kt < 4; ++kt)
+          for (int kt = 0; kt < NX; ++kt)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               sum[k0 + kt][i] += __builtin_amdgcn_exp2f(fmaf(x[kt][i], mul, -cur.lse));
@@ -160,29 +174,25 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weights_kernel(WeightArgs a) {
       v += dpp_f<kDppMirror>(v);
       sum[kt][i] = v;
     }
-  const int64_t base = ((int64_t)s * a.h_kv + g) * cap;
-  auto put = [&](int t, float v) __attribute__((always_inline)) {
-    a.acc_out[base + t] = a.acc ? fmaf(a.decay, a.acc[base + t], v) : v;
-  };
-  // lane (kg, r16) has the sums of keys 16 kt + 4 kg + i: it keeps those of
-  // 4 (kt % 4) + i = r16, one key a lane and 64
 #pragma unroll
-  for (int e = 0; e < NK / 4; ++e) {
+  for (int e = 0; e < NK / NX; ++e) {
     float mine = 0.f;
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt)
+    for (int kt = 0; kt < NX; ++kt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) mine = r16 == 4 * kt + i ? sum[4 * e + kt][i] : mine;
-    const int key = 64 * e + 16 * (r16 >> 2) + 4 * kg + (r16 & 3);
     if (ROWS)
-      s_sum[wave][key] = mine;
-    else if (t0 + key < cap)
-      put(t0 + key, mine);
+      s_sum[wave][64 * e + mine_key] = mine;
+    else if (mine_real)
+      a.acc_out[base + t0 + mine_key] = a.acc ? fmaf(a.decay, had, mine) : mine;
   }
   if (ROWS) {
     __syncthreads();
-    if (tid < kKeys && t0 + tid < cap)
-      put(t0 + tid, (s_sum[0][tid] + s_sum[1][tid]) + (s_sum[2][tid] + s_sum[3][tid]));
+    if (tid < kKeys && t0 + tid < cap) {
+      const float v = (s_sum[0][tid] + s_sum[1][tid]) + (s_sum[2][tid] + s_sum[3][tid]);
+      const int64_t t = base + t0 + tid;
+      a.acc_out[t] = a.acc ? fmaf(a.decay, a.acc[t], v) : v;
+    }
   }
 }
 
@@ -197,7 +207,7 @@ void launch(const WeightArgs& a, dim3 grid, hipStream_t s) {
 }
 template <bool ROWS>
 void launch(const WeightArgs& a, int dtype, int d, hipStream_t s) {
-  const int keys = ROWS ? 128 : 64 * kWaves, cap = a.pages.cap();
+  const int keys = ROWS ? 128 : kFewKeys * kWaves, cap = a.pages.cap();
   const dim3 grid((unsigned)((cap + keys - 1) / keys) * (unsigned)a.h_kv, (unsigned)a.n_seq);
   if (dtype == SPOT_DTYPE_BF16)
     d == 128 ? launch<Bf16, 128, ROWS>(a, grid, s) : launch<Bf16, 64, ROWS>(a, grid, s);
