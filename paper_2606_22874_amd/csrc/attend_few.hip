@@ -12,7 +12,9 @@
 // The four states meet in LDS; a tile split along its keys leaves (m, l, O) in the
 // workspace, and the part that finishes last joins them:
 //   M = max m,  L = sum l 2^(m - M),  out = sum O 2^(m - M) / L.
-// The keys' bytes bound it: each is read once for all 16 rows.
+// The keys' bytes bound it: each is read once for all 16 rows (decode, four sequences of
+// 131072 tokens, 8 KV heads of 128: 334 us, 6.4 TB/s).  On one short sequence the chain of
+// lengths, pages, keys and join does: 700 tokens 10.4 us, two blocks of keys a part.
 #include "decode_core.h"
 #include "paged_core.h"
 

