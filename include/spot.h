@@ -632,7 +632,8 @@ spot_status spot_sparse_prefill(const void *q, const void *k, const void *v, int
  * rows, n_s of them (none, one in a decode step, a chunk, a whole prompt), and
  * seq_len[s] counts its tokens with the new ones, so row i of the sequence is
  * token (and position) p = seq_len[s] - n_s + i of the cache.  seq_start is
- * ascending; its values are clamped to [0, rows] and a negative seq_len to 0.
+ * ascending; its values are clamped to [0, rows] and a negative seq_len to 0.  (Starts
+ * that are not ascending leave rows uncomputed or computed for either sequence.)
  * Rows before seq_start[0] and from seq_start[n_seq] on belong to no sequence:
  * their outputs are left as they were.  The lengths are read on the device only,
  * so a captured call may be replayed with others in place.

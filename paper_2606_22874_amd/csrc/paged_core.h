@@ -234,8 +234,13 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
     if (base == 0) q0 = q;
     const int T = tiles_of(q);
     steps += wave_sum((float)T * (float)span_blocks(q, window, cap));
-    if (!ROUND) tiles += wave_sum_i(T);
+    tiles += wave_sum_i(T);
   }
+  Part r;
+  r.s = -1;
+  // More tiles than ascending starts can give: the grid has no workgroups for them, and
+  // a split tile that lacks one would leave its counter standing.
+  if (tiles > (int)((unsigned)rows * (unsigned)G / TR) + n_seq) return r;
   const int least = ROUND ? 4 : tiles * h_kv <= 16 ? 2 : tiles * h_kv <= 96 ? 4 : 8;
   int per = max(least, (int)ceilf(steps * (float)h_kv / (float)kTarget));
   if (ROUND && n_seq <= 64) {
@@ -258,8 +263,6 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
     }
   }
   // the sequence that holds the unit
-  Part r;
-  r.s = -1;
   int unit0 = 0, slot0 = 0, cnt0 = 0;
   for (int base = 0; base < n_seq; base += 64) {
     Seq q = q0;

@@ -258,6 +258,23 @@ def test_attend_odd_lengths():
     check_attend(c)
 
 
+def test_attend_starts_that_overlap():
+    """Starts that are not ascending (not a valid call): nothing outside the rows, and the
+    workspace is as ready for the next call as before."""
+    for rows, cap in ((600, 2048), (40, 4096)):
+        c = Cache(17, [rows] + 9 * [0], [cap] * 10, 4, 1, 64, 16, BF)
+        ws = spot.paged_workspace(10, rows, 4, 1, 64, DEV)
+        want = check_attend(c, ws=ws)
+        good = c.starts.clone()
+        c.starts = i32([0, rows] * 5 + [rows])
+        out = torch.full((rows + 8, 4, 64), 7.0, dtype=BF, device=DEV)
+        spot.paged_attend(c.q, c.k, c.v, c.table, c.starts, c.len, out=out[:rows], ws=ws)
+        assert torch.all(out[rows:] == 7.0) and torch.all(ws[:2048] == 0)
+        c.starts = good
+        got = check_attend(c, ws=ws)
+        assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
 def test_attend_one_sequence_of_nan():
     """NaN and infinities of one sequence, one row or one document stay there."""
     for d in (64, 128):
