@@ -716,6 +716,35 @@ def test_other_streams_and_graphs():
             assert torch.equal(want[k], got[k]), (k, length)
 
 
+def test_shared_pages_and_two_streams_at_once():
+    """Sequences with a common prefix in the same pages, and calls that overlap in time,
+    each in a workspace of its own."""
+    c = Cache(41, [3, 90, 1], [700, 790, 701], 8, 2, 128, 64, BF)
+    c.table[1, :9] = c.table[0, :9]
+    c.table[2, :9] = c.table[0, :9]
+    want = check_attend(c, **rule_of(c, "all"))
+    w, tol = ref.weights(c.q, want[1], c.k, c.table, c.starts, c.len, 1 / math.sqrt(128), cap=20.0,
+                         **{k: v for k, v in rule_of(c, "all").items() if k != "softcap"})
+    got = spot.paged_weights(c.q, want[1], c.k, c.table, c.starts, c.len, **rule_of(c, "all"))
+    assert torch.all((got.double() - w).abs() <= tol)
+    big = Cache(42, [1, 300], [20000, 9000], 8, 2, 128, 64, BF)
+    calls = []
+    for x in (c, big, c, big):
+        rows = x.q.shape[0]
+        calls.append((x, spot.paged_workspace(len(x.n), rows, 8, 2, 128, DEV),
+                      torch.empty_like(x.q), torch.empty((rows, 8), device=DEV),
+                      torch.cuda.Stream()))
+    alone = [spot.paged_attend(x.q, x.k, x.v, x.table, x.starts, x.len) for x, *_ in calls]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for x, ws, out, lse, side in calls:
+            spot.paged_attend(x.q, x.k, x.v, x.table, x.starts, x.len, out=out, lse=lse, ws=ws,
+                              stream=side)
+    torch.cuda.synchronize()
+    for (_, _, out, lse, _), (o, l) in zip(calls, alone):
+        assert torch.equal(out, o) and torch.equal(lse, l)
+
+
 def test_refusals():
     c = Cache(1, [2, 1], [40, 30], 4, 2, 128, 16, BF)
     ok = dict(q=c.q, k_pages=c.k, v_pages=c.v, page_table=c.table, seq_start=c.starts,
