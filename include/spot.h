@@ -641,7 +641,9 @@ spot_status spot_sparse_prefill(const void *q, const void *k, const void *v, int
  * Element types: SPOT_DTYPE_BF16 or SPOT_DTYPE_FP16, the same for every array of a
  * call that has no other type given.  Arrays of no rows (rows = 0) or no sequences
  * may be NULL.  Limits: max_pages * page_size <= 2^30,
- * n_pages * h_kv * page_size < 2^31, rows * h_q < 2^31 (SPOT_ERR_SHAPE).
+ * n_pages * h_kv * page_size < 2^31, rows * h_q < 2^31 (SPOT_ERR_SHAPE; so do sizes
+ * that need 2^32 threads in a launch: 2^24 rows to rotate, 2^28 rows x heads of decode
+ * steps, 2^22 sequences x KV heads to evict from).
  */
 #define SPOT_DTYPE_BF16 0
 #define SPOT_DTYPE_FP16 1
@@ -710,7 +712,8 @@ spot_status spot_rotary(const void *x, int64_t x_stride, const int32_t *pos, int
  * its keys and values to a paged cache, in one launch (Section 2.1 and Appendix A;
  * Table 1 for the scaling): spot_rotary of every head of q into q_out and of every
  * head of k into the slot of its token in k_pages; v is copied to v_pages.  Tokens
- * that are not there (see above) and those with a negative position store nothing.
+ * that are not there (see above) or whose place in the cache is negative store
+ * nothing.
  *
  *  q, k, v  device [rows, h_q, d], [rows, h_kv, d] twice, with row strides in
  *           elements (slices of a fused projection's output may be given)

@@ -10,7 +10,11 @@ using namespace spot::paged;
 
 namespace {
 
-spot_status from_hip(hipError_t e) { return e == hipSuccess ? SPOT_OK : SPOT_ERR_HIP; }
+spot_status from_hip(hipError_t e) {
+  return e == hipSuccess                      ? SPOT_OK
+         : e == hipErrorInvalidConfiguration ? SPOT_ERR_SHAPE     // see launchable()
+                                             : SPOT_ERR_HIP;
+}
 
 bool aligned(const void* p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
@@ -108,6 +112,7 @@ spot_status spot_rotary(const void* x, int64_t x_stride, const int32_t* pos, int
   const int64_t row = (int64_t)heads * d;
   if (row > 1 << 24 || x_stride < row || out_stride < row || !aligned(x, 2) || !aligned(out, 2))
     return SPOT_ERR_SHAPE;
+  if (rows > 1 && out == x && out_stride != x_stride) return SPOT_ERR_SHAPE;
   if (rows == 0) return SPOT_OK;
   RotaryArgs a = {};
   a.q = in16(x);

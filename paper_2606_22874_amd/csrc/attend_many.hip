@@ -685,7 +685,9 @@ hipError_t launch_attend_many(AttendArgs a, int dtype, int d, void* ws, hipStrea
   a.ws.counters = static_cast<unsigned*>(ws);
   a.ws.ml = reinterpret_cast<float*>(static_cast<char*>(ws) + kCounterBytes);
   a.ws.o = a.ws.ml + (size_t)kMaxParts * kRows * 2;
-  const dim3 grid(attend_grid<kRows>(a));
+  const int64_t groups = attend_grid<kRows>(a);
+  if (!launchable(groups, 64 * kWaves)) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)groups);
   if (dtype == SPOT_DTYPE_BF16)
     d == 128 ? launch<Bf16, 128>(a, grid, s) : launch<Bf16, 64>(a, grid, s);
   else

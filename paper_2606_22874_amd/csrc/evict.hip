@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
   __shared__ Shared sm;
   const int tid = threadIdx.x;
   const int g = blockIdx.x % a.h_kv, s = blockIdx.x / a.h_kv;
-  const int cap = a.pages.cap();
+  const int cap = a.pages.room();
   const int len = min(max(a.seq_len[s], 0), cap);
   const int keep = min(len, a.budget);
   const float* acc = a.acc + ((int64_t)s * a.h_kv + g) * cap;
@@ -227,13 +227,13 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
 }  // namespace
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)a.n_seq * (unsigned)a.h_kv),
-                     dim3(kThreads), 0, s, a);
+  const int64_t work = (int64_t)min(a.budget, a.pages.room()) * (a.d / 8);   // most that stays
+  const int64_t heads = (int64_t)a.n_seq * a.h_kv, groups = (work + 255) / 256;
+  if (!launchable(heads, kThreads) || !launchable(groups, 256)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)heads), dim3(kThreads), 0, s, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int64_t work = (int64_t)min(a.budget, a.pages.cap()) * (a.d / 8);   // most that stays
-  hipLaunchKernelGGL(evict_move_kernel,
-                     dim3((unsigned)((work + 255) / 256), (unsigned)a.h_kv, (unsigned)a.n_seq),
+  if (e != hipSuccess || groups == 0) return e;
+  hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)groups, (unsigned)a.h_kv, (unsigned)a.n_seq),
                      dim3(256), 0, s, a);
   return hipGetLastError();
 }

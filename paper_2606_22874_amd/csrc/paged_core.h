@@ -308,6 +308,11 @@ struct Workspace {
 };
 constexpr size_t kCounterBytes = (kMaxSplit * sizeof(unsigned) + 255) / 256 * 256;
 
+// A launch's threads are counted in 32 bits a dimension.
+inline bool launchable(int64_t groups, unsigned threads) {
+  return groups < ((int64_t)1 << 32) / threads;
+}
+
 struct AttendArgs {
   const uint16_t *q, *k, *v;
   Pages pages;
@@ -328,12 +333,12 @@ size_t attend_many_workspace(int d);
 // Workgroups of a launch over tiles of TR rows: every tile in one part, and the parts
 // that kTarget shares of the work add.
 template <int TR>
-inline unsigned attend_grid(const AttendArgs& a) {
+inline int64_t attend_grid(const AttendArgs& a) {
   const int64_t rows = (int64_t)a.rows * (a.h_q / a.h_kv);
   int64_t tiles = rows / TR + a.n_seq;
   const int64_t most = (int64_t)a.n_seq * ((a.to - 1) / TR + 1);   // of sequences up to a.to
   if (tiles > most) tiles = most;
-  return (unsigned)((tiles + kTarget / a.h_kv + 2) * a.h_kv);
+  return (tiles + kTarget / a.h_kv + 2) * a.h_kv;
 }
 
 struct WeightArgs {

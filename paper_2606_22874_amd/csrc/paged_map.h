@@ -15,7 +15,9 @@ __device__ __forceinline__ int most(int a, int b) { return a > b ? a : b; }
 struct Pages {
   const int32_t* table;     // [n_seq, max_pages]
   int n_pages, page_size, max_pages;
-  __host__ __device__ __forceinline__ int cap() const { return n_pages > 0 ? max_pages * page_size : 0; }
+  // Tokens of a sequence: that its table has places for, and that may be there at all.
+  __host__ __device__ __forceinline__ int room() const { return max_pages * page_size; }
+  __host__ __device__ __forceinline__ int cap() const { return n_pages > 0 ? room() : 0; }
   // First row (of a pool of [n_pages, h_kv, page_size] rows) of the 16 keys from
   // token t (a multiple of 16, below cap()) of KV head g; -1 where the page's id
   // lies outside the pool.

@@ -176,6 +176,7 @@ void launch(const RotaryArgs& a, bool vec, bool il, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_rotary(const RotaryArgs& a, int dtype, bool interleaved, hipStream_t s) {
+  if (!launchable(a.rows, kThreads)) return hipErrorInvalidConfiguration;
   auto whole = [](const void* p, int64_t stride) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0;
   };

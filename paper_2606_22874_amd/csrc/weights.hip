@@ -34,11 +34,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weights_kernel(WeightArgs a) {
   __shared__ float s_sum[ROWS ? kWaves : 1][kKeys];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int r16 = lane & 15, kg = lane >> 4;
-  const int G = a.h_q / a.h_kv, cap = a.pages.cap();
+  const int G = a.h_q / a.h_kv, cap = a.pages.room();
   const int g = blockIdx.x % a.h_kv, s = blockIdx.y;
   const int t0 = (ROWS ? blockIdx.x / a.h_kv : (blockIdx.x / a.h_kv) * kWaves + wave) * kKeys;
   const Seq q = sequence(a.seq_start, a.seq_len, s, a.rows);
-  const int end = min(q.len, cap);
+  const int end = min(q.len, a.pages.cap());
 
   // lane (kg, r16) ends with the sums of keys 16 kt + 4 kg + i: it keeps those of
   // 4 (kt % 4) + i = r16, one key a lane and 64 (or 32: r16 < 8)
@@ -206,26 +206,28 @@ void launch(const WeightArgs& a, dim3 grid, hipStream_t s) {
   hipLaunchKernelGGL(f, grid, dim3(64 * kWaves), 0, s, a);
 }
 template <bool ROWS>
-void launch(const WeightArgs& a, int dtype, int d, hipStream_t s) {
-  const int keys = ROWS ? 128 : kFewKeys * kWaves, cap = a.pages.cap();
-  const dim3 grid((unsigned)((cap + keys - 1) / keys) * (unsigned)a.h_kv, (unsigned)a.n_seq);
+hipError_t launch(const WeightArgs& a, int dtype, int d, hipStream_t s) {
+  const int keys = ROWS ? 128 : kFewKeys * kWaves, cap = a.pages.room();
+  const int64_t groups = (int64_t)((cap + keys - 1) / keys) * a.h_kv;
+  if (!launchable(groups, 64 * kWaves)) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)groups, (unsigned)a.n_seq);
   if (dtype == SPOT_DTYPE_BF16)
     d == 128 ? launch<Bf16, 128, ROWS>(a, grid, s) : launch<Bf16, 64, ROWS>(a, grid, s);
   else
     d == 128 ? launch<Fp16, 128, ROWS>(a, grid, s) : launch<Fp16, 64, ROWS>(a, grid, s);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_weights(const WeightArgs& a, int dtype, int d, hipStream_t s) {
-  if (a.pages.cap() == 0) return hipSuccess;
+  if (a.pages.room() == 0) return hipSuccess;
   // By the mean of the rows (new tokens x heads of a group), as the lengths are on the
   // device.  8 KV heads, us, few / many: 32768 keys 32 rows 17 / 22, 64 rows 24 / 24, 128
   // rows 39 / 31; eight sequences of 4096 17 / 24, 25 / 26, 40 / 33; one 4.5 / 5.8,
   // 5.9 / 6.2, 8.6 / 8.0.
   const bool many = (int64_t)a.rows * (a.h_q / a.h_kv) > 64 * (int64_t)a.n_seq;
-  many ? launch<true>(a, dtype, d, s) : launch<false>(a, dtype, d, s);
-  return hipGetLastError();
+  return many ? launch<true>(a, dtype, d, s) : launch<false>(a, dtype, d, s);
 }
 
 }  // namespace paged

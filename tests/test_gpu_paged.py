@@ -564,6 +564,34 @@ def test_evict_missing_destination():
     assert torch.equal(kd[1, 0, 0], c.k[c.table[0, 3], 0, 2])
 
 
+def test_empty_pools_and_tables():
+    """No page in the pool, or no place in the table: tokens that are not there."""
+    c = Cache(8, [2, 5], [40, 70], 4, 2, 64, 16, BF)
+    n, rows, width = 2, 7, c.table.shape[1]
+    for n_pages, w in ((0, width), (c.k.shape[0], 0)):
+        out, lse = torch.full_like(c.q, 7.0), torch.full((rows, 4), 7.0, device=DEV)
+        ws = spot.paged_workspace(n, rows, 4, 2, 64, DEV)
+        args = [n_pages, 16, w, c.starts, c.len, n, rows, 4, 2, 64, 0.125, 0.0, None, 0, None, None]
+        spot.spot_paged_attend(c.q, c.k, c.v, c.table, *args, out, lse, ws)
+        assert torch.all(out == 0) and torch.all(lse == -math.inf)
+        acc = torch.rand((n, 2, width * 16), device=DEV)
+        got = torch.full_like(acc, 7.0)
+        spot.spot_paged_weights(c.q, lse, c.k, c.table, *args, acc, 0.5, got)
+        assert torch.equal(got, 0.5 * acc if w else torch.full_like(acc, 7.0))
+        kd, vd = torch.full_like(c.k, 3.0), torch.full_like(c.v, 3.0)
+        dst = torch.arange(2 * n, dtype=torch.int32, device=DEV)
+        idx = torch.empty((n, 2, 30), dtype=torch.int32, device=DEV)
+        new, acc2 = i32([9, 9]), torch.full((n, 2, 32), 7.0, device=DEV)
+        spot.spot_cache_evict(acc, c.k, c.v, c.table, n_pages, 16, w, c.len, n, 2, 64, 30, 1, 2,
+                              kd, vd, dst, c.k.shape[0], 2, idx, new, acc2, 32)
+        stay = 30 if w else 0
+        assert new.tolist() == [stay] * n
+        assert torch.all(idx[:, :, stay:] == -1) and torch.all(acc2[:, :, stay:] == 0)
+        for a in (kd, vd):
+            assert torch.all(a[:4].reshape(2, 2, 2, 16, 64).transpose(1, 2).reshape(
+                2, 2, 32, 64)[:, :, :stay] == 0) and torch.all(a[4:] == 3.0)
+
+
 def test_long_pool_offsets():
     """A pool of more than 2^32 elements, its last pages in use."""
     page, h_kv, d = 64, 4, 128

@@ -83,7 +83,8 @@ def test_rotary_refusals(lib):
     for name in ("x", "pos", "freq", "out"):
         assert call(f, base, **{name: None}) == 1, name
     for bad in (dict(rows=-1), dict(heads=0), dict(xs=255), dict(os=255), dict(x=P(17)),
-                dict(out=P(17)), dict(heads=2 ** 20, xs=2 ** 40, os=2 ** 40)):
+                dict(out=P(17)), dict(heads=2 ** 20, xs=2 ** 40, os=2 ** 40),
+                dict(x=P(32), out=P(32), os=264), dict(rows=2 ** 24)):
         assert call(f, base, **bad) == 2, bad
     for bad in (dict(d=127), dict(d=0), dict(d=1026), dict(rope=63), dict(rope=130), dict(rope=-2),
                 dict(rope=258, d=512, xs=1024, os=1024), dict(dtype=2), dict(amp=NAN),
