@@ -11,10 +11,12 @@ plain arguments; whatever it does not take (it answers None and has enqueued
 nothing) goes through the Python checks below, which are the reference for
 what is accepted and for every error.
 
-Convenience wrappers without the ``spot_`` prefix allocate outputs with torch.
+Convenience wrappers without the ``spot_`` prefix allocate outputs with torch, on the
+stream that the call goes to.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -801,6 +803,21 @@ def spot_probe_stream_read(buf, sink, stream=None):
 
 
 # --------------------------------------------------- allocating wrappers
+_HERE = contextlib.nullcontext()
+
+
+def _on(stream, device, *given):
+    """The context in which a wrapper makes what the caller left out: the call's stream.
+    What fills a tensor has to come before the kernel, and its memory may not be given to
+    another stream's work while the kernel runs."""
+    if stream is None or device.type == "cpu" or all(t is not None for t in given):
+        return _HERE
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device) if int(stream) else \
+            torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
+
+
 def selector_score(q_sel, w, k_sel, k_scale=None, kfmt="bf16", rows_per_seq=1, n_valid=None,
                    nblk=None, out=None, stream=None):
     """Block scores [rows, nblk] float32 for q_sel [rows, h_s, d_s]."""
@@ -811,8 +828,9 @@ def selector_score(q_sel, w, k_sel, k_scale=None, kfmt="bf16", rows_per_seq=1, n
         f = KFMT.get(kfmt, kfmt)
         per = h_s * d_s if f in (0, 3, 4) else h_s * d_s // 2
         nblk = k_sel.numel() // (n_seq * per)
-    if out is None:
-        out = torch.empty((rows, nblk), dtype=torch.float32, device=q_sel.device)
+    with _on(stream, q_sel.device, out):
+        if out is None:
+            out = torch.empty((rows, nblk), dtype=torch.float32, device=q_sel.device)
     spot_selector_score(q_sel, w, k_sel, k_scale, kfmt, n_seq, rows_per_seq, nblk, h_s, d_s,
                         n_valid, out, stream)
     return out
@@ -829,8 +847,9 @@ def selector_score_tokens(q_sel, w, k_tok, k_scale=None, kfmt="bf16", rows_per_s
         f = KFMT.get(kfmt, kfmt)
         per = h_s * d_s if f in (0, 3, 4) else h_s * d_s // 2
         l_cap = k_tok.numel() // (n_seq * per)
-    if out is None:
-        out = torch.empty((rows, l_cap // blk), dtype=torch.float32, device=q_sel.device)
+    with _on(stream, q_sel.device, out):
+        if out is None:
+            out = torch.empty((rows, l_cap // blk), dtype=torch.float32, device=q_sel.device)
     if blk == 64:
         spot_selector_score_tokens(q_sel, w, k_tok, k_scale, kfmt, n_seq, rows_per_seq, l_cap,
                                    h_s, d_s, seq_len, out, stream)
@@ -843,12 +862,13 @@ def selector_score_tokens(q_sel, w, k_tok, k_scale=None, kfmt="bf16", rows_per_s
 def select_blocks(scores, rule, n_valid=None, idx=None, count=None, nuc_mass=None, stream=None):
     rows, nblk = scores.shape
     dev = scores.device
-    if idx is None:
-        idx = torch.empty((rows, rule.k_max), dtype=torch.int32, device=dev)
-    if count is None:
-        count = torch.empty(rows, dtype=torch.int32, device=dev)
-    if nuc_mass is None:
-        nuc_mass = torch.empty(rows, dtype=torch.float32, device=dev)
+    with _on(stream, dev, idx, count, nuc_mass):
+        if idx is None:
+            idx = torch.empty((rows, rule.k_max), dtype=torch.int32, device=dev)
+        if count is None:
+            count = torch.empty(rows, dtype=torch.int32, device=dev)
+        if nuc_mass is None:
+            nuc_mass = torch.empty(rows, dtype=torch.float32, device=dev)
     spot_select_blocks(scores, rows, nblk, n_valid, rule.top_p, rule.k_max, rule.k_min,
                        rule.n_sink, rule.n_recent, idx, count, nuc_mass, stream)
     return idx, count, nuc_mass
@@ -868,12 +888,13 @@ def sparse_decode(q, k, v, seq_len, idx, count, sm_scale=None, out=None, lse=Non
     _, h_kv, l_cap, _ = k.shape
     k_max = idx.shape[-1]
     sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
-    if out is None:
-        out = torch.empty((batch, h_q, d), dtype=torch.bfloat16, device=q.device)
-    if lse is None:
-        lse = torch.empty((batch, h_q), dtype=torch.float32, device=q.device)
-    if ws is None:
-        ws = decode_workspace(batch, h_q, h_kv, d, k_max, q.device)
+    with _on(stream, q.device, out, lse, ws):
+        if out is None:
+            out = torch.empty((batch, h_q, d), dtype=torch.bfloat16, device=q.device)
+        if lse is None:
+            lse = torch.empty((batch, h_q), dtype=torch.float32, device=q.device)
+        if ws is None:
+            ws = decode_workspace(batch, h_q, h_kv, d, k_max, q.device)
     if blk == 64:
         spot_sparse_decode(q, k, v, seq_len, idx, count, k_max, batch, h_q, h_kv, d, l_cap,
                            sm_scale, out, lse, ws, stream)
@@ -887,12 +908,13 @@ def dense_decode(q, k, v, seq_len, sm_scale=None, out=None, lse=None, ws=None, s
     batch, h_q, d = q.shape
     _, h_kv, l_cap, _ = k.shape
     sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
-    if out is None:
-        out = torch.empty((batch, h_q, d), dtype=torch.bfloat16, device=q.device)
-    if lse is None:
-        lse = torch.empty((batch, h_q), dtype=torch.float32, device=q.device)
-    if ws is None:
-        ws = decode_workspace(batch, h_q, h_kv, d, l_cap // BLK, q.device)
+    with _on(stream, q.device, out, lse, ws):
+        if out is None:
+            out = torch.empty((batch, h_q, d), dtype=torch.bfloat16, device=q.device)
+        if lse is None:
+            lse = torch.empty((batch, h_q), dtype=torch.float32, device=q.device)
+        if ws is None:
+            ws = decode_workspace(batch, h_q, h_kv, d, l_cap // BLK, q.device)
     spot_dense_decode(q, k, v, seq_len, batch, h_q, h_kv, d, l_cap, sm_scale, out, lse, ws,
                       stream)
     return out, lse
@@ -903,10 +925,11 @@ def sparse_prefill(q, k, v, idx, count, sm_scale=None, out=None, lse=None, strea
     h_kv = k.shape[1]
     k_max = idx.shape[-1]
     sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
-    if out is None:
-        out = torch.empty_like(q, dtype=torch.bfloat16)
-    if lse is None:
-        lse = torch.empty((batch, h_q, L), dtype=torch.float32, device=q.device)
+    with _on(stream, q.device, out, lse):
+        if out is None:
+            out = torch.empty_like(q, dtype=torch.bfloat16)
+        if lse is None:
+            lse = torch.empty((batch, h_q, L), dtype=torch.float32, device=q.device)
     spot_sparse_prefill(q, k, v, L, idx, count, k_max, batch, h_q, h_kv, d, sm_scale, out, lse,
                         stream)
     return out, lse
@@ -929,14 +952,15 @@ def decode_step(q_sel, w, k_sel, q, k, v, seq_len, rule, k_scale=None, kfmt="bf1
     nblk = l_cap // BLK
     dev = q.device
     sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
-    scores = torch.empty((batch, nblk), dtype=torch.float32, device=dev)
-    idx = torch.empty((batch, rule.k_max), dtype=torch.int32, device=dev)
-    count = torch.empty(batch, dtype=torch.int32, device=dev)
-    mass = torch.empty(batch, dtype=torch.float32, device=dev)
-    out = torch.empty((batch, h_q, d), dtype=torch.bfloat16, device=dev)
-    lse = torch.empty((batch, h_q), dtype=torch.float32, device=dev)
-    if ws is None:
-        ws = step_workspace(batch, h_q, h_kv, d, rule.k_max, dev)
+    with _on(stream, dev, None):
+        scores = torch.empty((batch, nblk), dtype=torch.float32, device=dev)
+        idx = torch.empty((batch, rule.k_max), dtype=torch.int32, device=dev)
+        count = torch.empty(batch, dtype=torch.int32, device=dev)
+        mass = torch.empty(batch, dtype=torch.float32, device=dev)
+        out = torch.empty((batch, h_q, d), dtype=torch.bfloat16, device=dev)
+        lse = torch.empty((batch, h_q), dtype=torch.float32, device=dev)
+        if ws is None:
+            ws = step_workspace(batch, h_q, h_kv, d, rule.k_max, dev)
     spot_decode_step(q_sel, w, k_sel, k_scale, kfmt, h_s, d_s, n_valid, rule.top_p, rule.k_max,
                      rule.k_min, rule.n_sink, rule.n_recent, q, k, v, seq_len, batch, h_q, h_kv,
                      d, l_cap, sm_scale, scores, idx, count, mass, out, lse, ws, stream,
@@ -971,8 +995,9 @@ def rotary(x, pos, freq, amp=1.0, interleaved=False, inverse=False, out=None, st
     2 len(freq) elements of each head, pairs (i, i + len(freq)) or neighbours.
     inverse: by the negative angles (also the gradient of the rotation)."""
     rows, heads, d = x.shape
-    if out is None:
-        out = torch.empty((rows, heads, d), dtype=x.dtype, device=x.device)
+    with _on(stream, x.device, out):
+        if out is None:
+            out = torch.empty((rows, heads, d), dtype=x.dtype, device=x.device)
     spot_rotary(x, _strides(x, "x"), pos, rows, heads, d, 2 * freq.numel(), freq, amp,
                 (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_INVERSE if inverse else 0), out,
                 _strides(out, "out"), stream)
@@ -985,8 +1010,9 @@ def rotary_append(q, k, v, k_pages, v_pages, page_table, seq_start, seq_len, fre
     paged cache (see spot_paged_attend), and stores v beside it; returns q_out."""
     rows, h_q, d = q.shape
     n_pages, h_kv, page, _ = k_pages.shape
-    if q_out is None:
-        q_out = torch.empty((rows, h_q, d), dtype=q.dtype, device=q.device)
+    with _on(stream, q.device, q_out):
+        if q_out is None:
+            q_out = torch.empty((rows, h_q, d), dtype=q.dtype, device=q.device)
     spot_rotary_append(q, _strides(q, "q"), k, _strides(k, "k"), v, _strides(v, "v"), pos,
                        page_table, n_pages, page, page_table.shape[1], seq_start, seq_len,
                        seq_len.shape[0], rows, h_q, h_kv, d, 2 * freq.numel(), freq, amp,
@@ -1011,12 +1037,13 @@ def paged_attend(q, k_pages, v_pages, page_table, seq_start, seq_len, sm_scale=N
     n_seq, max_pages = page_table.shape
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(d)
-    if out is None:
-        out = torch.zeros((rows, h_q, d), dtype=q.dtype, device=q.device)
-    if lse is None:
-        lse = torch.full((rows, h_q), -math.inf, dtype=torch.float32, device=q.device)
-    if ws is None:
-        ws = paged_workspace(n_seq, rows, h_q, h_kv, d, q.device)
+    with _on(stream, q.device, out, lse, ws):
+        if out is None:
+            out = torch.zeros((rows, h_q, d), dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.full((rows, h_q), -math.inf, dtype=torch.float32, device=q.device)
+        if ws is None:
+            ws = paged_workspace(n_seq, rows, h_q, h_kv, d, q.device)
     spot_paged_attend(q, k_pages, v_pages, page_table, n_pages, page, max_pages, seq_start,
                       seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes, window,
                       prefix, first, out, lse, ws, stream)
@@ -1033,8 +1060,9 @@ def paged_weights(q, lse, k_pages, page_table, seq_start, seq_len, sm_scale=None
     n_seq, max_pages = page_table.shape
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(d)
-    if out is None:
-        out = torch.empty((n_seq, h_kv, max_pages * page), dtype=torch.float32, device=q.device)
+    with _on(stream, q.device, out):
+        if out is None:
+            out = torch.empty((n_seq, h_kv, max_pages * page), dtype=torch.float32, device=q.device)
     spot_paged_weights(q, lse, k_pages, page_table, n_pages, page, max_pages, seq_start, seq_len,
                        n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes, window, prefix, first,
                        acc, decay, out, stream)
@@ -1049,13 +1077,14 @@ def cache_evict(acc, k_pages, v_pages, page_table, seq_len, budget, n_sink, n_re
     n_pages, h_kv, page, d = k_pages.shape
     n_seq, max_pages = page_table.shape
     dev = k_pages.device
-    if idx is None:
-        idx = torch.empty((n_seq, h_kv, budget), dtype=torch.int32, device=dev)
-    if new_len is None:
-        new_len = torch.empty(n_seq, dtype=torch.int32, device=dev)
-    if acc_out is None:
-        acc_out = torch.empty((n_seq, h_kv, dst_table.shape[1] * page), dtype=torch.float32,
-                              device=dev)
+    with _on(stream, dev, idx, new_len, acc_out):
+        if idx is None:
+            idx = torch.empty((n_seq, h_kv, budget), dtype=torch.int32, device=dev)
+        if new_len is None:
+            new_len = torch.empty(n_seq, dtype=torch.int32, device=dev)
+        if acc_out is None:
+            acc_out = torch.empty((n_seq, h_kv, dst_table.shape[1] * page), dtype=torch.float32,
+                                  device=dev)
     spot_cache_evict(acc, k_pages, v_pages, page_table, n_pages, page, max_pages, seq_len, n_seq,
                      h_kv, d, budget, n_sink, n_recent, k_dst, v_dst, dst_table, k_dst.shape[0],
                      dst_table.shape[1], idx, new_len, acc_out, acc_out.shape[-1], stream)
