@@ -758,10 +758,11 @@ spot_status spot_rotary_append(const void *q, int64_t q_stride, const void *k, i
  *  prefix     device int32 [n_seq] or NULL;  first  device int32 [rows] or NULL
  *  out        device [rows, h_q, d] (output, rounded to nearest even), 16-byte aligned
  *  lse        device float [rows, h_q] (output, may be NULL)
- *  ws         device, at least spot_paged_workspace_bytes(...) of these sizes, 16-byte
- *             aligned, zero-filled before its first use; every call leaves it ready
- *             for the next one, of any sizes it is large enough for.  Calls that may
- *             overlap in time need separate workspaces.
+ *  ws         device, at least spot_paged_workspace_bytes(...) of these sizes or of
+ *             more sequences or rows, 16-byte aligned, its first
+ *             SPOT_PAGED_WORKSPACE_ZEROS bytes zero before its first use; every call
+ *             leaves it ready for the next one, of any sizes it is large enough for.
+ *             Calls that may overlap in time need separate workspaces.
  *
  * Numerics: FP32 scores and softmax, the probabilities rounded to the element type
  * for the product with V (FP32 accumulation).  The division of the work depends on
@@ -770,6 +771,10 @@ spot_status spot_rotary_append(const void *q, int64_t q_stride, const void *k, i
  * Supported: d 64 or 128, h_q any multiple of h_kv, finite sm_scale, softcap finite
  * and >= 0 (SPOT_ERR_UNSUPPORTED otherwise).
  */
+#define SPOT_PAGED_WORKSPACE_ZEROS 4096
+
+/* Bytes for every call of at most n_seq sequences and at most rows rows of these heads
+ * (grows with n_seq, rows and d; 0 where there is nothing to do). */
 size_t spot_paged_workspace_bytes(int n_seq, int rows, int h_q, int h_kv, int d);
 
 spot_status spot_paged_attend(const void *q, int dtype, const void *k_pages, const void *v_pages,

@@ -185,9 +185,12 @@ spot_status spot_rotary_append(const void* q, int64_t q_stride, const void* k, i
 
 size_t spot_paged_workspace_bytes(int n_seq, int rows, int h_q, int h_kv, int d) {
   if (n_seq < 1 || rows < 1 || h_q < 1 || h_kv < 1 || d < 1) return 0;
-  // A call with a short cache may go to the first kernel, one with a long to the second.
-  return launch_many(n_seq, rows, h_q / h_kv, kShortCache + 1) ? attend_many_workspace(d)
-                                                               : attend_few_workspace(d);
+  // Enough for every call of at most these sequences and rows: of as many rows the fewest
+  // sequences go to the second kernel first, two before one.
+  const int G = h_q / h_kv;
+  const bool many = launch_many(1, rows, G, kShortCache + 1) ||
+                    (n_seq > 1 && launch_many(2, rows, G, kShortCache + 1));
+  return many ? attend_many_workspace(d) : attend_few_workspace(d);
 }
 
 spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, const void* v_pages,
@@ -206,7 +209,11 @@ spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, con
   if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16))
     return SPOT_ERR_SHAPE;
   if (rows == 0 || n_seq == 0) return SPOT_OK;
-  if (!ws || ws_bytes < spot_paged_workspace_bytes(n_seq, rows, h_q, h_kv, d) || !aligned(ws, 16))
+  const int G = h_q / h_kv;
+  const int64_t cap = (int64_t)max_pages * page_size;
+  const bool many = launch_many(n_seq, rows, G, cap), few = n_seq > 1 || !many;
+  if (!ws || ws_bytes < (many ? attend_many_workspace(d) : attend_few_workspace(d)) ||
+      !aligned(ws, 16))
     return SPOT_ERR_WORKSPACE;
   AttendArgs a = {};
   a.q = in16(q);
@@ -222,9 +229,6 @@ spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, con
   a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first};
   a.out = out16(out);
   a.lse = lse;
-  const int G = h_q / h_kv;
-  const int64_t cap = (int64_t)max_pages * page_size;
-  const bool many = launch_many(n_seq, rows, G, cap), few = n_seq > 1 || !many;
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e = hipSuccess;
   if (many) {

@@ -306,7 +306,8 @@ struct Workspace {
   float* ml;            // [kMaxParts, TR, 2]
   float* o;             // [kMaxParts, TR, d]
 };
-constexpr size_t kCounterBytes = (kMaxSplit * sizeof(unsigned) + 255) / 256 * 256;
+constexpr size_t kCounterBytes = SPOT_PAGED_WORKSPACE_ZEROS;
+static_assert(kMaxSplit * sizeof(unsigned) <= kCounterBytes, "room for the counters");
 
 // A launch's threads are counted in 32 bits a dimension.
 inline bool launchable(int64_t groups, unsigned threads) {

@@ -201,6 +201,7 @@ U8 = (torch.uint8,)
 PAGED_DTYPE = {torch.bfloat16: 0, torch.float16: 1}
 ROPE_SCALING = {"none": 0, "linear": 1, "ntk": 2, "parts": 3, "yarn": 3}
 ROPE_INTERLEAVED, ROPE_INVERSE = 1, 2
+PAGED_WORKSPACE_ZEROS = 4096
 
 
 def _check(fn: str, st: int):
@@ -1021,9 +1022,12 @@ def rotary_append(q, k, v, k_pages, v_pages, page_table, seq_start, seq_len, fre
 
 
 def paged_workspace(n_seq, rows, h_q, h_kv, d, device="cuda"):
-    """Zero-filled workspace of paged_attend (each call leaves it ready for the next)."""
+    """Workspace of paged_attend for calls of at most n_seq sequences and rows rows, its
+    counters at zero (each call leaves it ready for the next)."""
     n = spot_paged_workspace_bytes(n_seq, rows, h_q, h_kv, d)
-    return torch.zeros(max(n, 16), dtype=torch.uint8, device=device)
+    ws = torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+    ws[:PAGED_WORKSPACE_ZEROS].zero_()
+    return ws
 
 
 def paged_attend(q, k_pages, v_pages, page_table, seq_start, seq_len, sm_scale=None, softcap=0.0,

@@ -100,3 +100,19 @@ def test_nothing_is_entered_for_tensors_that_are_given(name, log):
     log.clear()
     getattr(spot, name)(*args, stream=77, **given)
     assert [x[0] for x in log] == ["call"]
+
+
+def test_paged_workspace_grows_with_the_call():
+    """What is enough for n sequences and m rows is enough for fewer of either: a serving
+    loop keeps the workspace of its largest batch."""
+    spot.load()
+    size = spot.spot_paged_workspace_bytes
+    for h_q, h_kv in ((32, 8), (8, 8), (32, 1), (6, 2), (96, 1)):
+        for d in (64, 128):
+            n_seq, rows = (1, 2, 3, 4, 8, 64, 65, 1000), (1, 2, 3, 5, 8, 9, 16, 17, 33, 64, 65, 4000)
+            got = [[size(n, r, h_q, h_kv, d) for r in rows] for n in n_seq]
+            for a in got:
+                assert a == sorted(a) and a[0] >= spot.PAGED_WORKSPACE_ZEROS
+            for a in zip(*got):
+                assert list(a) == sorted(a)
+    assert size(0, 5, 8, 8, 64) == size(5, 0, 8, 8, 64) == 0
