@@ -639,11 +639,11 @@ spot_status spot_sparse_prefill(const void *q, const void *k, const void *v, int
  * so a captured call may be replayed with others in place.
  *
  * Element types: SPOT_DTYPE_BF16 or SPOT_DTYPE_FP16, the same for every array of a
- * call that has no other type given.  Arrays of no rows (rows = 0) or no sequences
- * may be NULL.  Limits: max_pages * page_size <= 2^30,
- * n_pages * h_kv * page_size < 2^31, rows * h_q < 2^31 (SPOT_ERR_SHAPE; so do sizes
- * that need 2^32 threads in a launch: 2^24 rows to rotate, 2^28 rows x heads of decode
- * steps, 2^22 sequences x KV heads to evict from).
+ * call that has no other type given.  Arrays without elements (no rows, no sequences,
+ * no pages in a pool, no places in a table) may be NULL.  Limits: max_pages *
+ * page_size <= 2^30, n_pages * h_kv * page_size < 2^31, rows * h_q < 2^31
+ * (SPOT_ERR_SHAPE; so do sizes that need 2^32 threads in a launch: 2^24 rows to rotate,
+ * 2^28 rows x heads of decode steps, 2^22 sequences x KV heads to evict from).
  */
 #define SPOT_DTYPE_BF16 0
 #define SPOT_DTYPE_FP16 1

@@ -27,6 +27,11 @@ bool valid_pages(int n_pages, int page_size, int max_pages, int h_kv) {
          (__int128)n_pages * h_kv * page_size < (__int128)1 << 31;
 }
 
+// Whether a pool or a table that has elements is not given.
+bool missing_pages(bool pools, int n_pages, const int32_t* table, int max_pages) {
+  return (n_pages > 0 && !pools) || (max_pages > 0 && !table);
+}
+
 // What spot_paged_attend and spot_paged_weights share.
 spot_status check_attend(int dtype, int n_pages, int page_size, int max_pages, int n_seq, int rows,
                          int h_q, int h_kv, int d, float sm_scale, float softcap, int window) {
@@ -140,8 +145,9 @@ spot_status spot_rotary_append(const void* q, int64_t q_stride, const void* k, i
                                const double* freq, float amp, int flags, void* q_out,
                                void* k_pages, void* v_pages, void* stream) {
   if ((!freq && rope_dim > 0) ||
-      (rows > 0 && n_seq > 0 && (!q || !k || !v || !page_table || !seq_start || !seq_len || !q_out ||
-                                 !k_pages || !v_pages)))
+      (rows > 0 && n_seq > 0 &&
+       (!q || !k || !v || !seq_start || !seq_len || !q_out ||
+        missing_pages(k_pages && v_pages, n_pages, page_table, max_pages))))
     return SPOT_ERR_NULL;
   if (n_seq < 0 || rows < 0 || h_q < 1 || !valid_pages(n_pages, page_size, max_pages, h_kv) ||
       (int64_t)rows * h_q > 0x7fffffff)
@@ -201,7 +207,8 @@ spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, con
                               const int32_t* first, void* out, float* lse, void* ws,
                               size_t ws_bytes, void* stream) {
   if (rows > 0 && n_seq > 0 &&
-      (!q || !k_pages || !v_pages || !page_table || !seq_start || !seq_len || !out))
+      (!q || !seq_start || !seq_len || !out ||
+       missing_pages(k_pages && v_pages, n_pages, page_table, max_pages)))
     return SPOT_ERR_NULL;
   const spot_status st = check_attend(dtype, n_pages, page_size, max_pages, n_seq, rows, h_q, h_kv,
                                       d, sm_scale, softcap, window);
@@ -251,7 +258,8 @@ spot_status spot_paged_weights(const void* q, const float* lse, int dtype, const
                                float softcap, const float* slopes, int window,
                                const int32_t* prefix, const int32_t* first, const float* acc,
                                float decay, float* acc_out, void* stream) {
-  if (n_seq > 0 && (!k_pages || !page_table || !seq_start || !seq_len || !acc_out ||
+  if (n_seq > 0 && (!seq_start || !seq_len || (max_pages > 0 && !acc_out) ||
+                    missing_pages(k_pages, n_pages, page_table, max_pages) ||
                     (rows > 0 && (!q || !lse))))
     return SPOT_ERR_NULL;
   const spot_status st = check_attend(dtype, n_pages, page_size, max_pages, n_seq, rows, h_q, h_kv,
@@ -285,8 +293,10 @@ spot_status spot_cache_evict(const float* acc, const void* k_pages, const void* 
                              const int32_t* dst_table, int n_dst_pages, int dst_max_pages,
                              int32_t* idx, int32_t* new_len, float* acc_out, int out_cap,
                              void* stream) {
-  if (!acc || !k_pages || !v_pages || !page_table || !seq_len || !k_dst || !v_dst || !dst_table ||
-      !idx || !new_len || !acc_out)
+  if (n_seq > 0 && (!seq_len || !idx || !new_len || (max_pages > 0 && !acc) ||
+                    (out_cap > 0 && !acc_out) ||
+                    missing_pages(k_pages && v_pages, n_pages, page_table, max_pages) ||
+                    missing_pages(k_dst && v_dst, n_dst_pages, dst_table, dst_max_pages)))
     return SPOT_ERR_NULL;
   if (n_seq < 0 || !valid_pages(n_pages, page_size, max_pages, h_kv) ||
       !valid_pages(n_dst_pages, page_size, dst_max_pages, h_kv))
@@ -299,8 +309,8 @@ spot_status spot_cache_evict(const float* acc, const void* k_pages, const void* 
   if (kept > (int64_t)dst_max_pages * page_size || kept > out_cap) return SPOT_ERR_SHAPE;
   if (!aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(k_dst, 16) || !aligned(v_dst, 16))
     return SPOT_ERR_SHAPE;
-  if (acc_out == acc || new_len == seq_len) return SPOT_ERR_SHAPE;
   if (n_seq == 0) return SPOT_OK;
+  if ((acc && acc_out == acc) || new_len == seq_len) return SPOT_ERR_SHAPE;
   EvictArgs a = {};
   a.acc = acc;
   a.k = in16(k_pages);

@@ -378,9 +378,9 @@ struct RotaryArgs {
   const uint16_t *q, *k, *v;
   int64_t q_stride, k_stride, v_stride, out_stride;   // elements from row to row
   const int32_t* pos;
-  uint16_t *q_out, *k_pages, *v_pages;                // k_pages NULL: q alone
+  uint16_t *q_out, *k_pages, *v_pages;
   Pages pages;
-  const int32_t *seq_start, *seq_len;
+  const int32_t *seq_start, *seq_len;                 // seq_start NULL: q alone
   int n_seq, rows, h_q, h_kv, d, rope_dim;
   float amp;
   bool inverse;

@@ -61,8 +61,9 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
   __shared__ float s_cos[kMaxPairs], s_sin[kMaxPairs];
   const int row = blockIdx.x, tid = threadIdx.x;
   const int half = a.rope_dim / 2;
+  const bool append = a.seq_start != nullptr;
   int pos, krow = -1;                        // krow: pool row of the slot, KV head 0
-  if (a.k_pages) {
+  if (append) {
     const Row r = find_row(a, row);
     if (r.s < 0) return;
     const int slot = r.q.len - r.q.n + r.i;
@@ -81,8 +82,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
     s_sin[tid] = a.inverse ? -sn * a.amp : sn * a.amp;
   }
   __syncthreads();
-  const int n_rot = a.h_q + (a.k_pages ? a.h_kv : 0);
-  const int n_vec = n_rot + (a.k_pages ? a.h_kv : 0);
+  const int n_rot = a.h_q + (append ? a.h_kv : 0);
+  const int n_vec = n_rot + (append ? a.h_kv : 0);
   const int d = a.d;
   // input and output of vector h: query heads, key heads, value heads
   auto place = [&](int h, const uint16_t*& in, uint16_t*& out) {
@@ -182,7 +183,7 @@ hipError_t launch_rotary(const RotaryArgs& a, int dtype, bool interleaved, hipSt
   };
   bool vec = a.d % 16 == 0 && a.rope_dim % 16 == 0 && whole(a.q, a.q_stride) &&
              whole(a.q_out, a.out_stride);
-  if (a.k_pages)
+  if (a.seq_start)
     vec = vec && whole(a.k, a.k_stride) && whole(a.v, a.v_stride) && whole(a.k_pages, 0) &&
           whole(a.v_pages, 0);
   dtype == SPOT_DTYPE_BF16 ? launch<Bf16>(a, vec, interleaved, s)
