@@ -983,6 +983,26 @@ def rope_frequencies(rope_dim, base=1.0e6, scaling="none", factor=1.0, orig_len=
     return freq, 0.1 * math.log(factor) + 1.0 if scaling == "yarn" else 1.0
 
 
+def _shape(t, name, n, *rest):
+    """[n or more, *rest]"""
+    if t is not None and (tuple(t.shape[1:]) != rest or t.shape[0] < n):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, need {(n, *rest)}")
+
+
+def _pools(k_pages, v_pages, d):
+    """[n_pages, h_kv, page_size] of two pools of d elements a token."""
+    n_pages, h_kv, page, _ = k_pages.shape
+    _shape(k_pages, "k_pages", n_pages, h_kv, page, d)
+    _shape(v_pages, "v_pages", n_pages, h_kv, page, d)
+    return n_pages, h_kv, page
+
+
+def _weights_of(t, name, cap):
+    """A row of weights is as long as a row of the page table has tokens."""
+    if t is not None and t.shape[-1] != cap:
+        raise ValueError(f"{name}: rows of {t.shape[-1]} weights for {cap} tokens")
+
+
 def _strides(t, name):
     """Row stride of [rows, heads, d] whose heads lie one after the other."""
     rows, heads, d = t.shape
@@ -996,6 +1016,7 @@ def rotary(x, pos, freq, amp=1.0, interleaved=False, inverse=False, out=None, st
     2 len(freq) elements of each head, pairs (i, i + len(freq)) or neighbours.
     inverse: by the negative angles (also the gradient of the rotation)."""
     rows, heads, d = x.shape
+    _shape(out, "out", rows, heads, d)
     with _on(stream, x.device, out):
         if out is None:
             out = torch.empty((rows, heads, d), dtype=x.dtype, device=x.device)
@@ -1010,7 +1031,10 @@ def rotary_append(q, k, v, k_pages, v_pages, page_table, seq_start, seq_len, fre
     """Rotates q [rows, h_q, d] into q_out and k [rows, h_kv, d] into the pages of a
     paged cache (see spot_paged_attend), and stores v beside it; returns q_out."""
     rows, h_q, d = q.shape
-    n_pages, h_kv, page, _ = k_pages.shape
+    n_pages, h_kv, page = _pools(k_pages, v_pages, d)
+    _shape(k, "k", rows, h_kv, d)
+    _shape(v, "v", rows, h_kv, d)
+    _shape(q_out, "q_out", rows, h_q, d)
     with _on(stream, q.device, q_out):
         if q_out is None:
             q_out = torch.empty((rows, h_q, d), dtype=q.dtype, device=q.device)
@@ -1037,7 +1061,8 @@ def paged_attend(q, k_pages, v_pages, page_table, seq_start, seq_len, sm_scale=N
     pages; k_pages, v_pages [n_pages, h_kv, page_size, d], page_table [n_seq,
     max_pages].  Returns (out [rows, h_q, d], lse [rows, h_q])."""
     rows, h_q, d = q.shape
-    n_pages, h_kv, page, _ = k_pages.shape
+    n_pages, h_kv, page = _pools(k_pages, v_pages, d)
+    _shape(out, "out", rows, h_q, d)
     n_seq, max_pages = page_table.shape
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(d)
@@ -1060,8 +1085,10 @@ def paged_weights(q, lse, k_pages, page_table, seq_start, seq_len, sm_scale=None
     """Attention weight each cached token received from q, summed per KV head, on top of
     decay * acc: [n_seq, h_kv, max_pages * page_size] float32.  lse from paged_attend."""
     rows, h_q, d = q.shape
-    n_pages, h_kv, page, _ = k_pages.shape
+    n_pages, h_kv, page = _pools(k_pages, None, d)
     n_seq, max_pages = page_table.shape
+    _weights_of(acc, "acc", max_pages * page)
+    _weights_of(out, "out", max_pages * page)
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(d)
     with _on(stream, q.device, out):
@@ -1078,8 +1105,13 @@ def cache_evict(acc, k_pages, v_pages, page_table, seq_len, budget, n_sink, n_re
     """Keeps `budget` tokens of each sequence and KV head (sinks, recent ones and the
     heaviest by acc) and copies them to the pages of dst_table; returns (idx [n_seq,
     h_kv, budget], new_len [n_seq], acc_out [n_seq, h_kv, dst_max_pages * page_size])."""
-    n_pages, h_kv, page, d = k_pages.shape
+    d = k_pages.shape[-1]
+    n_pages, h_kv, page = _pools(k_pages, v_pages, d)
+    n_dst = k_dst.shape[0]
+    _shape(k_dst, "k_dst", n_dst, h_kv, page, d)
+    _shape(v_dst, "v_dst", n_dst, h_kv, page, d)
     n_seq, max_pages = page_table.shape
+    _weights_of(acc, "acc", max_pages * page)
     dev = k_pages.device
     with _on(stream, dev, idx, new_len, acc_out):
         if idx is None:
@@ -1090,7 +1122,7 @@ def cache_evict(acc, k_pages, v_pages, page_table, seq_len, budget, n_sink, n_re
             acc_out = torch.empty((n_seq, h_kv, dst_table.shape[1] * page), dtype=torch.float32,
                                   device=dev)
     spot_cache_evict(acc, k_pages, v_pages, page_table, n_pages, page, max_pages, seq_len, n_seq,
-                     h_kv, d, budget, n_sink, n_recent, k_dst, v_dst, dst_table, k_dst.shape[0],
+                     h_kv, d, budget, n_sink, n_recent, k_dst, v_dst, dst_table, n_dst,
                      dst_table.shape[1], idx, new_len, acc_out, acc_out.shape[-1], stream)
     return idx, new_len, acc_out
 
