@@ -768,8 +768,9 @@ spot_status spot_rotary_append(const void *q, int64_t q_stride, const void *k, i
  * for the product with V (FP32 accumulation).  The division of the work depends on
  * the sizes and lengths only, and there are no floating-point atomics: the same
  * inputs give the same bits.
- * Supported: d 64 or 128, h_q any multiple of h_kv, finite sm_scale, softcap finite
- * and >= 0 (SPOT_ERR_UNSUPPORTED otherwise).
+ * Supported: d 64 or 128, h_q any multiple of h_kv, softcap >= 0, |sm_scale| and softcap
+ * at most 2.35e38 (finite when multiplied by log2(e)), and with a cap sm_scale / softcap
+ * finite, and 0 or a normal FP32 number (SPOT_ERR_UNSUPPORTED otherwise).
  */
 #define SPOT_PAGED_WORKSPACE_ZEROS 4096
 

@@ -1,6 +1,7 @@
 // C ABI of the operators on a paged cache: argument validation, then kernel
 // launches.  Nothing is enqueued unless every argument check passes.
 #include <algorithm>
+#include <float.h>
 #include <math.h>
 
 #include "paged_core.h"
@@ -39,8 +40,11 @@ spot_status check_attend(int dtype, int n_pages, int page_size, int max_pages, i
       !valid_pages(n_pages, page_size, max_pages, h_kv) || (int64_t)rows * h_q > 0x7fffffff)
     return SPOT_ERR_SHAPE;
   if (!valid_dtype(dtype) || (d != 64 && d != 128) || h_q % h_kv) return SPOT_ERR_UNSUPPORTED;
-  if (!isfinite(sm_scale) || !(softcap >= 0.f) || !isfinite(softcap) ||
-      (softcap > 0.f && !isfinite(sm_scale / softcap)))
+  // What the kernels multiply by: scale log2(e), cap log2(e) and scale / cap.
+  if (!isfinite(sm_scale * kLog2e) || !(softcap >= 0.f) || !isfinite(softcap * kLog2e))
+    return SPOT_ERR_UNSUPPORTED;
+  const float ratio = softcap > 0.f ? fabsf(sm_scale / softcap) : 0.f;
+  if (!isfinite(ratio) || (ratio < FLT_MIN && softcap > 0.f && sm_scale != 0.f))
     return SPOT_ERR_UNSUPPORTED;
   return SPOT_OK;
 }
