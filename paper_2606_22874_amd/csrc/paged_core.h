@@ -76,9 +76,11 @@ struct Fp16 {
 };
 
 // Wait states between matrix instructions and the ordinary ones that read their
-// results.  The compiler (ROCm 7.2) puts 8 after a chain of dependent MFMAs whose last
-// result lands in other registers than its addend, and then scores came back without
-// the chain's last product; 13 were enough, here are 16 more.
+// results: 8 are needed (4 passes).  Where a branch lies between, the compiler (ROCm 7.2)
+// counts them along one path only, and around a block that is skipped 1 to 3 were left:
+// scores came back without their last product.  16 states in place, before any branch,
+// make every path long enough.  The kernels that have none of this (decode, prefill,
+// scores, projections) have 8 on every path as they are built; a test looks at all.
 __device__ __forceinline__ void settle(f32x4& a) { asm volatile("s_nop 15" : "+v"(a)); }
 __device__ __forceinline__ void settle(f32x4 (&a)[2]) {
   asm volatile("s_nop 15" : "+v"(a[0]), "+v"(a[1]));
