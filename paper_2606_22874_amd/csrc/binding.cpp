@@ -687,6 +687,48 @@ PyObject* cache_evict(Args a) {
   });
 }
 
+// q, k, v, out, cap, acc, acc_out, pools...: whether the shapes that are given belong together:
+// pools [*, h_kv, page_size, d] alike, each second one with the pages of the one before it or
+// more, q [rows, *, d], k and v [rows or more, h_kv, d], out [rows or more, heads of q, d], rows
+// of acc and acc_out of cap weights.  Python's checks answer where this does not say yes.
+PyObject* paged_fits(Args a) {
+  auto tensor = [&](const Dev& t) -> const at::Tensor* {
+    if (!a.ok || t.none()) return nullptr;
+    if (!THPVariable_CheckExact(t.o)) return a.ok = false, nullptr;
+    return &THPVariable_Unpack(t.o);
+  };
+  const Dev q_(a), k_(a), v_(a), out_(a);
+  const int cap = a.integer();
+  const Dev acc_(a), acc_out_(a);
+  const at::Tensor *q = tensor(q_), *first = nullptr, *last = nullptr;
+  for (int i = 0; a.ok && a.i < a.n; ++i) {
+    const at::Tensor* p = tensor(Dev(a));
+    if (!p || p->dim() != 4 || (first && p->sizes().slice(1) != first->sizes().slice(1)) ||
+        (i % 2 && p->size(0) < last->size(0)))
+      return python_path();
+    if (!first) first = p;
+    last = p;
+  }
+  if (!a.ok || (q && q->dim() != 3) || (q && first && q->size(2) != first->size(3)))
+    return python_path();
+  for (const Dev* t : {&k_, &v_}) {
+    const at::Tensor* x = tensor(*t);
+    if (x && (x->dim() != 3 || !q || !first || x->size(0) < q->size(0) ||
+              x->size(1) != first->size(1) || x->size(2) != q->size(2)))
+      a.ok = false;
+  }
+  const at::Tensor* out = tensor(out_);
+  if (out && (out->dim() != 3 || !q || out->size(0) < q->size(0) ||
+              out->sizes().slice(1) != q->sizes().slice(1)))
+    a.ok = false;
+  for (const Dev* t : {&acc_, &acc_out_}) {
+    const at::Tensor* x = tensor(*t);
+    if (x && (x->dim() < 1 || x->size(-1) != cap)) a.ok = false;
+  }
+  if (!a.ok) return python_path();
+  Py_RETURN_TRUE;
+}
+
 // A tensor without storage or of a wrapped kind throws from its accessors:
 // the Python path then raises as it always did.
 template <PyObject* (*F)(Args)>
@@ -739,6 +781,7 @@ PyMethodDef methods[] = {{"init", init, METH_VARARGS, nullptr},
                          SPOT_ENTRY(paged_attend),
                          SPOT_ENTRY(paged_weights),
                          SPOT_ENTRY(cache_evict),
+                         SPOT_ENTRY(paged_fits),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods};
 

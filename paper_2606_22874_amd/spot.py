@@ -807,11 +807,11 @@ def spot_probe_stream_read(buf, sink, stream=None):
 _HERE = contextlib.nullcontext()
 
 
-def _on(stream, device, *given):
+def _on(stream, device):
     """The context in which a wrapper makes what the caller left out: the call's stream.
     What fills a tensor has to come before the kernel, and its memory may not be given to
     another stream's work while the kernel runs."""
-    if stream is None or device.type == "cpu" or all(t is not None for t in given):
+    if stream is None or device.type == "cpu":
         return _HERE
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(stream), device) if int(stream) else \
@@ -829,8 +829,8 @@ def selector_score(q_sel, w, k_sel, k_scale=None, kfmt="bf16", rows_per_seq=1, n
         f = KFMT.get(kfmt, kfmt)
         per = h_s * d_s if f in (0, 3, 4) else h_s * d_s // 2
         nblk = k_sel.numel() // (n_seq * per)
-    with _on(stream, q_sel.device, out):
-        if out is None:
+    if out is None:
+        with _on(stream, q_sel.device):
             out = torch.empty((rows, nblk), dtype=torch.float32, device=q_sel.device)
     spot_selector_score(q_sel, w, k_sel, k_scale, kfmt, n_seq, rows_per_seq, nblk, h_s, d_s,
                         n_valid, out, stream)
@@ -848,8 +848,8 @@ def selector_score_tokens(q_sel, w, k_tok, k_scale=None, kfmt="bf16", rows_per_s
         f = KFMT.get(kfmt, kfmt)
         per = h_s * d_s if f in (0, 3, 4) else h_s * d_s // 2
         l_cap = k_tok.numel() // (n_seq * per)
-    with _on(stream, q_sel.device, out):
-        if out is None:
+    if out is None:
+        with _on(stream, q_sel.device):
             out = torch.empty((rows, l_cap // blk), dtype=torch.float32, device=q_sel.device)
     if blk == 64:
         spot_selector_score_tokens(q_sel, w, k_tok, k_scale, kfmt, n_seq, rows_per_seq, l_cap,
@@ -863,13 +863,14 @@ def selector_score_tokens(q_sel, w, k_tok, k_scale=None, kfmt="bf16", rows_per_s
 def select_blocks(scores, rule, n_valid=None, idx=None, count=None, nuc_mass=None, stream=None):
     rows, nblk = scores.shape
     dev = scores.device
-    with _on(stream, dev, idx, count, nuc_mass):
-        if idx is None:
-            idx = torch.empty((rows, rule.k_max), dtype=torch.int32, device=dev)
-        if count is None:
-            count = torch.empty(rows, dtype=torch.int32, device=dev)
-        if nuc_mass is None:
-            nuc_mass = torch.empty(rows, dtype=torch.float32, device=dev)
+    if idx is None or count is None or nuc_mass is None:
+        with _on(stream, dev):
+            if idx is None:
+                idx = torch.empty((rows, rule.k_max), dtype=torch.int32, device=dev)
+            if count is None:
+                count = torch.empty(rows, dtype=torch.int32, device=dev)
+            if nuc_mass is None:
+                nuc_mass = torch.empty(rows, dtype=torch.float32, device=dev)
     spot_select_blocks(scores, rows, nblk, n_valid, rule.top_p, rule.k_max, rule.k_min,
                        rule.n_sink, rule.n_recent, idx, count, nuc_mass, stream)
     return idx, count, nuc_mass
@@ -889,13 +890,14 @@ def sparse_decode(q, k, v, seq_len, idx, count, sm_scale=None, out=None, lse=Non
     _, h_kv, l_cap, _ = k.shape
     k_max = idx.shape[-1]
     sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
-    with _on(stream, q.device, out, lse, ws):
-        if out is None:
-            out = torch.empty((batch, h_q, d), dtype=torch.bfloat16, device=q.device)
-        if lse is None:
-            lse = torch.empty((batch, h_q), dtype=torch.float32, device=q.device)
-        if ws is None:
-            ws = decode_workspace(batch, h_q, h_kv, d, k_max, q.device)
+    if out is None or lse is None or ws is None:
+        with _on(stream, q.device):
+            if out is None:
+                out = torch.empty((batch, h_q, d), dtype=torch.bfloat16, device=q.device)
+            if lse is None:
+                lse = torch.empty((batch, h_q), dtype=torch.float32, device=q.device)
+            if ws is None:
+                ws = decode_workspace(batch, h_q, h_kv, d, k_max, q.device)
     if blk == 64:
         spot_sparse_decode(q, k, v, seq_len, idx, count, k_max, batch, h_q, h_kv, d, l_cap,
                            sm_scale, out, lse, ws, stream)
@@ -909,13 +911,14 @@ def dense_decode(q, k, v, seq_len, sm_scale=None, out=None, lse=None, ws=None, s
     batch, h_q, d = q.shape
     _, h_kv, l_cap, _ = k.shape
     sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
-    with _on(stream, q.device, out, lse, ws):
-        if out is None:
-            out = torch.empty((batch, h_q, d), dtype=torch.bfloat16, device=q.device)
-        if lse is None:
-            lse = torch.empty((batch, h_q), dtype=torch.float32, device=q.device)
-        if ws is None:
-            ws = decode_workspace(batch, h_q, h_kv, d, l_cap // BLK, q.device)
+    if out is None or lse is None or ws is None:
+        with _on(stream, q.device):
+            if out is None:
+                out = torch.empty((batch, h_q, d), dtype=torch.bfloat16, device=q.device)
+            if lse is None:
+                lse = torch.empty((batch, h_q), dtype=torch.float32, device=q.device)
+            if ws is None:
+                ws = decode_workspace(batch, h_q, h_kv, d, l_cap // BLK, q.device)
     spot_dense_decode(q, k, v, seq_len, batch, h_q, h_kv, d, l_cap, sm_scale, out, lse, ws,
                       stream)
     return out, lse
@@ -926,11 +929,12 @@ def sparse_prefill(q, k, v, idx, count, sm_scale=None, out=None, lse=None, strea
     h_kv = k.shape[1]
     k_max = idx.shape[-1]
     sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
-    with _on(stream, q.device, out, lse):
-        if out is None:
-            out = torch.empty_like(q, dtype=torch.bfloat16)
-        if lse is None:
-            lse = torch.empty((batch, h_q, L), dtype=torch.float32, device=q.device)
+    if out is None or lse is None:
+        with _on(stream, q.device):
+            if out is None:
+                out = torch.empty_like(q, dtype=torch.bfloat16)
+            if lse is None:
+                lse = torch.empty((batch, h_q, L), dtype=torch.float32, device=q.device)
     spot_sparse_prefill(q, k, v, L, idx, count, k_max, batch, h_q, h_kv, d, sm_scale, out, lse,
                         stream)
     return out, lse
@@ -953,7 +957,7 @@ def decode_step(q_sel, w, k_sel, q, k, v, seq_len, rule, k_scale=None, kfmt="bf1
     nblk = l_cap // BLK
     dev = q.device
     sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
-    with _on(stream, dev, None):
+    with _on(stream, dev):
         scores = torch.empty((batch, nblk), dtype=torch.float32, device=dev)
         idx = torch.empty((batch, rule.k_max), dtype=torch.int32, device=dev)
         count = torch.empty(batch, dtype=torch.int32, device=dev)
@@ -989,26 +993,37 @@ def _shape(t, name, n, *rest):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, need {(n, *rest)}")
 
 
-def _pools(k_pages, v_pages, d):
-    """[n_pages, h_kv, page_size] of two pools of d elements a token."""
-    n_pages, h_kv, page, _ = k_pages.shape
-    _shape(k_pages, "k_pages", n_pages, h_kv, page, d)
-    _shape(v_pages, "v_pages", n_pages, h_kv, page, d)
-    return n_pages, h_kv, page
-
-
-def _weights_of(t, name, cap):
-    """A row of weights is as long as a row of the page table has tokens."""
-    if t is not None and t.shape[-1] != cap:
-        raise ValueError(f"{name}: rows of {t.shape[-1]} weights for {cap} tokens")
+def _fits(q, k, v, out, cap, acc, acc_out, *pools):
+    """The shapes that belong together: pools [*, h_kv, page_size, d] alike, the values' with the
+    pages of the keys' before them or more, q [rows, *, d], k and v [rows or more, h_kv, d], out
+    [rows or more, heads of q, d], rows of acc and acc_out of cap weights."""
+    if _native is not None and _native.paged_fits(q, k, v, out, cap, acc, acc_out, *pools):
+        return
+    h_kv = page = d = n = None
+    for i, (name, p) in enumerate(zip(("k_pages", "v_pages", "k_dst", "v_dst"), pools)):
+        if h_kv is None:
+            _, h_kv, page, d = p.shape
+        if q is not None:
+            d = q.shape[2]
+        _shape(p, name, n if i % 2 else 0, h_kv, page, d)
+        n = p.shape[0]
+    if q is not None:
+        rows, heads, d = q.shape
+        _shape(k, "k", rows, h_kv, d)
+        _shape(v, "v", rows, h_kv, d)
+        _shape(out, "out", rows, heads, d)
+    for name, t in (("acc", acc), ("acc_out", acc_out)):
+        if t is not None and t.shape[-1] != cap:
+            raise ValueError(f"{name}: rows of {t.shape[-1]} weights for {cap} tokens")
 
 
 def _strides(t, name):
     """Row stride of [rows, heads, d] whose heads lie one after the other."""
     rows, heads, d = t.shape
-    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+    row, head, one = t.stride()
+    if (d > 1 and one != 1) or (heads > 1 and head != d):
         raise ValueError(f"{name}: the heads of a row must lie one after the other")
-    return t.stride(0) if rows > 1 else heads * d
+    return row if rows > 1 else heads * d
 
 
 def rotary(x, pos, freq, amp=1.0, interleaved=False, inverse=False, out=None, stream=None):
@@ -1016,10 +1031,11 @@ def rotary(x, pos, freq, amp=1.0, interleaved=False, inverse=False, out=None, st
     2 len(freq) elements of each head, pairs (i, i + len(freq)) or neighbours.
     inverse: by the negative angles (also the gradient of the rotation)."""
     rows, heads, d = x.shape
-    _shape(out, "out", rows, heads, d)
-    with _on(stream, x.device, out):
-        if out is None:
+    if out is None:
+        with _on(stream, x.device):
             out = torch.empty((rows, heads, d), dtype=x.dtype, device=x.device)
+    else:
+        _fits(x, None, None, out, 0, None, None)
     spot_rotary(x, _strides(x, "x"), pos, rows, heads, d, 2 * freq.numel(), freq, amp,
                 (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_INVERSE if inverse else 0), out,
                 _strides(out, "out"), stream)
@@ -1031,12 +1047,10 @@ def rotary_append(q, k, v, k_pages, v_pages, page_table, seq_start, seq_len, fre
     """Rotates q [rows, h_q, d] into q_out and k [rows, h_kv, d] into the pages of a
     paged cache (see spot_paged_attend), and stores v beside it; returns q_out."""
     rows, h_q, d = q.shape
-    n_pages, h_kv, page = _pools(k_pages, v_pages, d)
-    _shape(k, "k", rows, h_kv, d)
-    _shape(v, "v", rows, h_kv, d)
-    _shape(q_out, "q_out", rows, h_q, d)
-    with _on(stream, q.device, q_out):
-        if q_out is None:
+    n_pages, h_kv, page, _ = k_pages.shape
+    _fits(q, k, v, q_out, 0, None, None, k_pages, v_pages)
+    if q_out is None:
+        with _on(stream, q.device):
             q_out = torch.empty((rows, h_q, d), dtype=q.dtype, device=q.device)
     spot_rotary_append(q, _strides(q, "q"), k, _strides(k, "k"), v, _strides(v, "v"), pos,
                        page_table, n_pages, page, page_table.shape[1], seq_start, seq_len,
@@ -1061,18 +1075,19 @@ def paged_attend(q, k_pages, v_pages, page_table, seq_start, seq_len, sm_scale=N
     pages; k_pages, v_pages [n_pages, h_kv, page_size, d], page_table [n_seq,
     max_pages].  Returns (out [rows, h_q, d], lse [rows, h_q])."""
     rows, h_q, d = q.shape
-    n_pages, h_kv, page = _pools(k_pages, v_pages, d)
-    _shape(out, "out", rows, h_q, d)
+    n_pages, h_kv, page, _ = k_pages.shape
+    _fits(q, None, None, out, 0, None, None, k_pages, v_pages)
     n_seq, max_pages = page_table.shape
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(d)
-    with _on(stream, q.device, out, lse, ws):
-        if out is None:
-            out = torch.zeros((rows, h_q, d), dtype=q.dtype, device=q.device)
-        if lse is None:
-            lse = torch.full((rows, h_q), -math.inf, dtype=torch.float32, device=q.device)
-        if ws is None:
-            ws = paged_workspace(n_seq, rows, h_q, h_kv, d, q.device)
+    if out is None or lse is None or ws is None:
+        with _on(stream, q.device):
+            if out is None:
+                out = torch.zeros((rows, h_q, d), dtype=q.dtype, device=q.device)
+            if lse is None:
+                lse = torch.full((rows, h_q), -math.inf, dtype=torch.float32, device=q.device)
+            if ws is None:
+                ws = paged_workspace(n_seq, rows, h_q, h_kv, d, q.device)
     spot_paged_attend(q, k_pages, v_pages, page_table, n_pages, page, max_pages, seq_start,
                       seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes, window,
                       prefix, first, out, lse, ws, stream)
@@ -1085,14 +1100,13 @@ def paged_weights(q, lse, k_pages, page_table, seq_start, seq_len, sm_scale=None
     """Attention weight each cached token received from q, summed per KV head, on top of
     decay * acc: [n_seq, h_kv, max_pages * page_size] float32.  lse from paged_attend."""
     rows, h_q, d = q.shape
-    n_pages, h_kv, page = _pools(k_pages, None, d)
+    n_pages, h_kv, page, _ = k_pages.shape
     n_seq, max_pages = page_table.shape
-    _weights_of(acc, "acc", max_pages * page)
-    _weights_of(out, "out", max_pages * page)
+    _fits(q, None, None, None, max_pages * page, acc, out, k_pages)
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(d)
-    with _on(stream, q.device, out):
-        if out is None:
+    if out is None:
+        with _on(stream, q.device):
             out = torch.empty((n_seq, h_kv, max_pages * page), dtype=torch.float32, device=q.device)
     spot_paged_weights(q, lse, k_pages, page_table, n_pages, page, max_pages, seq_start, seq_len,
                        n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes, window, prefix, first,
@@ -1105,24 +1119,21 @@ def cache_evict(acc, k_pages, v_pages, page_table, seq_len, budget, n_sink, n_re
     """Keeps `budget` tokens of each sequence and KV head (sinks, recent ones and the
     heaviest by acc) and copies them to the pages of dst_table; returns (idx [n_seq,
     h_kv, budget], new_len [n_seq], acc_out [n_seq, h_kv, dst_max_pages * page_size])."""
-    d = k_pages.shape[-1]
-    n_pages, h_kv, page = _pools(k_pages, v_pages, d)
-    n_dst = k_dst.shape[0]
-    _shape(k_dst, "k_dst", n_dst, h_kv, page, d)
-    _shape(v_dst, "v_dst", n_dst, h_kv, page, d)
+    n_pages, h_kv, page, d = k_pages.shape
     n_seq, max_pages = page_table.shape
-    _weights_of(acc, "acc", max_pages * page)
+    _fits(None, None, None, None, max_pages * page, acc, None, k_pages, v_pages, k_dst, v_dst)
     dev = k_pages.device
-    with _on(stream, dev, idx, new_len, acc_out):
-        if idx is None:
-            idx = torch.empty((n_seq, h_kv, budget), dtype=torch.int32, device=dev)
-        if new_len is None:
-            new_len = torch.empty(n_seq, dtype=torch.int32, device=dev)
-        if acc_out is None:
-            acc_out = torch.empty((n_seq, h_kv, dst_table.shape[1] * page), dtype=torch.float32,
-                                  device=dev)
+    if idx is None or new_len is None or acc_out is None:
+        with _on(stream, dev):
+            if idx is None:
+                idx = torch.empty((n_seq, h_kv, budget), dtype=torch.int32, device=dev)
+            if new_len is None:
+                new_len = torch.empty(n_seq, dtype=torch.int32, device=dev)
+            if acc_out is None:
+                acc_out = torch.empty((n_seq, h_kv, dst_table.shape[1] * page), dtype=torch.float32,
+                                      device=dev)
     spot_cache_evict(acc, k_pages, v_pages, page_table, n_pages, page, max_pages, seq_len, n_seq,
-                     h_kv, d, budget, n_sink, n_recent, k_dst, v_dst, dst_table, n_dst,
+                     h_kv, d, budget, n_sink, n_recent, k_dst, v_dst, dst_table, k_dst.shape[0],
                      dst_table.shape[1], idx, new_len, acc_out, acc_out.shape[-1], stream)
     return idx, new_len, acc_out
 

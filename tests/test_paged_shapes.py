@@ -49,3 +49,33 @@ def test_shapes_that_fit(monkeypatch):
     args[10] = i32(2, 9)
     spot.cache_evict(*args, acc_out=t(2, 2, 999, dtype=F32))
     assert len(done) == 2
+
+
+def test_native_and_python_agree(monkeypatch):
+    """The native check answers only where Python's passes, and always there."""
+    spot.load()
+    native, seen = spot._native, []
+
+    class Both:
+        def __getattr__(self, name):
+            return getattr(native, name)
+
+        @staticmethod
+        def paged_fits(*a):
+            seen.append(native.paged_fits(*a))
+            return None                              # and then Python's
+    monkeypatch.setattr(spot, "_native", Both())
+    for name, bad in BAD.items():
+        for b in [{}] + bad:
+            args = list(calls()[name][0])
+            for k, v in b.items():
+                if isinstance(k, int):
+                    args[k] = v
+            kw = {k: v for k, v in b.items() if isinstance(k, str)}
+            if not b and name == "rotary":
+                kw = dict(out=t(3, 4, 64))
+            seen.clear()
+            with pytest.raises(ValueError) as e:     # at the latest: not device tensors
+                getattr(spot, name)(*args, **kw)
+            fits = "device" in str(e.value)
+            assert fits == (not b) and seen == [True if fits else None], (name, b, str(e.value))
