@@ -675,8 +675,9 @@ spot_status spot_sparse_prefill(const void *q, const void *k, const void *v, int
  *  freq   host double [rope_dim / 2] (output; may be NULL where rope_dim is 0)
  *
  * rope_dim even, 0 <= rope_dim <= 256; rope_base finite and > 0; with a scaling,
- * factor finite and >= 1; for SPOT_ROPE_PARTS orig_len >= 1 and low < high, finite
- * (otherwise SPOT_ERR_UNSUPPORTED).  Nothing is enqueued.
+ * factor finite and >= 1; for SPOT_ROPE_PARTS orig_len >= 1 and low < high, finite;
+ * every frequency finite, and the base that SPOT_ROPE_BASE makes (otherwise
+ * SPOT_ERR_UNSUPPORTED).  Nothing is enqueued.
  */
 spot_status spot_rope_frequencies(int rope_dim, double rope_base, int scaling, double factor,
                                   int orig_len, double low, double high, double *freq);

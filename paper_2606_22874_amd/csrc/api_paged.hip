@@ -98,6 +98,10 @@ spot_status spot_rope_frequencies(int rope_dim, double rope_base, int scaling, d
   double base = rope_base;
   if (scaling == SPOT_ROPE_BASE && rope_dim > 2)
     base *= pow(factor, (double)rope_dim / (rope_dim - 2));
+  // the pair farthest from 1 is the last one
+  if (rope_dim > 0 &&
+      (!isfinite(base) || !isfinite(pow(base, -2.0 * (rope_dim / 2 - 1) / rope_dim))))
+    return SPOT_ERR_UNSUPPORTED;
   for (int i = 0; i < rope_dim / 2; ++i) {
     double f = pow(base, -2.0 * i / rope_dim);
     if (scaling == SPOT_ROPE_LINEAR) f /= factor;

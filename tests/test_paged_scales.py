@@ -32,3 +32,19 @@ def test_scales(f32, ok):
              length=nz, n_seq=2, rows=3, h_q=8, h_kv=2, d=128, scale=0.1, cap=0.0, slopes=None,
              window=0, prefix=None, first=None, acc=None, decay=1.0, out=nz, stream=None)
     assert call(lib.spot_paged_weights, w, **f32) == (0 if ok else 3)
+
+
+@pytest.mark.parametrize("kw", [dict(rope_base=1e200, scaling="ntk", factor=1e150),
+                                dict(rope_dim=4, scaling="ntk", factor=1e155),
+                                dict(rope_base=5e-324, rope_dim=256)])
+def test_frequencies_stay_finite(kw):
+    """A base or a frequency beyond FP64 is refused, not returned as infinity or zero."""
+    if not os.path.exists(build.SO):
+        build.build()
+    kw = dict(kw)
+    r, base = kw.pop("rope_dim", 64), kw.pop("rope_base", 1e4)
+    with pytest.raises(spot.SpotError) as e:
+        spot.rope_frequencies(r, base, **kw)
+    assert e.value.status == 3
+    f, _ = spot.rope_frequencies(4, 1e4, "ntk", factor=1e150)
+    assert f.tolist()[0] == 1.0 and 0 < f.tolist()[1] < 1e-100
