@@ -670,7 +670,9 @@ spot_status spot_sparse_prefill(const void *q, const void *k, const void *v, int
  * Appendix A rotates part of each head.  Frequency i of rope_dim / 2 is
  * f_i = rope_base^(-2i / rope_dim), scaled as the constants above say.  YaRN is
  * SPOT_ROPE_PARTS with low = 1, high = 32 and, in the rotations, the factor
- * amp = 0.1 ln(factor) + 1.
+ * amp = 0.1 ln(factor) + 1.  Its ramp runs in the turns of a pair, as that method's paper
+ * writes it; checkpoints whose code ramps in the pair's index between rounded ends need
+ * frequencies of that form, which the rotations take like any others.
  *
  *  freq   host double [rope_dim / 2] (output; may be NULL where rope_dim is 0)
  *
@@ -702,7 +704,8 @@ spot_status spot_rope_frequencies(int rope_dim, double rope_base, int scaling, d
  *
  * Any d and rope_dim that are even, rope_dim <= min(d, 256), d <= 1024; arrays on a
  * 2-byte boundary (16-byte chunks are used where pointers, strides, d and rope_dim
- * are multiples of 16 bytes resp. elements).  Strides >= heads * d.
+ * are multiples of 16 bytes resp. elements; otherwise pairs of 2-byte elements).
+ * Strides >= heads * d; heads * d <= 2^24.
  */
 spot_status spot_rotary(const void *x, int64_t x_stride, const int32_t *pos, int rows, int heads,
                         int d, int rope_dim, const double *freq, float amp, int flags, int dtype,
@@ -824,7 +827,8 @@ spot_status spot_paged_weights(const void *q, const float *lse, int dtype, const
  *     token first; NaN ranks below every number).
  * The kept tokens, ascending, become tokens 0, 1, ... of the head in the pages of
  * dst_table, with their weights, so that causal order stays; the heads of a sequence
- * keep different tokens, but equally many.  Later attention counts distances and
+ * keep different tokens, but equally many.  A kept token that is not there in
+ * page_table becomes one that is, with keys and values 0.  Later attention counts distances and
  * windows in places of the new cache, and rotated keys keep their angles (give
  * spot_rotary_append the text positions).
  *

@@ -22,7 +22,7 @@
 // 8192 tokens: 963 to 811; the other way round 3848 and 945).
 // The copies fly behind a softmax and are down before the wave's next matrix phase: the
 // compiler orders the LDS reads of a wave with a copy in flight one by one.
-// A prompt of 16000 tokens, 64 heads of 128 over 8: 3.8 .. 3.95 ms, 1.06 .. 1.1 PFLOP/s;
+// A prompt of 16000 tokens, 64 heads of 128 over 8: 3.8 .. 4.0 ms, 1.05 .. 1.1 PFLOP/s;
 // the matrix cores are busy 44 % of the cycles, the vector units 50 %.  Tiles of 128 rows
 // (4 waves, two workgroups a CU) read the keys twice as often: 14 % slower; a third pair
 // of buffers, or touching the next blocks ahead for L2, 3 .. 5 %.
@@ -515,7 +515,8 @@ __global__ __launch_bounds__(64 * kWaves) void attend_many_kernel(AttendArgs a) 
   __syncthreads();
   if (s_odd) {
     // The infinite and NaN elements that mend() left out, for the rows that see their
-    // tokens: p v of each, p from the row's score once more.  Rare, and slow.
+    // tokens: p v of each, p from the row's score once more.  Rare, and slow (one near the
+    // end of a 16000-token prompt makes 4 ms 14).
 #pragma unroll 1
     for (int tok = max(e0 * 64, LO); tok < min(e1 * 64, HI); ++tok) {
       const int t0 = tok & ~63;
