@@ -737,6 +737,8 @@ spot_status spot_rotary_append(const void *q, int64_t q_stride, const void *k, i
                                const double *freq, float amp, int flags, void *q_out,
                                void *k_pages, void *v_pages, void *stream);
 
+#define SPOT_PAGED_WORKSPACE_ZEROS 4096
+
 /*
  * spot_paged_attend -- attention of new tokens over a paged cache (Section 3: dense
  * attention, the method's baseline; Appendix B: attention in the prefill regime),
@@ -767,6 +769,8 @@ spot_status spot_rotary_append(const void *q, int64_t q_stride, const void *k, i
  *             SPOT_PAGED_WORKSPACE_ZEROS bytes zero before its first use; every call
  *             leaves it ready for the next one, of any sizes it is large enough for.
  *             Calls that may overlap in time need separate workspaces.
+ *             spot_paged_workspace_bytes(...) is enough for every call of at most
+ *             these sequences and rows (0 where there is nothing to do).
  *
  * Numerics: FP32 scores and softmax, the probabilities rounded to the element type
  * for the product with V (FP32 accumulation).  The division of the work depends on
@@ -776,10 +780,6 @@ spot_status spot_rotary_append(const void *q, int64_t q_stride, const void *k, i
  * at most 2.35e38 (finite when multiplied by log2(e)), and with a cap sm_scale / softcap
  * finite, and 0 or a normal FP32 number (SPOT_ERR_UNSUPPORTED otherwise).
  */
-#define SPOT_PAGED_WORKSPACE_ZEROS 4096
-
-/* Bytes for every call of at most n_seq sequences and at most rows rows of these heads
- * (grows with n_seq, rows and d; 0 where there is nothing to do). */
 size_t spot_paged_workspace_bytes(int n_seq, int rows, int h_q, int h_kv, int d);
 
 spot_status spot_paged_attend(const void *q, int dtype, const void *k_pages, const void *v_pages,
