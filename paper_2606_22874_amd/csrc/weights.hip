@@ -9,7 +9,7 @@
 // workgroup take 128 keys between them (4.9 TB/s over four sequences of 20000 .. 32768
 // keys, 41 us).  Many rows (bound by exponentials and matrix instructions): they take
 // the same 128 keys and a quarter of the rows each (64 tokens of 64 heads over 32768
-// keys: 59 us, 580 TFLOP/s).  A key belongs to one workgroup, so there are no atomics
+// keys: 60 us, 574 TFLOP/s).  A key belongs to one workgroup, so there are no atomics
 // and the order of the sums is fixed.
 #include "decode_core.h"
 #include "paged_core.h"
