@@ -737,6 +737,63 @@ spot_status spot_rotary_append(const void *q, int64_t q_stride, const void *k, i
                                const double *freq, float amp, int flags, void *q_out,
                                void *k_pages, void *v_pages, void *stream);
 
+/* Most axes of a position. */
+#define SPOT_ROPE_AXES 8
+
+/*
+ * spot_rotary_axes -- spot_rotary with positions of several axes (of images and video:
+ * time, row, column; text has the same number on all; Section 2.1 and Appendix A for the
+ * rotation): pair i takes its angle from pos[row, axis[i]] * freq[i].  Which pairs belong to which axis is the caller's (runs of
+ * pairs, or the axes in turn).  Other arguments, numerics and errors as spot_rotary.
+ *
+ *  pos      device int32 [rows, n_axes]
+ *  axis     host uint8 [rope_dim / 2], each below n_axes (read during the call; may be
+ *           NULL where rope_dim is 0)
+ *
+ * 1 <= n_axes <= SPOT_ROPE_AXES (SPOT_ERR_UNSUPPORTED); n_axes 0 is spot_rotary, pos of
+ * [rows] and axis not read.
+ */
+spot_status spot_rotary_axes(const void *x, int64_t x_stride, const int32_t *pos, int n_axes,
+                             const uint8_t *axis, int rows, int heads, int d, int rope_dim,
+                             const double *freq, float amp, int flags, int dtype, void *out,
+                             int64_t out_stride, void *stream);
+
+/*
+ * An 8-bit paged cache: the pools hold e4m3 codes (OCP: 4 exponent bits, 3 of mantissa,
+ * largest 448, NaN, no infinity), one byte an element, and beside each pool lie scales
+ * [n_pages, h_kv, page_size / 16], one byte (E8M0) for the 16 tokens from a multiple of 16
+ * of one head: the element is code * 2^(scale - 127).  Every such number is one of BF16
+ * (FP16 within its range: beyond it infinite, below it rounded), as which the attention
+ * takes it.  Scales 1 .. 254; a scale of 255 makes its elements NaN.
+ *
+ * spot_rotary_append8 -- spot_rotary_append into an 8-bit cache, with positions of one axis
+ * or several (Section 2.1 and Appendix A for the rotation; Section 5.3 quantizes the
+ * selector's cache, this the attention's).  The scale of 16 tokens and a head is the least power of two, from 2^-100 on,
+ * with which no value of the new ones among them exceeds 448; a rotated pair (a, b) of a key
+ * counts as |amp| (|a| + |b|), whatever its position.  Where earlier tokens of the 16 are in
+ * the cache, the scale is at least theirs (as the scales hold it), and if it grows, their
+ * codes are rounded again (to nearest even, as all are).  Values are rounded once, from
+ * FP32.  Infinite values become the largest that the cache and the element type have (up to
+ * 448 2^(scale - 127); FP16: 61440), NaN stays NaN; neither, nor a pair whose sum is not
+ * finite, counts for the scale.  Slots behind the last new token keep their codes.
+ *
+ *  pos, n_axes, axis   n_axes 0: pos [rows] or NULL as spot_rotary_append has it (axis is
+ *           not read); otherwise as spot_rotary_axes
+ *  k_pages, v_pages    device uint8 [n_pages, h_kv, page_size, d], 16-byte aligned
+ *  k_scale, v_scale    device uint8 [n_pages, h_kv, page_size / 16]
+ * The rest as spot_rotary_append.  d 64 or 128 (SPOT_ERR_UNSUPPORTED).  Two sequences must
+ * not write to one page in one call.
+ */
+spot_status spot_rotary_append8(const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                                const void *v, int64_t v_stride, int dtype, const int32_t *pos,
+                                int n_axes, const uint8_t *axis, const int32_t *page_table,
+                                int n_pages, int page_size, int max_pages,
+                                const int32_t *seq_start, const int32_t *seq_len, int n_seq,
+                                int rows, int h_q, int h_kv, int d, int rope_dim,
+                                const double *freq, float amp, int flags, void *q_out,
+                                void *k_pages, void *v_pages, uint8_t *k_scale, uint8_t *v_scale,
+                                void *stream);
+
 #define SPOT_PAGED_WORKSPACE_ZEROS 4096
 
 /*
@@ -789,6 +846,41 @@ spot_status spot_paged_attend(const void *q, int dtype, const void *k_pages, con
                               float softcap, const float *slopes, int window,
                               const int32_t *prefix, const int32_t *first, void *out, float *lse,
                               void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * spot_paged_attend_sinks -- spot_paged_attend with first tokens that stay visible behind a
+ * window (Section 2.3 always keeps a sink prefix): a row also sees the tokens t, up to its own and below hi, of
+ *     [max(0, first[row]), max(0, first[row]) + n_sink)
+ * that lie before its window.  Bias and positions count as for any token.  n_sink >= 0
+ * (SPOT_ERR_SHAPE); 0, or no window, is spot_paged_attend.
+ */
+spot_status spot_paged_attend_sinks(const void *q, int dtype, const void *k_pages,
+                                    const void *v_pages, const int32_t *page_table, int n_pages,
+                                    int page_size, int max_pages, const int32_t *seq_start,
+                                    const int32_t *seq_len, int n_seq, int rows, int h_q, int h_kv,
+                                    int d, float sm_scale, float softcap, const float *slopes,
+                                    int window, int n_sink, const int32_t *prefix,
+                                    const int32_t *first, void *out, float *lse, void *ws,
+                                    size_t ws_bytes, void *stream);
+
+/*
+ * spot_paged_attend8 -- spot_paged_attend_sinks over an 8-bit cache (see
+ * spot_rotary_append8; Section 3 for dense attention, Section 5.3 for a quantized cache):
+ * attention over the elements code * 2^(scale - 127), with the same
+ * arguments, workspace, numerics and errors, and
+ *
+ *  k_pages, v_pages   device uint8 [n_pages, h_kv, page_size, d], 16-byte aligned
+ *  k_scale, v_scale   device uint8 [n_pages, h_kv, page_size / 16]
+ * dtype is that of q and out.
+ */
+spot_status spot_paged_attend8(const void *q, int dtype, const void *k_pages, const void *v_pages,
+                               const uint8_t *k_scale, const uint8_t *v_scale,
+                               const int32_t *page_table, int n_pages, int page_size, int max_pages,
+                               const int32_t *seq_start, const int32_t *seq_len, int n_seq, int rows,
+                               int h_q, int h_kv, int d, float sm_scale, float softcap,
+                               const float *slopes, int window, int n_sink, const int32_t *prefix,
+                               const int32_t *first, void *out, float *lse, void *ws,
+                               size_t ws_bytes, void *stream);
 
 /*
  * spot_paged_weights -- the attention weight that each cached token receives, summed

@@ -79,6 +79,43 @@ bool launch_many(int n_seq, int rows, int G, int64_t cap) {
   return (int64_t)rows * G > (n_seq == 1 ? few_rows(n_seq, cap) : 16 * (int64_t)n_seq);
 }
 
+// The launches of an attention over 16-bit pages, or 8-bit ones (a.k8).
+spot_status attend(AttendArgs a, int dtype, int d, void* ws, size_t ws_bytes, hipStream_t s) {
+  const int G = a.h_q / a.h_kv;
+  const int64_t cap = (int64_t)a.pages.max_pages * a.pages.page_size;
+  const bool many = launch_many(a.n_seq, a.rows, G, cap), few = a.n_seq > 1 || !many;
+  if (!ws || ws_bytes < (many ? attend_many_workspace(d) : attend_few_workspace(d)) ||
+      !aligned(ws, 16))
+    return SPOT_ERR_WORKSPACE;
+  hipError_t e = hipSuccess;
+  if (many) {
+    a.from = few ? kFewRows : 0;
+    a.to = 0x7fffffff;
+    e = a.k8 ? launch_attend_many8(a, dtype, d, ws, s) : launch_attend_many(a, dtype, d, ws, s);
+  }
+  if (few && e == hipSuccess) {
+    a.from = 0;
+    a.to = many ? kFewRows : 0x7fffffff;
+    e = a.k8 ? launch_attend_few8(a, dtype, d, ws, s) : launch_attend_few(a, dtype, d, ws, s);
+  }
+  return from_hip(e);
+}
+
+// Axes of the pairs: none (one position a row), or of n_axes.
+spot_status check_axes(int n_axes, const uint8_t* axis, const int32_t* pos, int rows, int rope_dim) {
+  if (n_axes < 0 || n_axes > SPOT_ROPE_AXES) return SPOT_ERR_UNSUPPORTED;
+  if (n_axes > 0) {
+    if ((rope_dim > 0 && !axis) || (rows > 0 && !pos)) return SPOT_ERR_NULL;
+    for (int i = 0; i < rope_dim / 2; ++i)
+      if (axis[i] >= n_axes) return SPOT_ERR_UNSUPPORTED;
+  }
+  return SPOT_OK;
+}
+void set_axes(RotaryArgs& a, int n_axes, const uint8_t* axis) {
+  a.n_axes = n_axes;
+  if (n_axes > 0) std::copy(axis, axis + a.rope_dim / 2, a.axis);
+}
+
 const uint16_t* in16(const void* p) { return static_cast<const uint16_t*>(p); }
 uint16_t* out16(void* p) { return static_cast<uint16_t*>(p); }
 
@@ -120,10 +157,20 @@ spot_status spot_rope_frequencies(int rope_dim, double rope_base, int scaling, d
 spot_status spot_rotary(const void* x, int64_t x_stride, const int32_t* pos, int rows, int heads,
                         int d, int rope_dim, const double* freq, float amp, int flags, int dtype,
                         void* out, int64_t out_stride, void* stream) {
+  return spot_rotary_axes(x, x_stride, pos, 0, nullptr, rows, heads, d, rope_dim, freq, amp, flags,
+                          dtype, out, out_stride, stream);
+}
+
+spot_status spot_rotary_axes(const void* x, int64_t x_stride, const int32_t* pos, int n_axes,
+                             const uint8_t* axis, int rows, int heads, int d, int rope_dim,
+                             const double* freq, float amp, int flags, int dtype, void* out,
+                             int64_t out_stride, void* stream) {
   if ((!freq && rope_dim > 0) || (rows > 0 && (!x || !pos || !out))) return SPOT_ERR_NULL;
   if (rows < 0 || heads < 1) return SPOT_ERR_SHAPE;
   const spot_status st = check_rope(d, rope_dim, freq, amp, flags, dtype);
   if (st != SPOT_OK) return st;
+  const spot_status ax = check_axes(n_axes, axis, pos, rows, rope_dim);
+  if (ax != SPOT_OK) return ax;
   const int64_t row = (int64_t)heads * d;
   if (row > 1 << 24 || x_stride < row || out_stride < row || !aligned(x, 2) || !aligned(out, 2))
     return SPOT_ERR_SHAPE;
@@ -143,6 +190,7 @@ spot_status spot_rotary(const void* x, int64_t x_stride, const int32_t* pos, int
   a.amp = amp;
   a.inverse = flags & SPOT_ROPE_INVERSE;
   for (int i = 0; i < rope_dim / 2; ++i) a.freq.f[i] = freq[i];
+  set_axes(a, n_axes, axis);
   return from_hip(launch_rotary(a, dtype, flags & SPOT_ROPE_INTERLEAVED,
                                 static_cast<hipStream_t>(stream)));
 }
@@ -199,6 +247,68 @@ spot_status spot_rotary_append(const void* q, int64_t q_stride, const void* k, i
                                 static_cast<hipStream_t>(stream)));
 }
 
+spot_status spot_rotary_append8(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                const void* v, int64_t v_stride, int dtype, const int32_t* pos,
+                                int n_axes, const uint8_t* axis, const int32_t* page_table,
+                                int n_pages, int page_size, int max_pages,
+                                const int32_t* seq_start, const int32_t* seq_len, int n_seq,
+                                int rows, int h_q, int h_kv, int d, int rope_dim,
+                                const double* freq, float amp, int flags, void* q_out,
+                                void* k_pages, void* v_pages, uint8_t* k_scale, uint8_t* v_scale,
+                                void* stream) {
+  if ((!freq && rope_dim > 0) ||
+      (rows > 0 && n_seq > 0 &&
+       (!q || !k || !v || !seq_start || !seq_len || !q_out ||
+        missing_pages(k_pages && v_pages && k_scale && v_scale, n_pages, page_table, max_pages))))
+    return SPOT_ERR_NULL;
+  if (n_seq < 0 || rows < 0 || h_q < 1 || !valid_pages(n_pages, page_size, max_pages, h_kv) ||
+      (int64_t)rows * h_q > 0x7fffffff)
+    return SPOT_ERR_SHAPE;
+  const spot_status st = check_rope(d, rope_dim, freq, amp, flags, dtype);
+  if (st != SPOT_OK) return st;
+  const spot_status ax = check_axes(n_axes, axis, pos, n_seq > 0 ? rows : 0, rope_dim);
+  if (ax != SPOT_OK) return ax;
+  if (d != 64 && d != 128) return SPOT_ERR_UNSUPPORTED;
+  if ((int64_t)h_q * d > 1 << 24 || (int64_t)h_kv * d > 1 << 24 || q_stride < (int64_t)h_q * d ||
+      k_stride < (int64_t)h_kv * d || v_stride < (int64_t)h_kv * d)
+    return SPOT_ERR_SHAPE;
+  if (rows > 0 && q_out == q && q_stride != (int64_t)h_q * d) return SPOT_ERR_SHAPE;
+  for (const void* p : {q, k, v, (const void*)q_out})
+    if (!aligned(p, 2)) return SPOT_ERR_SHAPE;
+  if (!aligned(k_pages, 16) || !aligned(v_pages, 16)) return SPOT_ERR_SHAPE;
+  if (rows == 0 || n_seq == 0) return SPOT_OK;
+  Append8Args args = {};
+  RotaryArgs& a = args.r;
+  a.q = in16(q);
+  a.k = in16(k);
+  a.v = in16(v);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.out_stride = (int64_t)h_q * d;
+  a.pos = pos;
+  a.q_out = out16(q_out);
+  args.k8 = static_cast<uint8_t*>(k_pages);
+  args.v8 = static_cast<uint8_t*>(v_pages);
+  args.k_scale = k_scale;
+  args.v_scale = v_scale;
+  a.pages = Pages{page_table, n_pages, page_size, max_pages};
+  a.seq_start = seq_start;
+  a.seq_len = seq_len;
+  a.n_seq = n_seq;
+  a.rows = rows;
+  a.h_q = h_q;
+  a.h_kv = h_kv;
+  a.d = d;
+  a.rope_dim = rope_dim;
+  a.amp = amp;
+  a.inverse = flags & SPOT_ROPE_INVERSE;
+  for (int i = 0; i < rope_dim / 2; ++i) a.freq.f[i] = freq[i];
+  set_axes(a, n_axes, axis);
+  return from_hip(launch_append8(args, dtype, flags & SPOT_ROPE_INTERLEAVED,
+                                 static_cast<hipStream_t>(stream)));
+}
+
 size_t spot_paged_workspace_bytes(int n_seq, int rows, int h_q, int h_kv, int d) {
   if (n_seq < 1 || rows < 1 || h_q < 1 || h_kv < 1 || d < 1) return 0;
   // Enough for every call of at most these sequences and rows: of as many rows the fewest
@@ -209,13 +319,14 @@ size_t spot_paged_workspace_bytes(int n_seq, int rows, int h_q, int h_kv, int d)
   return many ? attend_many_workspace(d) : attend_few_workspace(d);
 }
 
-spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, const void* v_pages,
-                              const int32_t* page_table, int n_pages, int page_size, int max_pages,
-                              const int32_t* seq_start, const int32_t* seq_len, int n_seq, int rows,
-                              int h_q, int h_kv, int d, float sm_scale, float softcap,
-                              const float* slopes, int window, const int32_t* prefix,
-                              const int32_t* first, void* out, float* lse, void* ws,
-                              size_t ws_bytes, void* stream) {
+spot_status spot_paged_attend_sinks(const void* q, int dtype, const void* k_pages,
+                                    const void* v_pages, const int32_t* page_table, int n_pages,
+                                    int page_size, int max_pages, const int32_t* seq_start,
+                                    const int32_t* seq_len, int n_seq, int rows, int h_q, int h_kv,
+                                    int d, float sm_scale, float softcap, const float* slopes,
+                                    int window, int n_sink, const int32_t* prefix,
+                                    const int32_t* first, void* out, float* lse, void* ws,
+                                    size_t ws_bytes, void* stream) {
   if (rows > 0 && n_seq > 0 &&
       (!q || !seq_start || !seq_len || !out ||
        missing_pages(k_pages && v_pages, n_pages, page_table, max_pages)))
@@ -223,15 +334,10 @@ spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, con
   const spot_status st = check_attend(dtype, n_pages, page_size, max_pages, n_seq, rows, h_q, h_kv,
                                       d, sm_scale, softcap, window);
   if (st != SPOT_OK) return st;
+  if (n_sink < 0) return SPOT_ERR_SHAPE;
   if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16))
     return SPOT_ERR_SHAPE;
   if (rows == 0 || n_seq == 0) return SPOT_OK;
-  const int G = h_q / h_kv;
-  const int64_t cap = (int64_t)max_pages * page_size;
-  const bool many = launch_many(n_seq, rows, G, cap), few = n_seq > 1 || !many;
-  if (!ws || ws_bytes < (many ? attend_many_workspace(d) : attend_few_workspace(d)) ||
-      !aligned(ws, 16))
-    return SPOT_ERR_WORKSPACE;
   AttendArgs a = {};
   a.q = in16(q);
   a.k = in16(k_pages);
@@ -243,22 +349,61 @@ spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, con
   a.rows = rows;
   a.h_q = h_q;
   a.h_kv = h_kv;
-  a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first};
+  a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first, n_sink};
   a.out = out16(out);
   a.lse = lse;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  hipError_t e = hipSuccess;
-  if (many) {
-    a.from = few ? kFewRows : 0;
-    a.to = 0x7fffffff;
-    e = launch_attend_many(a, dtype, d, ws, s);
-  }
-  if (few && e == hipSuccess) {
-    a.from = 0;
-    a.to = many ? kFewRows : 0x7fffffff;
-    e = launch_attend_few(a, dtype, d, ws, s);
-  }
-  return from_hip(e);
+  return attend(a, dtype, d, ws, ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, const void* v_pages,
+                              const int32_t* page_table, int n_pages, int page_size, int max_pages,
+                              const int32_t* seq_start, const int32_t* seq_len, int n_seq, int rows,
+                              int h_q, int h_kv, int d, float sm_scale, float softcap,
+                              const float* slopes, int window, const int32_t* prefix,
+                              const int32_t* first, void* out, float* lse, void* ws,
+                              size_t ws_bytes, void* stream) {
+  return spot_paged_attend_sinks(q, dtype, k_pages, v_pages, page_table, n_pages, page_size,
+                                 max_pages, seq_start, seq_len, n_seq, rows, h_q, h_kv, d, sm_scale,
+                                 softcap, slopes, window, 0, prefix, first, out, lse, ws, ws_bytes,
+                                 stream);
+}
+
+spot_status spot_paged_attend8(const void* q, int dtype, const void* k_pages, const void* v_pages,
+                               const uint8_t* k_scale, const uint8_t* v_scale,
+                               const int32_t* page_table, int n_pages, int page_size, int max_pages,
+                               const int32_t* seq_start, const int32_t* seq_len, int n_seq, int rows,
+                               int h_q, int h_kv, int d, float sm_scale, float softcap,
+                               const float* slopes, int window, int n_sink, const int32_t* prefix,
+                               const int32_t* first, void* out, float* lse, void* ws,
+                               size_t ws_bytes, void* stream) {
+  if (rows > 0 && n_seq > 0 &&
+      (!q || !seq_start || !seq_len || !out ||
+       missing_pages(k_pages && v_pages && k_scale && v_scale, n_pages, page_table, max_pages)))
+    return SPOT_ERR_NULL;
+  const spot_status st = check_attend(dtype, n_pages, page_size, max_pages, n_seq, rows, h_q, h_kv,
+                                      d, sm_scale, softcap, window);
+  if (st != SPOT_OK) return st;
+  if (n_sink < 0) return SPOT_ERR_SHAPE;
+  if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16))
+    return SPOT_ERR_SHAPE;
+  if (rows == 0 || n_seq == 0) return SPOT_OK;
+  AttendArgs a = {};
+  a.q = in16(q);
+  a.k8 = static_cast<const uint8_t*>(k_pages);
+  a.v8 = static_cast<const uint8_t*>(v_pages);
+  a.k_scale = k_scale;
+  a.v_scale = v_scale;
+  a.pages = Pages{page_table, n_pages, page_size, max_pages};
+  a.seq_start = seq_start;
+  a.seq_len = seq_len;
+  a.n_seq = n_seq;
+  a.rows = rows;
+  a.h_q = h_q;
+  a.h_kv = h_kv;
+  a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first, n_sink};
+  a.out = out16(out);
+  a.lse = lse;
+  return attend(a, dtype, d, ws, ws_bytes, static_cast<hipStream_t>(stream));
 }
 
 spot_status spot_paged_weights(const void* q, const float* lse, int dtype, const void* k_pages,
@@ -289,7 +434,7 @@ spot_status spot_paged_weights(const void* q, const float* lse, int dtype, const
   a.rows = rows;
   a.h_q = h_q;
   a.h_kv = h_kv;
-  a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first};
+  a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first, 0};
   a.acc = acc;
   a.decay = decay;
   a.acc_out = acc_out;

@@ -1,0 +1,312 @@
+// Rotary positions and the append of keys and values to an 8-bit paged cache (gfx950).
+//
+// Keys (rotated) and values become e4m3 codes with one power of two for every 16 tokens of
+// a head: the smallest for which no value of theirs exceeds the largest code, 448.  A
+// rotated pair (a, b) counts as amp (|a| + |b|), which bounds both of its values at any
+// angle: the scale follows from the inputs alone, whatever the rounding of sines.  (At
+// most a factor of 2 sqrt 2 above what the values need, of 2^15 that the codes span at full
+// precision.)  New tokens that join earlier ones of their 16 keep the scale or raise it;
+// then the earlier codes are rounded again, which costs those of the smallest values bits
+// and leaves the others as they were, the factor being a power of two.
+//
+// The queries' rows are rotated as by rotary_kernel, a workgroup each; four heads' keys, or
+// values, of 16 tokens are another workgroup, one head a wave.  Every element is read and
+// written once and memory bounds it; sines of a token are made once for its queries and
+// once for every four KV heads.
+#include <algorithm>
+
+#include "cache8.h"
+#include "rotary_core.h"
+
+namespace spot {
+namespace paged {
+namespace {
+
+using namespace rot;
+
+constexpr int kHeads = 4;             // of a workgroup: one a wave
+constexpr int kLeast = 27;            // least scale, 2^-100: its products are BF16 numbers
+constexpr float kTop = 448.f;         // the largest code
+
+// The largest e4m3 number times a power of two that the element type has: values beyond
+// it are held back to it.
+template <class T>
+constexpr float kLargest = 61440.f;                               // FP16
+template <>
+constexpr float kLargest<Bf16> = 240.f * 1.329227995784916e36f;   // 2^120
+
+// 16 tokens that new ones belong to.
+struct Group {
+  int s;                  // sequence (-1: no work)
+  int t0;                 // first token
+  int from, to;           // new tokens of the 16: [from, to)
+  int row;                // row of the first of them
+};
+// Number `unit` of all sequences' groups, found by one wave.
+__device__ __forceinline__ Group find_group(const RotaryArgs& a, int unit) {
+  const int lane = __lane_id();
+  Group r = {-1, 0, 0, 0, 0};
+  int at = 0;
+  for (int base = 0; base < a.n_seq; base += 64) {
+    Seq q = {0, 0, 0};
+    if (base + lane < a.n_seq) q = sequence(a.seq_start, a.seq_len, base + lane, a.rows);
+    // tokens at negative places are not there
+    const int first = max(q.len - q.n, 0), n = q.n > 0 && q.len > first
+                                                   ? (q.len - 1) / kGroupKeys - first / kGroupKeys + 1
+                                                   : 0;
+    const int incl = wave_incl_scan_i(n);
+    const uint64_t hit = __ballot(unit >= at + incl - n && unit < at + incl);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      const int in = unit - at - __builtin_amdgcn_readlane(incl - n, l);
+      const int f = __builtin_amdgcn_readlane(first, l), len = __builtin_amdgcn_readlane(q.len, l);
+      const int start = __builtin_amdgcn_readlane(q.start, l);
+      const int p0 = len - __builtin_amdgcn_readlane(q.n, l);
+      r.s = base + l;
+      r.t0 = (f / kGroupKeys + in) * kGroupKeys;
+      r.from = max(f - r.t0, 0);
+      r.to = min(len - r.t0, kGroupKeys);
+      r.row = start + (r.t0 + r.from - p0);
+      return r;
+    }
+    at += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return r;
+}
+
+// The byte of the smallest power of two n with x <= 448 n.
+__device__ __forceinline__ int scale_byte(float x) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, x);
+  // 448 = 1.75 x 2^8
+  const int e = (int)(b >> 23) - 8 + ((b & 0x7fffffu) > 0x600000u);
+  return max(e, kLeast);
+}
+__device__ __forceinline__ float power(int e) {          // 2^e, at least 2^-126
+  return __builtin_bit_cast(float, (uint32_t)(max(e, -126) + 127) << 23);
+}
+
+// x / 2^(byte - 127) within the codes (NaN stays).
+template <class T>
+__device__ __forceinline__ float fit(float x, float inv) {
+  constexpr float L = kLargest<T>;
+  x = x > L ? L : x;
+  x = x < -L ? -L : x;
+  x *= inv;
+  x = x > kTop ? kTop : x;
+  return x < -kTop ? -kTop : x;
+}
+__device__ __forceinline__ uint32_t code4(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+}
+
+// A head's 16 tokens, keys (K) or values; lane l: token l / 4, pairs of elements.
+// VEC: pairs of 16-byte chunks, l % 4 and 4 further on; otherwise every fourth pair.
+template <class T, int D, bool VEC, bool IL, bool K>
+__device__ __forceinline__ void store_head(const Append8Args& args, const Group& gr, int krow, int h,
+                                           const float* s_cos, const float* s_sin, int pitch) {
+  const RotaryArgs& a = args.r;
+  constexpr int NP = D / 8;                  // pairs of a lane
+  const int lane = threadIdx.x & 63, tk = lane >> 2, part = lane & 3;
+  const int half = K ? a.rope_dim / 2 : 0;
+  const bool now = tk >= gr.from && tk < gr.to;
+  const int64_t row = gr.row + (now ? tk - gr.from : 0);
+  const uint16_t* const in = (K ? a.k + row * a.k_stride : a.v + row * a.v_stride) + h * D;
+  const int64_t slots = (int64_t)krow + (int64_t)h * a.pages.page_size;   // of the 16 tokens
+  uint8_t* const pool = K ? args.k8 : args.v8;
+  uint8_t* const scales = K ? args.k_scale : args.v_scale;
+  uint8_t* const out = pool + (slots + tk) * D;
+
+  float xa[NP], xb[NP];
+  float turned = 0.f, plain = 0.f;           // largest magnitudes of finite values
+  auto count = [&](float a, float b, bool rot) {
+    if (rot) {
+      const float x = fabsf(a) + fabsf(b);
+      turned = x < INFINITY ? fmaxf(turned, x) : turned;
+    } else {
+      plain = fabsf(a) < INFINITY ? fmaxf(plain, fabsf(a)) : plain;
+      plain = fabsf(b) < INFINITY ? fmaxf(plain, fabsf(b)) : plain;
+    }
+  };
+  if (now) {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int m = 0; m < NP / 8; ++m) {
+        const int u = part + 4 * m;
+        const bool hf = !IL && u < half / 8, rot = IL ? 16 * u < 2 * half : hf;
+        const int ca = hf ? 8 * u : 16 * u, cb = hf ? half + 8 * u : 16 * u + 8;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(in + ca);
+        const u32x4 y = *reinterpret_cast<const u32x4*>(in + cb);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float nx = T::lo(e < 4 ? x[e] : y[e - 4]), ny = T::hi(e < 4 ? x[e] : y[e - 4]);
+          const float fx = e & 1 ? T::hi(x[e / 2]) : T::lo(x[e / 2]);
+          const float fy = e & 1 ? T::hi(y[e / 2]) : T::lo(y[e / 2]);
+          xa[8 * m + e] = hf ? fx : nx;
+          xb[8 * m + e] = hf ? fy : ny;
+          count(xa[8 * m + e], xb[8 * m + e], rot);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < NP; ++m) {
+        const int i = part + 4 * m;
+        const bool rot = i < half;
+        const int ia = rot && !IL ? i : 2 * i, ib = rot && !IL ? i + half : 2 * i + 1;
+        xa[m] = T::one(in[ia]);
+        xb[m] = T::one(in[ib]);
+        count(xa[m], xb[m], rot);
+      }
+    }
+  }
+  const float top = wave_max(fmaxf(turned * fabsf(a.amp), plain));
+  const int64_t at = slots / kGroupKeys;
+  int byte = scale_byte(top < INFINITY ? top : 3.4028235e38f);
+  if (gr.from > 0) {
+    const int old = scales[at];
+    if (byte > old) {          // the earlier tokens' codes once more
+      if (tk < gr.from) {
+        const float down = power(old - byte);
+        uint32_t* const c = reinterpret_cast<uint32_t*>(out) + part * (D / 16);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(c[i], false);
+          const f32x2 y = __builtin_amdgcn_cvt_pk_f32_fp8(c[i], true);
+          c[i] = code4(x[0] * down, x[1] * down, y[0] * down, y[1] * down);
+        }
+      }
+    } else {
+      byte = old;
+    }
+  }
+  if (lane == 0) scales[at] = (uint8_t)byte;
+  if (!now) return;
+  const float inv = power(127 - byte);
+  auto turn_at = [&](int m, int p) {
+    const f32x2 t = turn(xa[m], xb[m], s_cos[tk * pitch + p], s_sin[tk * pitch + p]);
+    xa[m] = t[0];
+    xb[m] = t[1];
+  };
+  if constexpr (VEC) {
+#pragma unroll
+    for (int m = 0; m < NP / 8; ++m) {
+      const int u = part + 4 * m;
+      const bool hf = !IL && u < half / 8, rot = IL ? 16 * u < 2 * half : hf;
+      const int ca = hf ? 8 * u : 16 * u, cb = hf ? half + 8 * u : 16 * u + 8;
+      if (K && rot) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) turn_at(8 * m + e, 8 * u + e);
+      }
+      float x[8], y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float a0 = fit<T>(xa[8 * m + e], inv), b0 = fit<T>(xb[8 * m + e], inv);
+        xa[8 * m + e] = a0;
+        xb[8 * m + e] = b0;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float* A = xa + 8 * m;
+        const float* B = xb + 8 * m;
+        x[2 * e] = hf ? A[2 * e] : A[e];
+        x[2 * e + 1] = hf ? A[2 * e + 1] : B[e];
+        y[2 * e] = hf ? B[2 * e] : A[4 + e];
+        y[2 * e + 1] = hf ? B[2 * e + 1] : B[4 + e];
+      }
+      *reinterpret_cast<u32x2*>(out + ca) = u32x2{code4(x[0], x[1], x[2], x[3]),
+                                                  code4(x[4], x[5], x[6], x[7])};
+      *reinterpret_cast<u32x2*>(out + cb) = u32x2{code4(y[0], y[1], y[2], y[3]),
+                                                  code4(y[4], y[5], y[6], y[7])};
+    }
+  } else {
+#pragma unroll
+    for (int m = 0; m < NP; ++m) {
+      const int i = part + 4 * m;
+      const bool rot = i < half;
+      const int ia = rot && !IL ? i : 2 * i, ib = rot && !IL ? i + half : 2 * i + 1;
+      if (K && rot) turn_at(m, i);
+      const uint32_t c = code4(fit<T>(xa[m], inv), fit<T>(xb[m], inv), 0.f, 0.f);
+      out[ia] = (uint8_t)c;
+      out[ib] = (uint8_t)(c >> 8);
+    }
+  }
+}
+
+// Workgroups: `units` groups x ceil(h_kv / 4) x (keys, values), then the queries' rows.
+template <class T, int D, bool VEC, bool IL, bool AXES>
+__global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args args, int units) {
+  const RotaryArgs& a = args.r;
+  const int chunks = (a.h_kv + kHeads - 1) / kHeads;
+  const int64_t first = (int64_t)units * chunks * 2;
+  if (blockIdx.x >= first) {
+    rotate_row<T, VEC, IL, AXES, true>(a, (int)(blockIdx.x - first));
+    return;
+  }
+  constexpr int kPitch = D / 2 + 1;          // rows of sines in other banks
+  __shared__ float s_cos[kGroupKeys * kPitch], s_sin[kGroupKeys * kPitch];
+  const int tid = threadIdx.x, wave = tid >> 6;
+  const bool keys = blockIdx.x % 2 == 0;
+  const int chunk = blockIdx.x / 2 % chunks;
+  const Group gr = find_group(a, blockIdx.x / 2 / chunks);
+  if (gr.s < 0 || gr.t0 >= a.pages.cap()) return;
+  const int krow = a.pages.row(gr.s, gr.t0, 0, a.h_kv);
+  if (krow < 0) return;
+  const int h = chunk * kHeads + wave;
+  if (keys) {
+    const int half = a.rope_dim / 2;
+    for (int i = tid; i < (gr.to - gr.from) * half; i += kThreads) {
+      const int tk = gr.from + i / half, p = i % half;
+      const int row = gr.row + tk - gr.from;
+      const int pos = AXES    ? a.pos[(int64_t)row * a.n_axes + a.axis[p]]
+                      : a.pos ? a.pos[row]
+                              : gr.t0 + tk;
+      float sn, cs;
+      rope_sincos(pos, a.freq.f[p], sn, cs);
+      s_cos[tk * kPitch + p] = cs * a.amp;
+      s_sin[tk * kPitch + p] = a.inverse ? -sn * a.amp : sn * a.amp;
+    }
+    __syncthreads();
+    if (h < a.h_kv) store_head<T, D, VEC, IL, true>(args, gr, krow, h, s_cos, s_sin, kPitch);
+  } else {
+    if (h < a.h_kv) store_head<T, D, VEC, IL, false>(args, gr, krow, h, s_cos, s_sin, kPitch);
+  }
+}
+
+template <class T, int D, bool AXES>
+void launch(const Append8Args& a, int units, dim3 grid, bool vec, bool il, hipStream_t s) {
+  auto f = vec ? (il ? append8_kernel<T, D, true, true, AXES>
+                     : append8_kernel<T, D, true, false, AXES>)
+               : (il ? append8_kernel<T, D, false, true, AXES>
+                     : append8_kernel<T, D, false, false, AXES>);
+  hipLaunchKernelGGL(f, grid, dim3(kThreads), 0, s, a, units);
+}
+
+}  // namespace
+
+hipError_t launch_append8(const Append8Args& args, int dtype, bool interleaved, hipStream_t s) {
+  const RotaryArgs& a = args.r;
+  // groups that new tokens of ascending starts can belong to
+  const int64_t units = std::min((int64_t)a.rows, (int64_t)a.rows / kGroupKeys + 2 * (int64_t)a.n_seq);
+  const int64_t groups = units * ((a.h_kv + kHeads - 1) / kHeads) * 2 + a.rows;
+  if (!launchable(groups, kThreads)) return hipErrorInvalidConfiguration;
+  auto whole = [](const void* p, int64_t stride) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0;
+  };
+  const bool vec = a.rope_dim % 16 == 0 && whole(a.q, a.q_stride) && whole(a.q_out, a.out_stride) &&
+                   whole(a.k, a.k_stride) && whole(a.v, a.v_stride);
+  const dim3 grid((unsigned)groups);
+  auto go = [&](auto t) {
+    typedef decltype(t) T;
+    if (a.n_axes > 0)
+      a.d == 128 ? launch<T, 128, true>(args, (int)units, grid, vec, interleaved, s)
+                 : launch<T, 64, true>(args, (int)units, grid, vec, interleaved, s);
+    else
+      a.d == 128 ? launch<T, 128, false>(args, (int)units, grid, vec, interleaved, s)
+                 : launch<T, 64, false>(args, (int)units, grid, vec, interleaved, s);
+  };
+  dtype == SPOT_DTYPE_BF16 ? go(Bf16()) : go(Fp16());
+  return hipGetLastError();
+}
+
+}  // namespace paged
+}  // namespace spot

@@ -15,41 +15,13 @@
 // The keys' bytes bound it: each is read once for all 16 rows (decode, four sequences of
 // 131072 tokens, 8 KV heads of 128: 334 us, 6.4 TB/s).  On one short sequence the chain of
 // lengths, pages, keys and join does: 700 tokens 10.4 us, two blocks of keys a part.
-#include "decode_core.h"
-#include "paged_core.h"
+#include "attend_join.h"
 
 namespace spot {
 namespace paged {
 namespace {
 
-using dec::lanes_max_xor16;
-using dec::lanes_max_xor32;
-using dec::lanes_sum_xor16;
-using dec::lanes_sum_xor32;
-using dec::wave_lds_sync;
-
-constexpr int kRows = 16;          // rows of a tile
-constexpr int kWaves = 4;
-constexpr int kListBlocks = 512;   // blocks whose pages are looked up at once
-
-template <int D>
-struct Smem {
-  struct Merge {
-    float ml[kWaves][kRows][2];
-    alignas(16) float o[kWaves][kRows][D];
-  };
-  struct Join {
-    float weight[kMaxJoin][kRows];  // of part and row: 2^(m - M) / L
-  };
-  union {
-    alignas(16) unsigned char kv[kWaves][2 * 16 * D * 2];   // a wave's V rows, then its K rows
-    Merge merge;
-    Join join;
-  };
-  int list[kListBlocks * 4];       // pool row of each 16-key group, -1 without a page
-  Part part;
-  int last;
-};
+using namespace few;
 
 // Physical 16-byte chunk of logical chunk c of row r: K is read 16 rows x one chunk
 // at a time, V 8 bytes from each of 8 rows at two neighbouring chunks.
@@ -62,21 +34,22 @@ __device__ __forceinline__ int swz_v(int r, int c) {
   return D == 128 ? c ^ ((r & 7) << 1) : c ^ (((r >> 1) & 3) << 1);
 }
 
-template <class T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a) {
+// SINK: the rows also see the first tokens of their text, before the window.
+template <class T, int D, bool CAP, bool BIAS, bool SINK>
+__device__ __forceinline__ void attend_few(const AttendArgs& a) {
   constexpr int RB = D * 2;             // bytes of a row
   constexpr int LR = 64 * 16 / RB;      // rows of a wave's load: 4 or 8
   constexpr int NL = 16 / LR;           // loads of 16 rows
   constexpr int CH = D / 8;             // 16-byte chunks of a row
-  constexpr int PL = D / 64;
-  __shared__ Smem<D> sm;
+  __shared__ Smem<D, 2 * 16 * D * 2> sm;   // kv: a wave's V rows, then its K rows
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int r16 = lane & 15, kg = lane >> 4;
   const int G = a.h_q / a.h_kv, g = blockIdx.x % a.h_kv;
   const int cap = a.pages.cap();
   if (wave == 0) {
     const Part p = find_part<kRows, 0>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len, a.n_seq,
-                                       a.rows, G, a.h_kv, a.rule.window, cap, a.from, a.to);
+                                       a.rows, G, a.h_kv, a.rule.window, SINK ? a.rule.sink : 0,
+                                       cap, a.from, a.to);
     if (lane == 0) sm.part = p;
   }
   __syncthreads();
@@ -87,8 +60,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
   const unsigned j = pt.tile * kRows + r16, n_rows = pt.q.n * G;
   const bool real = j < n_rows;
   const int tok = real ? j / G : 0, head = g * G + (real ? j - tok * G : 0);
-  int lo = 0, hi = 0;
-  if (real) visible(a.rule, pt.q, pt.s, tok, cap, lo, hi);
+  int lo = 0, hi = 0, from = 0, end = 0;
+  if (real) {
+    if constexpr (SINK)
+      visible(a.rule, pt.q, pt.s, tok, cap, lo, hi, from, end);
+    else
+      visible(a.rule, pt.q, pt.s, tok, cap, lo, hi);
+  }
+  // (with sinks, comparisons are joined without branches: of a select behind short-circuit
+  // ones and a uniform branch the compiler, ROCm 7.2, has kept the uniform part only)
+  auto sees = [&](int t) { return ((t >= lo) & (t < hi)) | ((t >= from) & (t < end)); };
   const Scores<CAP, BIAS> sc(a.rule, pt.q, tok, head);
   u32x4 qf[D / 32];
   const size_t qrow = (size_t)(pt.q.start + tok) * a.h_q + head;
@@ -104,7 +85,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
   const int FLO = (int)wave_max_u(real ? (uint32_t)(any ? lo : 0x7fffffff) : 0u);
   const int FHI = (int)wave_min_u(real ? (uint32_t)hi : 0x7fffffffu);
 
-  const int b0 = LO < HI ? LO / 64 : 0, b1 = LO < HI ? (HI + 63) / 64 : 0;
+  int SLO = 0, SHI = 0;                 // of the sinks
+  Blocks bl = {0, 0, LO < HI ? LO / 64 : 0, 0};
+  bl.n = LO < HI ? (HI + 63) / 64 - bl.main0 : 0;
+  if constexpr (SINK) {
+    SLO = (int)wave_min_u(end > from ? (uint32_t)from : 0x7fffffffu);
+    SHI = (int)wave_max_u((uint32_t)end);
+    bl = blocks_of(LO, HI, SLO, SHI);
+  }
+  // blocks of the part by their number among those of the tile; 16-bit calls without
+  // sinks number them by their place
+  const int b0 = SINK ? 0 : bl.main0, b1 = b0 + bl.n;
+  auto block = [&](int i) { return SINK ? bl.at(i) : i; };
   const int share = (b1 - b0 + pt.n_split - 1) / pt.n_split;
   const int e0 = min(b0 + pt.split * share, b1), e1 = min(e0 + share, b1);
 
@@ -120,7 +112,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
     const int nb = min(kListBlocks, e1 - c0);
     if (c0 > e0) __syncthreads();       // the list is done with
     for (int i = tid; i < 4 * nb; i += 64 * kWaves) {
-      const int t = c0 * 64 + i * kGroupKeys;
+      const int t = SINK ? block(c0 + i / 4) * 64 + i % 4 * kGroupKeys : c0 * 64 + i * kGroupKeys;
       sm.list[i] = t < cap ? a.pages.row(pt.s, t, g, a.h_kv) : -1;
     }
     __syncthreads();
@@ -138,7 +130,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
     // not see must not meet an infinite or NaN value that another row does see (odd).
     bool odd = false;
     auto front = [&](u32x4(&kr)[NL], u32x4(&vr)[NL], int n) -> f32x4 {
-      const int t0 = (c0 + n) * 64 + wave * 16;
+      const int t0 = block(c0 + n) * 64 + wave * 16;
       odd = false;
       // Values that no row sees never meet the zero probabilities: they may be
       // infinite or NaN.
@@ -147,7 +139,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
           const int t = t0 + i * LR + lane / CH;
-          if (!page || t < LO || t >= HI) vr[i] = u32x4{0u, 0u, 0u, 0u};
+          if constexpr (SINK) {
+            const bool seen = page & (((t >= LO) & (t < HI)) | ((t >= SLO) & (t < SHI)));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vr[i][e] = seen ? vr[i][e] : 0u;
+          } else {
+            if (!page || t < LO || t >= HI) vr[i] = u32x4{0u, 0u, 0u, 0u};
+          }
         }
       }
       if (t0 < FLO || t0 + 16 > FHI) {
@@ -175,7 +173,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
       return s;
     };
     auto back = [&](int n, f32x4 s) {
-      const int t0 = (c0 + n) * 64 + wave * 16;
+      const int t0 = block(c0 + n) * 64 + wave * 16;
       f32x4 quad[1] = {s};
       sc(quad, (float)(sc.p - (t0 + 4 * kg)));
       float x[4] = {quad[0][0], quad[0][1], quad[0][2], quad[0][3]};
@@ -184,7 +182,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int t = t0 + 4 * kg + i;
-          if (!page || t < lo || t >= hi) x[i] = -INFINITY;
+          if constexpr (SINK)
+            x[i] = page & sees(t) ? x[i] : -INFINITY;
+          else if (!page || t < lo || t >= hi)
+            x[i] = -INFINITY;
         }
       }
       float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) - T::kShift;
@@ -223,7 +224,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
         for (int k = 0; k < 16; ++k) {
           const float pk = __shfl(k & 2 ? (k & 1 ? p[3] : p[2]) : (k & 1 ? p[1] : p[0]),
                                   (k >> 2) * 16 + r16);
-          const bool sees = t0 + k >= lo && t0 + k < hi;
+          const bool seen = SINK ? sees(t0 + k) : t0 + k >= lo && t0 + k < hi;
           const unsigned char* row = vs + k * RB + (kg & 1) * 8;
 #pragma unroll
           for (int dt = 0; dt < D / 16; ++dt) {
@@ -232,7 +233,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const uint32_t h = i & 1 ? y[i >> 1] >> 16 : y[i >> 1] & 0xffffu;
-              if (sees && (~h & T::kExponent) == 0u)
+              if (seen && (~h & T::kExponent) == 0u)
                 o[dt][i] = fmaf(pk, T::one((uint16_t)h), o[dt][i]);
             }
           }
@@ -279,137 +280,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a
     }
   }
 
-  settle(o);
-  // the four waves' states, then one row per wave and turn
-  const float l_row = lanes_sum_xor32(lanes_sum_xor16(l_lane));
-  __syncthreads();
-  if (kg == 0) {
-    sm.merge.ml[wave][r16][0] = m_run;
-    sm.merge.ml[wave][r16][1] = l_row;
-  }
-#pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt)
-    *reinterpret_cast<f32x4*>(&sm.merge.o[wave][r16][16 * dt + 4 * kg]) = o[dt];
-  __syncthreads();
-  const int n_real = min((unsigned)kRows, n_rows - pt.tile * kRows);
-  auto row_of = [&](int c) __attribute__((always_inline)) {   // row of the tile in out
-    const unsigned jc = pt.tile * kRows + c, tc = jc / (unsigned)G;
-    return (size_t)(pt.q.start + tc) * a.h_q + g * G + (jc - tc * G);
-  };
-  const size_t slot0 = ((size_t)pt.slot * a.h_kv + (size_t)g * pt.n_split);
-  float* const wml = a.ws.ml + (slot0 + pt.split) * kRows * 2;
-  float* const wo = a.ws.o + (slot0 + pt.split) * kRows * D;
-  for (int c = wave; c < n_real; c += kWaves) {
-    float M = -INFINITY, L = 0.f, acc[PL] = {};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-      if (sm.merge.ml[w][c][1] != 0.f) M = fmaxf(M, sm.merge.ml[w][c][0]);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float lw = sm.merge.ml[w][c][1];
-      if (lw != 0.f) {
-        const float wt = __builtin_amdgcn_exp2f(sm.merge.ml[w][c][0] - M);
-        L = fmaf(lw, wt, L);
-#pragma unroll
-        for (int e = 0; e < PL; ++e) acc[e] = fmaf(sm.merge.o[w][c][PL * lane + e], wt, acc[e]);
-      }
-    }
-    if (pt.n_split > 1) {
-      if constexpr (PL == 2)
-        dec::store_coherent(wo + c * D + 2 * lane, make_float2(acc[0], acc[1]));
-      else
-        __hip_atomic_store(wo + c * D + lane, acc[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (lane == 0) dec::store_coherent(wml + c * 2, make_float2(M, L));
-    } else {
-      const size_t row = row_of(c);
-      const float inv = L == 0.f ? 0.f : 1.f / L;
-      if constexpr (PL == 2)
-        reinterpret_cast<uint32_t*>(a.out + row * D)[lane] = T::pack2(acc[0] * inv, acc[1] * inv);
-      else
-        a.out[row * D + lane] = T::round(acc[0] * inv);
-      if (a.lse && lane == 0)
-        a.lse[row] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
-    }
-  }
-  if (pt.n_split == 1) return;
+  finish<T, D>(sm, a, pt, g, G, n_rows, m_run, l_lane, o);
+}
 
-  dec::wait_stores();
-  __syncthreads();
-  unsigned* const counter = a.ws.counters + (size_t)pt.counter * a.h_kv + g;
-  if (tid == 0)
-    sm.last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-              (unsigned)(pt.n_split - 1);
-  __syncthreads();
-  if (!sm.last) return;
-  // Row c of 16 threads: each has the (m, l) of every 16th part, then D / 16 dims.  The
-  // first parts' O is on its way while the weights are made.
-  constexpr int E = D / 32, U = 4;           // float pairs of a thread; parts in flight
-  const int c = min(tid >> 4, n_real - 1), k = tid & 15, n = pt.n_split;
-  const float* const ml = a.ws.ml + (slot0 * kRows + c) * 2;
-  const float* const po = a.ws.o + (slot0 * kRows + c) * D + k * 2 * E;
-  float2 v[U][E];
-  auto load = [&](int u0) __attribute__((always_inline)) {
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        v[u][e] = dec::load_coherent(po + (size_t)min(u0 + u, n - 1) * kRows * D + 2 * e);
-  };
-  load(0);
-  constexpr int P = kMaxJoin / 16;
-  float2 t[P];
-  float M = -INFINITY, L = 0.f;
-#pragma unroll
-  for (int i = 0; i < P; ++i) {
-    t[i] = make_float2(-INFINITY, 0.f);
-    if (k + 16 * i < n) t[i] = dec::load_coherent(ml + (size_t)(k + 16 * i) * kRows * 2);
-  }
-#pragma unroll
-  for (int i = 0; i < P; ++i)
-    if (t[i].y != 0.f) M = fmaxf(M, t[i].x);
-  M = fmaxf(M, dpp_f<kDppQuadXor1>(M));
-  M = fmaxf(M, dpp_f<kDppQuadXor2>(M));
-  M = fmaxf(M, dpp_f<kDppHalfMirror>(M));
-  M = fmaxf(M, dpp_f<kDppMirror>(M));
-  float wt[P];
-#pragma unroll
-  for (int i = 0; i < P; ++i) {
-    wt[i] = t[i].y != 0.f ? __builtin_amdgcn_exp2f(t[i].x - M) : 0.f;
-    if (t[i].y != 0.f) L = fmaf(t[i].y, wt[i], L);
-  }
-  L += dpp_f<kDppQuadXor1>(L);
-  L += dpp_f<kDppQuadXor2>(L);
-  L += dpp_f<kDppHalfMirror>(L);
-  L += dpp_f<kDppMirror>(L);
-  const float inv = L == 0.f ? 0.f : 1.f / L;
-#pragma unroll
-  for (int i = 0; i < P; ++i)
-    if (k + 16 * i < n) sm.join.weight[k + 16 * i][tid >> 4] = wt[i] * inv;
-  wave_lds_sync();               // a row's threads lie in one wave
-  float2 acc[E] = {};
-  for (int u0 = 0; u0 < n; u0 += U) {
-    if (u0) load(u0);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (u0 + u >= n) continue;
-      const float w = sm.join.weight[u0 + u][tid >> 4];
-      if (w == 0.f) continue;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        acc[e].x = fmaf(v[u][e].x, w, acc[e].x);
-        acc[e].y = fmaf(v[u][e].y, w, acc[e].y);
-      }
-    }
-  }
-  if (tid >> 4 < n_real) {
-    const size_t row = row_of(c);
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      reinterpret_cast<uint32_t*>(a.out + row * D)[k * E + e] = T::pack2(acc[e].x, acc[e].y);
-    if (a.lse && k == 0)
-      a.lse[row] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
-  }
-  if (tid == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+template <class T, int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(64 * kWaves, 2) void attend_few_kernel(AttendArgs a) {
+  attend_few<T, D, CAP, BIAS, false>(a);
+}
+template <class T, int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(64 * kWaves, 2) void sinks_few_kernel(AttendArgs a) {
+  attend_few<T, D, CAP, BIAS, true>(a);
 }
 
 template <class T, int D>
@@ -418,7 +298,10 @@ void launch(const AttendArgs& a, dim3 grid, hipStream_t s) {
   auto f = cap ? (bias ? attend_few_kernel<T, D, true, true> : attend_few_kernel<T, D, true, false>)
                : (bias ? attend_few_kernel<T, D, false, true>
                        : attend_few_kernel<T, D, false, false>);
-  hipLaunchKernelGGL(f, grid, dim3(64 * kWaves), 0, s, a);
+  auto g = cap ? (bias ? sinks_few_kernel<T, D, true, true> : sinks_few_kernel<T, D, true, false>)
+               : (bias ? sinks_few_kernel<T, D, false, true>
+                       : sinks_few_kernel<T, D, false, false>);
+  hipLaunchKernelGGL(a.rule.sink > 0 ? g : f, grid, dim3(64 * kWaves), 0, s, a);
 }
 
 }  // namespace

@@ -32,7 +32,8 @@ __attribute__((used)) const char kBuiltFor[] = "spot binding for torch " SPOT_TO
 // Entry points of the loaded libspot, in the order spot.py passes them.
 enum Fn {
   kScore, kScoreQ, kScoreTokensBlk, kProject, kProjectPooled, kPool, kSelect, kSparseBlk, kDense,
-  kPrefill, kStep, kStepQ, kStepStatic, kRotary, kRotaryAppend, kAttend, kWeights, kEvict, kFns
+  kPrefill, kStep, kStepQ, kStepStatic, kRotary, kRotaryAppend, kAttend, kWeights, kEvict,
+  kRotaryAxes, kRotaryAppend8, kAttendSinks, kAttend8, kFns
 };
 void* g_fn[kFns];
 PyObject* g_stream_type;    // torch.cuda.Stream
@@ -41,7 +42,9 @@ PyObject* g_stream_attr;    // "cuda_stream"
 template <typename F>
 F fn(Fn i, F) { return reinterpret_cast<F>(g_fn[i]); }
 
-enum : unsigned { BF16 = 1, I16 = 2, I32 = 4, F32 = 8, U8 = 16, I8 = 32, F16 = 64, ANY = ~0u };
+enum : unsigned {
+  BF16 = 1, I16 = 2, I32 = 4, F32 = 8, U8 = 16, I8 = 32, F16 = 64, F8 = 128, E8 = 256, ANY = ~0u
+};
 constexpr unsigned kBf = BF16 | I16;
 
 unsigned dtype_bit(at::ScalarType t) {
@@ -53,6 +56,8 @@ unsigned dtype_bit(at::ScalarType t) {
     case at::kByte: return U8;
     case at::kChar: return I8;
     case at::kHalf: return F16;
+    case at::kFloat8_e4m3fn: return F8;
+    case at::kFloat8_e8m0fnu: return E8;
     default: return 0;
   }
 }
@@ -687,6 +692,150 @@ PyObject* cache_evict(Args a) {
   });
 }
 
+// Axes of the pairs, on the host; where the call has none (axes 0) it is not read.
+const uint8_t* axis_of(Args& a, const Dev& t, int axes, int rope_dim) {
+  if (t.none()) return a.ok = a.ok && axes == 0, nullptr;
+  if (!a.ok || !THPVariable_CheckExact(t.o)) return a.ok = false, nullptr;
+  const at::Tensor& x = THPVariable_Unpack(t.o);
+  if (!x.is_cpu() || x.scalar_type() != at::kByte || !x.is_contiguous() ||
+      (axes > 0 && x.numel() < rope_dim / 2))
+    return a.ok = false, nullptr;
+  return static_cast<const uint8_t*>(x.data_ptr());
+}
+
+// Scales of an 8-bit pool.
+big pool_scales(int n_pages, int h_kv, int page_size) { return (big)n_pages * h_kv * page_size / 16; }
+
+// x, x_stride, pos, n_axes, axis, rows, heads, d, rope_dim, freq, amp, flags, out, out_stride,
+// stream
+PyObject* rotary_axes(Args a) {
+  Dev x(a);
+  const int64_t xs = wide(a);
+  Dev pos(a);
+  const int axes = a.integer();
+  Dev axis(a);
+  const int rows = a.integer(), heads = a.integer(), d = a.integer(), rope = a.integer();
+  Dev freq(a);
+  const float amp = a.real();
+  const int flags = a.integer();
+  Dev out(a);
+  const int64_t os = wide(a);
+  void* st = a.stream();
+  const Element el(a, x);
+  const Place place(a, x, pos, out);
+  void *xp = rows_of(a, x, el.bit, rows, xs, (big)heads * d), *pp = pos.ptr(a, I32, (big)rows * axes),
+       *op = rows_of(a, out, el.bit, rows, os, (big)heads * d);
+  const double* fr = freq_of(a, freq, rope);
+  const uint8_t* ax = axis_of(a, axis, axes, rope);
+  return finish(a, [&] {
+    return fn(kRotaryAxes, &spot_rotary_axes)(xp, xs, ip(pp), axes, ax, rows, heads, d, rope, fr, amp,
+                                              flags, el.dtype, op, os, st);
+  });
+}
+
+// q, q_stride, k, k_stride, v, v_stride, pos, n_axes, axis, page_table, n_pages, page_size,
+// max_pages, seq_start, seq_len, n_seq, rows, h_q, h_kv, d, rope_dim, freq, amp, flags, q_out,
+// k_pages, v_pages, k_scale, v_scale, stream
+PyObject* rotary_append8(Args a) {
+  Dev q(a);
+  const int64_t qs = wide(a);
+  Dev k(a);
+  const int64_t ks = wide(a);
+  Dev v(a);
+  const int64_t vs = wide(a);
+  Dev pos(a);
+  const int axes = a.integer();
+  Dev axis(a), tab(a);
+  const int np = a.integer(), ps = a.integer(), mp = a.integer();
+  Dev start(a), len(a);
+  const int ns = a.integer(), rows = a.integer(), hq = a.integer(), hkv = a.integer(),
+            d = a.integer(), rope = a.integer();
+  Dev freq(a);
+  const float amp = a.real();
+  const int flags = a.integer();
+  Dev qo(a), kp(a), vp(a), ksc(a), vsc(a);
+  void* st = a.stream();
+  const Element el(a, q);
+  const Place place(a, q, k, v, pos, tab, start, len, qo, kp, vp, ksc, vsc);
+  const big pool = (big)np * hkv * ps * d;
+  void *qp = rows_of(a, q, el.bit, rows, qs, (big)hq * d),
+       *kip = rows_of(a, k, el.bit, rows, ks, (big)hkv * d),
+       *vip = rows_of(a, v, el.bit, rows, vs, (big)hkv * d), *pp = pos.opt(a, I32, (big)rows * (axes > 1 ? axes : 1)),
+       *tp = tab.ptr(a, I32, (big)ns * mp), *sp = start.ptr(a, I32, (big)ns + 1),
+       *lp = len.ptr(a, I32, ns), *qop = qo.ptr(a, el.bit, (big)rows * hq * d),
+       *kpp = kp.ptr(a, U8 | F8, pool), *vpp = vp.ptr(a, U8 | F8, pool),
+       *ksp = ksc.ptr(a, U8 | E8, pool_scales(np, hkv, ps)),
+       *vsp = vsc.ptr(a, U8 | E8, pool_scales(np, hkv, ps));
+  const double* fr = freq_of(a, freq, rope);
+  const uint8_t* ax = axis_of(a, axis, axes, rope);
+  return finish(a, [&] {
+    return fn(kRotaryAppend8, &spot_rotary_append8)(
+        qp, qs, kip, ks, vip, vs, el.dtype, ip(pp), axes, ax, ip(tp), np, ps, mp, ip(sp), ip(lp), ns, rows, hq,
+        hkv, d, rope, fr, amp, flags, qop, kpp, vpp,
+        static_cast<uint8_t*>(ksp), static_cast<uint8_t*>(vsp), st);
+  });
+}
+
+// q, k_pages, v_pages, page_table, n_pages, page_size, max_pages, seq_start, seq_len, n_seq, rows,
+// h_q, h_kv, d, sm_scale, softcap, slopes, window, n_sink, prefix, first, out, lse, ws, stream
+PyObject* paged_attend_sinks(Args a) {
+  Dev q(a), kp(a), vp(a), tab(a);
+  const int np = a.integer(), ps = a.integer(), mp = a.integer();
+  Dev start(a), len(a);
+  const int ns = a.integer(), rows = a.integer(), hq = a.integer(), hkv = a.integer(),
+            d = a.integer();
+  const float scale = a.real(), softcap = a.real();
+  Dev slopes(a);
+  const int window = a.integer(), sink = a.integer();
+  Dev prefix(a), first(a), out(a), lse(a), ws(a);
+  void* st = a.stream();
+  const Element el(a, q);
+  const Place place(a, q, kp, vp, tab, start, len, slopes, prefix, first, out, lse, ws);
+  const big pool = (big)np * hkv * ps * d, n = (big)rows * hq * d;
+  void *qp = q.ptr(a, el.bit, n), *kpp = kp.ptr(a, el.bit, pool), *vpp = vp.ptr(a, el.bit, pool),
+       *tp = tab.ptr(a, I32, (big)ns * mp), *sp = start.ptr(a, I32, (big)ns + 1),
+       *lp = len.ptr(a, I32, ns), *slp = slopes.opt(a, F32, hq), *prp = prefix.opt(a, I32, ns),
+       *fp_ = first.opt(a, I32, rows), *op = out.ptr(a, el.bit, n),
+       *lsp = lse.opt(a, F32, (big)rows * hq), *wp = ws.ptr(a, ANY, 0);
+  const size_t wb = a.ok ? ws.bytes() : 0;
+  return finish(a, [&] {
+    return fn(kAttendSinks, &spot_paged_attend_sinks)(
+        qp, el.dtype, kpp, vpp, ip(tp), np, ps, mp, ip(sp), ip(lp), ns, rows, hq, hkv, d, scale,
+        softcap, fp(slp), window, sink, ip(prp), ip(fp_), op, static_cast<float*>(lsp), wp, wb, st);
+  });
+}
+
+// q, k_pages, v_pages, k_scale, v_scale, page_table, n_pages, page_size, max_pages, seq_start, seq_len, n_seq, rows,
+// h_q, h_kv, d, sm_scale, softcap, slopes, window, n_sink, prefix, first, out, lse, ws, stream
+PyObject* paged_attend8(Args a) {
+  Dev q(a), kp(a), vp(a), ksc(a), vsc(a), tab(a);
+  const int np = a.integer(), ps = a.integer(), mp = a.integer();
+  Dev start(a), len(a);
+  const int ns = a.integer(), rows = a.integer(), hq = a.integer(), hkv = a.integer(),
+            d = a.integer();
+  const float scale = a.real(), softcap = a.real();
+  Dev slopes(a);
+  const int window = a.integer(), sink = a.integer();
+  Dev prefix(a), first(a), out(a), lse(a), ws(a);
+  void* st = a.stream();
+  const Element el(a, q);
+  const Place place(a, q, kp, vp, ksc, vsc, tab, start, len, slopes, prefix, first, out, lse, ws);
+  const big pool = (big)np * hkv * ps * d, n = (big)rows * hq * d;
+  void *qp = q.ptr(a, el.bit, n), *kpp = kp.ptr(a, U8 | F8, pool), *vpp = vp.ptr(a, U8 | F8, pool),
+       *ksp = ksc.ptr(a, U8 | E8, pool_scales(np, hkv, ps)),
+       *vsp = vsc.ptr(a, U8 | E8, pool_scales(np, hkv, ps)),
+       *tp = tab.ptr(a, I32, (big)ns * mp), *sp = start.ptr(a, I32, (big)ns + 1),
+       *lp = len.ptr(a, I32, ns), *slp = slopes.opt(a, F32, hq), *prp = prefix.opt(a, I32, ns),
+       *fp_ = first.opt(a, I32, rows), *op = out.ptr(a, el.bit, n),
+       *lsp = lse.opt(a, F32, (big)rows * hq), *wp = ws.ptr(a, ANY, 0);
+  const size_t wb = a.ok ? ws.bytes() : 0;
+  return finish(a, [&] {
+    return fn(kAttend8, &spot_paged_attend8)(
+        qp, el.dtype, kpp, vpp, static_cast<uint8_t*>(ksp), static_cast<uint8_t*>(vsp), ip(tp), np, ps, mp, ip(sp), ip(lp), ns, rows, hq, hkv, d, scale,
+        softcap, fp(slp), window, sink, ip(prp), ip(fp_), op, static_cast<float*>(lsp), wp, wb, st);
+  });
+}
+
 // q, k, v, out, cap, acc, acc_out, pools...: whether the shapes that are given belong together:
 // pools [*, h_kv, page_size, d] alike, each second one with the pages of the one before it or
 // more, q [rows, *, d], k and v [rows or more, h_kv, d], out [rows or more, heads of q, d], rows
@@ -781,6 +930,10 @@ PyMethodDef methods[] = {{"init", init, METH_VARARGS, nullptr},
                          SPOT_ENTRY(paged_attend),
                          SPOT_ENTRY(paged_weights),
                          SPOT_ENTRY(cache_evict),
+                         SPOT_ENTRY(rotary_axes),
+                         SPOT_ENTRY(rotary_append8),
+                         SPOT_ENTRY(paged_attend_sinks),
+                         SPOT_ENTRY(paged_attend8),
                          SPOT_ENTRY(paged_fits),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods};

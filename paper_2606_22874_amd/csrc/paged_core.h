@@ -192,10 +192,11 @@ struct Part {
 };
 
 // Blocks of 64 keys that the rows of a sequence see at most (documents aside).
-__device__ __forceinline__ int span_blocks(const Seq& q, int window, int cap) {
+__device__ __forceinline__ int span_blocks(const Seq& q, int window, int sink, int cap) {
   const int hi = min(q.len, cap), p0 = q.len - q.n;
   const int lo = window > 0 && window <= p0 ? p0 - window + 1 : 0;
-  return hi > lo ? (hi + 63) / 64 - lo / 64 : 0;
+  const int sinks = sink > 0 ? min((sink - 1) / 64 + 1, min(lo, cap) / 64) : 0;
+  return (hi > lo ? (hi + 63) / 64 - lo / 64 : 0) + sinks;
 }
 
 // The part of unit `unit` (of the parts of all tiles of TR rows, one KV head), found by
@@ -217,7 +218,8 @@ constexpr int kMaxJoin = 64;
 template <int TR, int ROUND>
 __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
                                           const int32_t* seq_len, int n_seq, int rows, int G,
-                                          int h_kv, int window, int cap, int from, int to) {
+                                          int h_kv, int window, int sink, int cap, int from,
+                                          int to) {
   const int lane = __lane_id();
   auto most_parts = [](int nb) {
     return ROUND ? kMaxJoin : min(kMaxJoin, (int)ceilf(2.f * sqrtf((float)nb)));
@@ -235,7 +237,7 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
     if (base + lane < n_seq) q = sequence(seq_start, seq_len, base + lane, rows);
     if (base == 0) q0 = q;
     const int T = tiles_of(q);
-    steps += wave_sum((float)T * (float)span_blocks(q, window, cap));
+    steps += wave_sum((float)T * (float)span_blocks(q, window, sink, cap));
     tiles += wave_sum_i(T);
   }
   Part r;
@@ -246,7 +248,7 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
   const int least = ROUND ? 4 : tiles * h_kv <= 16 ? 2 : tiles * h_kv <= 96 ? 4 : 8;
   int per = max(least, (int)ceilf(steps * (float)h_kv / (float)kTarget));
   if (ROUND && n_seq <= 64) {
-    const int T = tiles_of(q0), nb = T ? span_blocks(q0, window, cap) : 0;
+    const int T = tiles_of(q0), nb = T ? span_blocks(q0, window, sink, cap) : 0;
     if (__ballot(nb > per)) {
       int best = 0x7fffffff, at = per;
       for (int e = 8; e <= 32; e += e < 12 ? 1 : e < 20 ? 2 : 4) {
@@ -272,7 +274,7 @@ __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,
       q = Seq{0, 0, 0};
       if (base + lane < n_seq) q = sequence(seq_start, seq_len, base + lane, rows);
     }
-    const int T = tiles_of(q), nb = span_blocks(q, window, cap);
+    const int T = tiles_of(q), nb = span_blocks(q, window, sink, cap);
     const int ns = max(1, min((nb + per - 1) / per, most_parts(nb)));
     const int units = T * ns;
     const int incl = wave_incl_scan_i(units);
@@ -318,6 +320,7 @@ inline bool launchable(int64_t groups, unsigned threads) {
 
 struct AttendArgs {
   const uint16_t *q, *k, *v;
+  const uint8_t *k8, *v8, *k_scale, *v_scale;   // of an 8-bit cache, in place of k and v
   Pages pages;
   const int32_t *seq_start, *seq_len;
   int n_seq, rows, h_q, h_kv;
@@ -332,6 +335,10 @@ hipError_t launch_attend_few(AttendArgs a, int dtype, int d, void* ws, hipStream
 size_t attend_few_workspace(int d);
 hipError_t launch_attend_many(AttendArgs a, int dtype, int d, void* ws, hipStream_t s);
 size_t attend_many_workspace(int d);
+hipError_t launch_sinks_many(AttendArgs a, int dtype, int d, void* ws, hipStream_t s);
+// The same over an 8-bit cache.
+hipError_t launch_attend_few8(AttendArgs a, int dtype, int d, void* ws, hipStream_t s);
+hipError_t launch_attend_many8(AttendArgs a, int dtype, int d, void* ws, hipStream_t s);
 
 // Workgroups of a launch over tiles of TR rows: every tile in one part, and the parts
 // that kTarget shares of the work add.
@@ -386,9 +393,18 @@ struct RotaryArgs {
   int n_seq, rows, h_q, h_kv, d, rope_dim;
   float amp;
   bool inverse;
+  int n_axes;              // 0: one position a row; else [rows, n_axes]
+  uint8_t axis[kMaxPairs];
   PairFreq freq;
 };
 hipError_t launch_rotary(const RotaryArgs& a, int dtype, bool interleaved, hipStream_t s);
+
+// The same into an 8-bit cache.
+struct Append8Args {
+  RotaryArgs r;            // k_pages, v_pages not used
+  uint8_t *k8, *v8, *k_scale, *v_scale;
+};
+hipError_t launch_append8(const Append8Args& a, int dtype, bool interleaved, hipStream_t s);
 
 }  // namespace paged
 }  // namespace spot

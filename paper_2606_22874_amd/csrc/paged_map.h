@@ -45,12 +45,14 @@ __device__ __forceinline__ Seq sequence(const int32_t* seq_start, const int32_t*
 
 // What an attention call sees and how its scores are made: score x = cap *
 // tanh(scale s / cap) (cap 0: scale s) - slope_h |p - t|, for the tokens t of
-// [lo, hi), lo = max(first, p - window + 1), hi = max(p + 1, prefix).
+// [lo, hi), lo = max(first, p - window + 1), hi = max(p + 1, prefix), and those of
+// [first, first + sink) before lo.
 struct Rule {
   float scale, cap;
   const float* slopes;
   int window;
   const int32_t *prefix, *first;
+  int sink;
 };
 
 // Visible tokens [lo, hi) of a row (lo = hi = 0 where there are none).
@@ -63,6 +65,56 @@ __device__ __forceinline__ void visible(const Rule& u, const Seq& q, int s, int 
   lo = u.window > 0 && u.window <= p ? p - u.window + 1 : 0;
   if (u.first) lo = most(lo, u.first[q.start + i]);
   if (lo >= hi) lo = hi = 0;
+}
+
+// The same with sinks: also [from, end) (from = end = 0 where there are none).
+__device__ __forceinline__ void visible(const Rule& u, const Seq& q, int s, int i, int cap, int& lo,
+                                        int& hi, int& from, int& end) {
+  const int p = q.len - q.n + i;
+  hi = p + 1;
+  if (u.prefix) hi = most(hi, least(u.prefix[s], q.len));
+  hi = least(hi, cap);
+  from = u.first ? most(u.first[q.start + i], 0) : 0;
+  lo = u.window > 0 && u.window <= p ? p - u.window + 1 : 0;
+  lo = most(lo, from);
+  end = least(lo - from > u.sink ? from + u.sink : lo, hi);
+  if (from >= end) from = end = 0;
+  if (lo >= hi) lo = hi = 0;
+}
+
+// The blocks of 64 keys that a tile of rows goes through, numbered from 0: n_sink ones
+// from `sink0` on, then those from `main0` on.
+struct Blocks {
+  int sink0, n_sink, main0, n;
+  __host__ __device__ __forceinline__ int at(int i) const {
+    return i < n_sink ? sink0 + i : main0 + (i - n_sink);
+  }
+};
+// Of rows that see tokens of [lo, hi) and [from, end), both empty where lo >= hi resp.
+// from >= end.  Intervals that share a block, or lie the other way round, are one run.
+__device__ __forceinline__ Blocks blocks_of(int lo, int hi, int from, int end) {
+  Blocks b = {0, 0, 0, 0};
+  int m0 = 0, m1 = 0;
+  if (lo < hi) {
+    m0 = lo / 64;
+    m1 = (hi - 1) / 64 + 1;
+  }
+  if (from < end) {
+    const int s0 = from / 64, s1 = (end - 1) / 64 + 1;
+    if (lo >= hi) {
+      m0 = s0;
+      m1 = s1;
+    } else if (s1 > m0) {
+      m0 = least(m0, s0);
+      m1 = most(m1, s1);
+    } else {
+      b.sink0 = s0;
+      b.n_sink = s1 - s0;
+    }
+  }
+  b.main0 = m0;
+  b.n = b.n_sink + m1 - m0;
+  return b;
 }
 
 }  // namespace paged

@@ -47,7 +47,8 @@ SYMBOLS = ["spot_status_str", "spot_version", "spot_selector_score",
            "spot_test_force_expiry",
            "spot_rope_frequencies", "spot_rotary", "spot_rotary_append",
            "spot_paged_workspace_bytes", "spot_paged_attend", "spot_paged_weights",
-           "spot_cache_evict",
+           "spot_cache_evict", "spot_rotary_axes", "spot_rotary_append8",
+           "spot_paged_attend_sinks", "spot_paged_attend8",
            "spot_probe_stream_read", "spot_probe_sink_words"]
 
 
@@ -119,6 +120,13 @@ def load(path: Optional[str] = None):
                                          P, P, P, F, P, P]
         L.spot_cache_evict.argtypes = [P, P, P, P, I, I, I, P, I, I, I, I, I, I, P, P, P, I, I, P,
                                        P, P, I, P]
+        L.spot_rotary_axes.argtypes = [P, Q, P, I, P, I, I, I, I, P, F, I, I, P, Q, P]
+        L.spot_rotary_append8.argtypes = [P, Q, P, Q, P, Q, I, P, I, P, P, I, I, I, P, P, I, I, I,
+                                          I, I, I, P, F, I, P, P, P, P, P, P]
+        L.spot_paged_attend_sinks.argtypes = [P, I, P, P, P, I, I, I, P, P, I, I, I, I, I, F, F, P,
+                                              I, I, P, P, P, P, P, Z, P]
+        L.spot_paged_attend8.argtypes = [P, I, P, P, P, P, P, I, I, I, P, P, I, I, I, I, I, F, F, P,
+                                         I, I, P, P, P, P, P, Z, P]
         L.spot_probe_stream_read.argtypes = [P, Z, P, P]
         L.spot_probe_stream_read.restype = ctypes.c_int32
         L.spot_probe_sink_words.restype = I
@@ -130,7 +138,9 @@ def load(path: Optional[str] = None):
                      "spot_dense_decode", "spot_sparse_prefill", "spot_decode_step",
                      "spot_decode_step_q", "spot_decode_step_static", "spot_decode_step_status",
                      "spot_rope_frequencies", "spot_rotary", "spot_rotary_append",
-                     "spot_paged_attend", "spot_paged_weights", "spot_cache_evict"):
+                     "spot_paged_attend", "spot_paged_weights", "spot_cache_evict",
+                     "spot_rotary_axes", "spot_rotary_append8", "spot_paged_attend_sinks",
+                     "spot_paged_attend8"):
             getattr(L, name).restype = ctypes.c_int32
         if path is None:
             _load_native(L)
@@ -152,7 +162,8 @@ def _load_native(L):
                  L.spot_select_blocks, L.spot_sparse_decode_blk, L.spot_dense_decode,
                  L.spot_sparse_prefill, L.spot_decode_step, L.spot_decode_step_q,
                  L.spot_decode_step_static, L.spot_rotary, L.spot_rotary_append,
-                 L.spot_paged_attend, L.spot_paged_weights, L.spot_cache_evict)
+                 L.spot_paged_attend, L.spot_paged_weights, L.spot_cache_evict, L.spot_rotary_axes,
+                 L.spot_rotary_append8, L.spot_paged_attend_sinks, L.spot_paged_attend8)
         _binding.init(tuple(ctypes.cast(f, ctypes.c_void_p).value for f in order),
                       torch.cuda.Stream)
         _native = _binding
@@ -196,6 +207,8 @@ BF16 = (torch.bfloat16, torch.int16)
 I32 = (torch.int32,)
 F32 = (torch.float32,)
 U8 = (torch.uint8,)
+CODES8 = (torch.uint8, torch.float8_e4m3fn)
+SCALES8 = (torch.uint8, torch.float8_e8m0fnu)
 
 
 PAGED_DTYPE = {torch.bfloat16: 0, torch.float16: 1}
@@ -633,6 +646,25 @@ def _freq(freq, rope_dim):
         raise ValueError(f"freq: {freq.numel()} elements, need {rope_dim // 2}")
 
 
+def _axis(axis, n_axes, rope_dim):
+    """Axes of the pairs; not read where the call has none."""
+    if axis is None and n_axes == 0:
+        return
+    if not isinstance(axis, torch.Tensor) or axis.device.type != "cpu" or \
+            axis.dtype != torch.uint8 or not axis.is_contiguous():
+        raise ValueError("axis must be a contiguous uint8 host tensor")
+    if n_axes > 0 and axis.numel() < rope_dim // 2:
+        raise ValueError(f"axis: {axis.numel()} elements, need {rope_dim // 2}")
+
+
+def _pools8(k_pages, v_pages, k_scale, v_scale, tokens, d):
+    """Codes and scales of 8-bit pools of tokens x d elements."""
+    _dev(k_pages, "k_pages", CODES8, tokens * d)
+    _dev(v_pages, "v_pages", CODES8, tokens * d)
+    _dev(k_scale, "k_scale", SCALES8, tokens // 16)
+    _dev(v_scale, "v_scale", SCALES8, tokens // 16)
+
+
 def spot_rope_frequencies(rope_dim, rope_base, scaling, factor, orig_len, low, high, freq):
     _freq(freq, rope_dim)
     _check("spot_rope_frequencies", load().spot_rope_frequencies(
@@ -794,6 +826,127 @@ def spot_cache_evict(acc, k_pages, v_pages, page_table, n_pages, page_size, max_
             max_pages, _ptr(seq_len), n_seq, h_kv, d, budget, n_sink, n_recent, _ptr(k_dst),
             _ptr(v_dst), _ptr(dst_table), n_dst_pages, dst_max_pages, _ptr(idx), _ptr(new_len),
             _ptr(acc_out), out_cap, s))
+
+
+def spot_rotary_axes(x, x_stride, pos, n_axes, axis, rows, heads, d, rope_dim, freq, amp, flags, out,
+                     out_stride, stream=None):
+    if _native is not None:
+        st = _native.rotary_axes(x, x_stride, pos, n_axes, axis, rows, heads, d, rope_dim, freq,
+                                 amp, flags, out, out_stride, stream)
+        if st is not None:
+            return _check("spot_rotary_axes", st)
+    dt = _element(x, "x")
+    _row_tensor(x, "x", x.dtype, rows, x_stride, heads * d)
+    _dev(pos, "pos", I32, rows * n_axes)
+    _axis(axis, n_axes, rope_dim)
+    _freq(freq, rope_dim)
+    _row_tensor(out, "out", x.dtype, rows, out_stride, heads * d)
+    dev, s = _same_device(stream, x, pos, out)
+    with torch.cuda.device(dev):
+        _check("spot_rotary_axes", load().spot_rotary_axes(
+            _ptr(x), x_stride, _ptr(pos), n_axes, _ptr(axis), rows, heads, d, rope_dim, _ptr(freq), float(amp), flags,
+            dt, _ptr(out), out_stride, s))
+
+
+def spot_rotary_append8(q, q_stride, k, k_stride, v, v_stride, pos, n_axes, axis, page_table, n_pages,
+                        page_size, max_pages, seq_start, seq_len, n_seq, rows, h_q, h_kv, d,
+                        rope_dim, freq, amp, flags, q_out, k_pages, v_pages, k_scale, v_scale,
+                        stream=None):
+    if _native is not None:
+        st = _native.rotary_append8(q, q_stride, k, k_stride, v, v_stride, pos, n_axes, axis,
+                                    page_table, n_pages, page_size, max_pages, seq_start, seq_len,
+                                    n_seq, rows, h_q, h_kv, d, rope_dim, freq, amp, flags, q_out,
+                                    k_pages, v_pages, k_scale, v_scale, stream)
+        if st is not None:
+            return _check("spot_rotary_append8", st)
+    dt = _element(q, "q")
+    el = (q.dtype,)
+    _row_tensor(q, "q", q.dtype, rows, q_stride, h_q * d)
+    _row_tensor(k, "k", q.dtype, rows, k_stride, h_kv * d)
+    _row_tensor(v, "v", q.dtype, rows, v_stride, h_kv * d)
+    _opt(pos, "pos", I32, rows * max(n_axes, 1))
+    _axis(axis, n_axes, rope_dim)
+    _dev(page_table, "page_table", I32, n_seq * max_pages)
+    _dev(seq_start, "seq_start", I32, n_seq + 1)
+    _dev(seq_len, "seq_len", I32, n_seq)
+    _freq(freq, rope_dim)
+    _dev(q_out, "q_out", el, rows * h_q * d)
+    _pools8(k_pages, v_pages, k_scale, v_scale, n_pages * h_kv * page_size, d)
+    dev, s = _same_device(stream, q, k, v, pos, page_table, seq_start, seq_len, q_out, k_pages,
+                          v_pages, k_scale, v_scale)
+    with torch.cuda.device(dev):
+        _check("spot_rotary_append8", load().spot_rotary_append8(
+            _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, dt, _ptr(pos),
+            n_axes, _ptr(axis), _ptr(page_table), n_pages, page_size, max_pages, _ptr(seq_start), _ptr(seq_len),
+            n_seq, rows, h_q, h_kv, d, rope_dim, _ptr(freq), float(amp), flags, _ptr(q_out),
+            _ptr(k_pages), _ptr(v_pages), _ptr(k_scale), _ptr(v_scale), s))
+
+
+def spot_paged_attend_sinks(q, k_pages, v_pages, page_table, n_pages, page_size, max_pages, seq_start,
+                            seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes, window,
+                            n_sink, prefix, first, out, lse, ws, stream=None):
+    if _native is not None:
+        st = _native.paged_attend_sinks(q, k_pages, v_pages, page_table, n_pages, page_size,
+                                        max_pages, seq_start, seq_len, n_seq, rows, h_q, h_kv, d,
+                                        sm_scale, softcap, slopes, window, n_sink, prefix, first,
+                                        out, lse, ws, stream)
+        if st is not None:
+            return _check("spot_paged_attend_sinks", st)
+    dt = _element(q, "q")
+    el = (q.dtype,)
+    _dev(q, "q", el, rows * h_q * d)
+    _dev(k_pages, "k_pages", el, n_pages * h_kv * page_size * d)
+    _dev(v_pages, "v_pages", el, n_pages * h_kv * page_size * d)
+    _dev(page_table, "page_table", I32, n_seq * max_pages)
+    _dev(seq_start, "seq_start", I32, n_seq + 1)
+    _dev(seq_len, "seq_len", I32, n_seq)
+    _opt(slopes, "slopes", F32, h_q)
+    _opt(prefix, "prefix", I32, n_seq)
+    _opt(first, "first", I32, rows)
+    _dev(out, "out", el, rows * h_q * d)
+    _opt(lse, "lse", F32, rows * h_q)
+    _dev(ws, "ws", None)
+    dev, s = _same_device(stream, q, k_pages, v_pages, page_table, seq_start, seq_len, slopes,
+                          prefix, first, out, lse, ws)
+    with torch.cuda.device(dev):
+        _check("spot_paged_attend_sinks", load().spot_paged_attend_sinks(
+            _ptr(q), dt, _ptr(k_pages), _ptr(v_pages), _ptr(page_table), n_pages, page_size,
+            max_pages, _ptr(seq_start), _ptr(seq_len), n_seq, rows, h_q, h_kv, d, float(sm_scale),
+            float(softcap), _ptr(slopes), window, n_sink, _ptr(prefix), _ptr(first), _ptr(out), _ptr(lse),
+            _ptr(ws), ws.numel() * ws.element_size(), s))
+
+
+def spot_paged_attend8(q, k_pages, v_pages, k_scale, v_scale, page_table, n_pages, page_size,
+                       max_pages, seq_start, seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap,
+                       slopes, window, n_sink, prefix, first, out, lse, ws, stream=None):
+    if _native is not None:
+        st = _native.paged_attend8(q, k_pages, v_pages, k_scale, v_scale, page_table, n_pages,
+                                   page_size, max_pages, seq_start, seq_len, n_seq, rows, h_q, h_kv,
+                                   d, sm_scale, softcap, slopes, window, n_sink, prefix, first, out,
+                                   lse, ws, stream)
+        if st is not None:
+            return _check("spot_paged_attend8", st)
+    dt = _element(q, "q")
+    el = (q.dtype,)
+    _dev(q, "q", el, rows * h_q * d)
+    _pools8(k_pages, v_pages, k_scale, v_scale, n_pages * h_kv * page_size, d)
+    _dev(page_table, "page_table", I32, n_seq * max_pages)
+    _dev(seq_start, "seq_start", I32, n_seq + 1)
+    _dev(seq_len, "seq_len", I32, n_seq)
+    _opt(slopes, "slopes", F32, h_q)
+    _opt(prefix, "prefix", I32, n_seq)
+    _opt(first, "first", I32, rows)
+    _dev(out, "out", el, rows * h_q * d)
+    _opt(lse, "lse", F32, rows * h_q)
+    _dev(ws, "ws", None)
+    dev, s = _same_device(stream, q, k_pages, v_pages, k_scale, v_scale, page_table, seq_start, seq_len, slopes,
+                          prefix, first, out, lse, ws)
+    with torch.cuda.device(dev):
+        _check("spot_paged_attend8", load().spot_paged_attend8(
+            _ptr(q), dt, _ptr(k_pages), _ptr(v_pages), _ptr(k_scale), _ptr(v_scale),
+            _ptr(page_table), n_pages, page_size, max_pages, _ptr(seq_start), _ptr(seq_len), n_seq, rows, h_q, h_kv, d, float(sm_scale),
+            float(softcap), _ptr(slopes), window, n_sink, _ptr(prefix), _ptr(first), _ptr(out), _ptr(lse),
+            _ptr(ws), ws.numel() * ws.element_size(), s))
 
 
 def spot_probe_stream_read(buf, sink, stream=None):
@@ -1026,19 +1179,36 @@ def _strides(t, name):
     return row if rows > 1 else heads * d
 
 
-def rotary(x, pos, freq, amp=1.0, interleaved=False, inverse=False, out=None, stream=None):
+def _axes_of(axis, pos, freq):
+    """The number of axes of positions [rows, axes] with the axis of each pair."""
+    if axis is None:
+        return 0
+    if pos is None or pos.dim() != 2 or axis.numel() != freq.numel():
+        raise ValueError("axis: need pos [rows, axes] and an axis for every frequency")
+    return pos.shape[1]
+
+
+def rotary(x, pos, freq, amp=1.0, interleaved=False, inverse=False, out=None, stream=None,
+           axis=None):
     """Rotary positions of x [rows, heads, d] (rows may be strided): the first
     2 len(freq) elements of each head, pairs (i, i + len(freq)) or neighbours.
-    inverse: by the negative angles (also the gradient of the rotation)."""
+    inverse: by the negative angles (also the gradient of the rotation).
+    axis (uint8 host tensor, one for every frequency): pair i turns by pos[row, axis[i]] of
+    pos [rows, axes]."""
     rows, heads, d = x.shape
     if out is None:
         with _on(stream, x.device):
             out = torch.empty((rows, heads, d), dtype=x.dtype, device=x.device)
     else:
         _fits(x, None, None, out, 0, None, None)
-    spot_rotary(x, _strides(x, "x"), pos, rows, heads, d, 2 * freq.numel(), freq, amp,
-                (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_INVERSE if inverse else 0), out,
-                _strides(out, "out"), stream)
+    flags = (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_INVERSE if inverse else 0)
+    n_axes = _axes_of(axis, pos, freq)
+    if n_axes:
+        spot_rotary_axes(x, _strides(x, "x"), pos, n_axes, axis, rows, heads, d, 2 * freq.numel(),
+                         freq, amp, flags, out, _strides(out, "out"), stream)
+    else:
+        spot_rotary(x, _strides(x, "x"), pos, rows, heads, d, 2 * freq.numel(), freq, amp, flags,
+                    out, _strides(out, "out"), stream)
     return out
 
 
@@ -1059,6 +1229,33 @@ def rotary_append(q, k, v, k_pages, v_pages, page_table, seq_start, seq_len, fre
     return q_out
 
 
+def _scales(k_scale, v_scale, n_pages, h_kv, page):
+    """The scales of 8-bit pools: [n_pages or more, h_kv, page_size / 16]."""
+    _shape(k_scale, "k_scale", n_pages, h_kv, page // 16)
+    _shape(v_scale, "v_scale", n_pages, h_kv, page // 16)
+
+
+def rotary_append8(q, k, v, k_pages, v_pages, k_scale, v_scale, page_table, seq_start, seq_len,
+                   freq, amp=1.0, interleaved=False, pos=None, q_out=None, stream=None, axis=None):
+    """rotary_append into an 8-bit paged cache: e4m3 codes k_pages, v_pages [n_pages, h_kv,
+    page_size, d] (uint8 or float8_e4m3fn) and a power of two for every 16 tokens of a head,
+    k_scale, v_scale [n_pages, h_kv, page_size / 16] (uint8 or float8_e8m0fnu).  axis and pos
+    [rows, axes] as in rotary.  Returns q_out."""
+    rows, h_q, d = q.shape
+    n_pages, h_kv, page, _ = k_pages.shape
+    _fits(q, k, v, q_out, 0, None, None, k_pages, v_pages)
+    _scales(k_scale, v_scale, n_pages, h_kv, page)
+    if q_out is None:
+        with _on(stream, q.device):
+            q_out = torch.empty((rows, h_q, d), dtype=q.dtype, device=q.device)
+    spot_rotary_append8(q, _strides(q, "q"), k, _strides(k, "k"), v, _strides(v, "v"), pos,
+                        _axes_of(axis, pos, freq), axis, page_table, n_pages, page,
+                        page_table.shape[1], seq_start, seq_len, seq_len.shape[0], rows, h_q, h_kv,
+                        d, 2 * freq.numel(), freq, amp, ROPE_INTERLEAVED if interleaved else 0,
+                        q_out, k_pages, v_pages, k_scale, v_scale, stream)
+    return q_out
+
+
 def paged_workspace(n_seq, rows, h_q, h_kv, d, device="cuda"):
     """Workspace of paged_attend for calls of at most n_seq sequences and rows rows, its
     counters at zero (each call leaves it ready for the next)."""
@@ -1068,12 +1265,26 @@ def paged_workspace(n_seq, rows, h_q, h_kv, d, device="cuda"):
     return ws
 
 
+def _attend_outputs(q, out, lse, ws, n_seq, h_kv, stream):
+    """What an attention's caller left out, made on the call's stream."""
+    rows, h_q, d = q.shape
+    with _on(stream, q.device):
+        if out is None:
+            out = torch.zeros((rows, h_q, d), dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.full((rows, h_q), -math.inf, dtype=torch.float32, device=q.device)
+        if ws is None:
+            ws = paged_workspace(n_seq, rows, h_q, h_kv, d, q.device)
+    return out, lse, ws
+
+
 def paged_attend(q, k_pages, v_pages, page_table, seq_start, seq_len, sm_scale=None, softcap=0.0,
                  slopes=None, window=0, prefix=None, first=None, out=None, lse=None, ws=None,
-                 stream=None):
+                 stream=None, n_sink=0):
     """Attention of the packed new tokens q [rows, h_q, d] of every sequence over its
     pages; k_pages, v_pages [n_pages, h_kv, page_size, d], page_table [n_seq,
-    max_pages].  Returns (out [rows, h_q, d], lse [rows, h_q])."""
+    max_pages].  n_sink: as many first tokens (of the sequence, or from first on) stay visible
+    before the window.  Returns (out [rows, h_q, d], lse [rows, h_q])."""
     rows, h_q, d = q.shape
     n_pages, h_kv, page, _ = k_pages.shape
     _fits(q, None, None, out, 0, None, None, k_pages, v_pages)
@@ -1081,16 +1292,35 @@ def paged_attend(q, k_pages, v_pages, page_table, seq_start, seq_len, sm_scale=N
     if sm_scale is None:
         sm_scale = 1.0 / math.sqrt(d)
     if out is None or lse is None or ws is None:
-        with _on(stream, q.device):
-            if out is None:
-                out = torch.zeros((rows, h_q, d), dtype=q.dtype, device=q.device)
-            if lse is None:
-                lse = torch.full((rows, h_q), -math.inf, dtype=torch.float32, device=q.device)
-            if ws is None:
-                ws = paged_workspace(n_seq, rows, h_q, h_kv, d, q.device)
+        out, lse, ws = _attend_outputs(q, out, lse, ws, n_seq, h_kv, stream)
+    if n_sink:
+        spot_paged_attend_sinks(q, k_pages, v_pages, page_table, n_pages, page, max_pages, seq_start,
+                                seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes,
+                                window, n_sink, prefix, first, out, lse, ws, stream)
+        return out, lse
     spot_paged_attend(q, k_pages, v_pages, page_table, n_pages, page, max_pages, seq_start,
                       seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes, window,
                       prefix, first, out, lse, ws, stream)
+    return out, lse
+
+
+def paged_attend8(q, k_pages, v_pages, k_scale, v_scale, page_table, seq_start, seq_len,
+                  sm_scale=None, softcap=0.0, slopes=None, window=0, n_sink=0, prefix=None,
+                  first=None, out=None, lse=None, ws=None, stream=None):
+    """paged_attend over an 8-bit cache (see rotary_append8): the elements are
+    code * 2^(scale - 127).  Returns (out [rows, h_q, d] of q's type, lse [rows, h_q])."""
+    rows, h_q, d = q.shape
+    n_pages, h_kv, page, _ = k_pages.shape
+    _fits(q, None, None, out, 0, None, None, k_pages, v_pages)
+    _scales(k_scale, v_scale, n_pages, h_kv, page)
+    n_seq, max_pages = page_table.shape
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(d)
+    if out is None or lse is None or ws is None:
+        out, lse, ws = _attend_outputs(q, out, lse, ws, n_seq, h_kv, stream)
+    spot_paged_attend8(q, k_pages, v_pages, k_scale, v_scale, page_table, n_pages, page, max_pages,
+                       seq_start, seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes,
+                       window, n_sink, prefix, first, out, lse, ws, stream)
     return out, lse
 
 
