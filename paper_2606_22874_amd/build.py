@@ -27,7 +27,8 @@ ARCH = "gfx950"
 SOURCES = ["api.hip", "api_paged.hip", "frontend.hip", "frontend_mfma.hip", "score.hip",
            "score_many.hip", "score_tokens.hip", "select.hip", "decode.hip", "step.hip",
            "prefill.hip", "rotary.hip", "attend_few.hip", "attend_few8.hip", "attend_many.hip",
-           "attend_many_sinks.hip", "attend_many8.hip", "append8.hip", "weights.hip",
+           "attend_many_sinks.hip", "attend_many8.hip",
+           "attend_many8_sinks.hip", "append8.hip", "weights.hip",
            "evict.hip", "probe.hip"]
 
 HIPCC_FLAGS = [

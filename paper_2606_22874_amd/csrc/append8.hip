@@ -103,49 +103,159 @@ __device__ __forceinline__ uint32_t code4(float a, float b, float c, float d) {
 // A head's 16 tokens, keys (K) or values; lane l: token l / 4, pairs of elements.
 // VEC: pairs of 16-byte chunks, l % 4 and 4 further on; otherwise every fourth pair.
 template <class T, int D, bool VEC, bool IL, bool K>
-__device__ __forceinline__ void store_head(const Append8Args& args, const Group& gr, int krow, int h,
-                                           const float* s_cos, const float* s_sin, int pitch) {
-  const RotaryArgs& a = args.r;
-  constexpr int NP = D / 8;                  // pairs of a lane
-  const int lane = threadIdx.x & 63, tk = lane >> 2, part = lane & 3;
-  const int half = K ? a.rope_dim / 2 : 0;
-  const bool now = tk >= gr.from && tk < gr.to;
-  const int64_t row = gr.row + (now ? tk - gr.from : 0);
-  const uint16_t* const in = (K ? a.k + row * a.k_stride : a.v + row * a.v_stride) + h * D;
-  const int64_t slots = (int64_t)krow + (int64_t)h * a.pages.page_size;   // of the 16 tokens
-  uint8_t* const pool = K ? args.k8 : args.v8;
-  uint8_t* const scales = K ? args.k_scale : args.v_scale;
-  uint8_t* const out = pool + (slots + tk) * D;
+struct Head {
+  static constexpr int NP = D / 8;           // pairs of a lane
+  // (values alone: a reference to the arguments would put them all into scratch memory)
+  uint8_t *pool, *scales;
+  int64_t head_rows;                         // from KV head 0 to this one
+  float amp;
+  int half, from, tk, part, old;
+  bool now;
+  const uint16_t* in;
+  u32x4 raw[VEC ? NP / 4 : 1];
 
-  float xa[NP], xb[NP];
-  float turned = 0.f, plain = 0.f;           // largest magnitudes of finite values
-  auto count = [&](float a, float b, bool rot) {
-    if (rot) {
-      const float x = fabsf(a) + fabsf(b);
-      turned = x < INFINITY ? fmaxf(turned, x) : turned;
-    } else {
-      plain = fabsf(a) < INFINITY ? fmaxf(plain, fabsf(a)) : plain;
-      plain = fabsf(b) < INFINITY ? fmaxf(plain, fabsf(b)) : plain;
-    }
+  __device__ __forceinline__ Head(const Append8Args& args, const Group& gr, int h) {
+    const RotaryArgs& a = args.r;
+    const int lane = threadIdx.x & 63;
+    pool = K ? args.k8 : args.v8;
+    scales = K ? args.k_scale : args.v_scale;
+    head_rows = (int64_t)h * a.pages.page_size;
+    amp = fabsf(a.amp);
+    half = K ? a.rope_dim / 2 : 0;
+    from = gr.from;
+    tk = lane >> 2;
+    part = lane & 3;
+    now = tk >= from && tk < gr.to;
+    const int64_t row = gr.row + (now ? tk - from : 0);
+    in = (K ? a.k + row * a.k_stride : a.v + row * a.v_stride) + h * D;
+  }
+  struct Unit {
+    int u, ca, cb;
+    bool hf, rot;
   };
-  if (now) {
+  __device__ __forceinline__ Unit unit(int m) const {
+    const int u = part + 4 * m;
+    const bool hf = !IL && u < half / 8;
+    return Unit{u, hf ? 8 * u : 16 * u, hf ? half + 8 * u : 16 * u + 8, hf,
+                IL ? 16 * u < 2 * half : hf};
+  }
+  // The new tokens' elements, on their way.
+  __device__ __forceinline__ void load() {
     if constexpr (VEC) {
 #pragma unroll
       for (int m = 0; m < NP / 8; ++m) {
-        const int u = part + 4 * m;
-        const bool hf = !IL && u < half / 8, rot = IL ? 16 * u < 2 * half : hf;
-        const int ca = hf ? 8 * u : 16 * u, cb = hf ? half + 8 * u : 16 * u + 8;
-        const u32x4 x = *reinterpret_cast<const u32x4*>(in + ca);
-        const u32x4 y = *reinterpret_cast<const u32x4*>(in + cb);
+        raw[2 * m] = raw[2 * m + 1] = u32x4{0u, 0u, 0u, 0u};
+        if (now) {
+          const Unit t = unit(m);
+          raw[2 * m] = *reinterpret_cast<const u32x4*>(in + t.ca);
+          raw[2 * m + 1] = *reinterpret_cast<const u32x4*>(in + t.cb);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ int64_t slots(int krow) const {   // pool row of the 16 tokens
+    return krow + head_rows;
+  }
+  // The scale of the earlier tokens.
+  __device__ __forceinline__ void load_scale(int krow) {
+    old = 0;
+    if (from > 0) old = scales[slots(krow) / kGroupKeys];
+  }
+  __device__ __forceinline__ void store(int krow, const float* s_cos, const float* s_sin,
+                                        int pitch) {
+    float xa[NP], xb[NP];
+    float turned = 0.f, plain = 0.f;         // largest magnitudes of finite values
+    auto count = [&](float a, float b, bool rot) {
+      if (rot) {
+        const float x = fabsf(a) + fabsf(b);
+        turned = x < INFINITY ? fmaxf(turned, x) : turned;
+      } else {
+        plain = fabsf(a) < INFINITY ? fmaxf(plain, fabsf(a)) : plain;
+        plain = fabsf(b) < INFINITY ? fmaxf(plain, fabsf(b)) : plain;
+      }
+    };
+    if (now) {
+      if constexpr (VEC) {
+#pragma unroll
+        for (int m = 0; m < NP / 8; ++m) {
+          const Unit t = unit(m);
+          const u32x4 x = raw[2 * m], y = raw[2 * m + 1];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float nx = T::lo(e < 4 ? x[e] : y[e - 4]), ny = T::hi(e < 4 ? x[e] : y[e - 4]);
+            const float fx = e & 1 ? T::hi(x[e / 2]) : T::lo(x[e / 2]);
+            const float fy = e & 1 ? T::hi(y[e / 2]) : T::lo(y[e / 2]);
+            xa[8 * m + e] = t.hf ? fx : nx;
+            xb[8 * m + e] = t.hf ? fy : ny;
+            count(xa[8 * m + e], xb[8 * m + e], t.rot);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int m = 0; m < NP; ++m) {
+          const int i = part + 4 * m;
+          const bool rot = i < half;
+          const int ia = rot && !IL ? i : 2 * i, ib = rot && !IL ? i + half : 2 * i + 1;
+          xa[m] = T::one(in[ia]);
+          xb[m] = T::one(in[ib]);
+          count(xa[m], xb[m], rot);
+        }
+      }
+    }
+    const float top = wave_max(fmaxf(turned * amp, plain));
+    const int64_t at = slots(krow) / kGroupKeys;
+    uint8_t* const out = pool + (slots(krow) + tk) * D;
+    int byte = scale_byte(top < INFINITY ? top : 3.4028235e38f);
+    if (from > 0) {
+      if (byte > old) {          // the earlier tokens' codes once more
+        if (tk < from) {
+          const float down = power(old - byte);
+          uint32_t* const c = reinterpret_cast<uint32_t*>(out) + part * (D / 16);
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(c[i], false);
+            const f32x2 y = __builtin_amdgcn_cvt_pk_f32_fp8(c[i], true);
+            c[i] = code4(x[0] * down, x[1] * down, y[0] * down, y[1] * down);
+          }
+        }
+      } else {
+        byte = old;
+      }
+    }
+    if ((threadIdx.x & 63) == 0) scales[at] = (uint8_t)byte;
+    if (!now) return;
+    const float inv = power(127 - byte);
+    auto turn_at = [&](int m, int p) {
+      const f32x2 t = turn(xa[m], xb[m], s_cos[tk * pitch + p], s_sin[tk * pitch + p]);
+      xa[m] = t[0];
+      xb[m] = t[1];
+    };
+    if constexpr (VEC) {
+#pragma unroll
+      for (int m = 0; m < NP / 8; ++m) {
+        const Unit t = unit(m);
+        if (K && t.rot) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) turn_at(8 * m + e, 8 * t.u + e);
+        }
+        float x[8], y[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float nx = T::lo(e < 4 ? x[e] : y[e - 4]), ny = T::hi(e < 4 ? x[e] : y[e - 4]);
-          const float fx = e & 1 ? T::hi(x[e / 2]) : T::lo(x[e / 2]);
-          const float fy = e & 1 ? T::hi(y[e / 2]) : T::lo(y[e / 2]);
-          xa[8 * m + e] = hf ? fx : nx;
-          xb[8 * m + e] = hf ? fy : ny;
-          count(xa[8 * m + e], xb[8 * m + e], rot);
+          xa[8 * m + e] = fit<T>(xa[8 * m + e], inv);
+          xb[8 * m + e] = fit<T>(xb[8 * m + e], inv);
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float a0 = xa[8 * m + e], b0 = xb[8 * m + e];
+          const float a1 = xa[8 * m + e / 2], b1 = xb[8 * m + e / 2];
+          const float a2 = xa[8 * m + 4 + e / 2], b2 = xb[8 * m + 4 + e / 2];
+          x[e] = t.hf ? a0 : e & 1 ? b1 : a1;
+          y[e] = t.hf ? b0 : e & 1 ? b2 : a2;
+        }
+        *reinterpret_cast<u32x2*>(out + t.ca) = u32x2{code4(x[0], x[1], x[2], x[3]),
+                                                      code4(x[4], x[5], x[6], x[7])};
+        *reinterpret_cast<u32x2*>(out + t.cb) = u32x2{code4(y[0], y[1], y[2], y[3]),
+                                                      code4(y[4], y[5], y[6], y[7])};
       }
     } else {
 #pragma unroll
@@ -153,84 +263,14 @@ __device__ __forceinline__ void store_head(const Append8Args& args, const Group&
         const int i = part + 4 * m;
         const bool rot = i < half;
         const int ia = rot && !IL ? i : 2 * i, ib = rot && !IL ? i + half : 2 * i + 1;
-        xa[m] = T::one(in[ia]);
-        xb[m] = T::one(in[ib]);
-        count(xa[m], xb[m], rot);
+        if (K && rot) turn_at(m, i);
+        const uint32_t c = code4(fit<T>(xa[m], inv), fit<T>(xb[m], inv), 0.f, 0.f);
+        out[ia] = (uint8_t)c;
+        out[ib] = (uint8_t)(c >> 8);
       }
     }
   }
-  const float top = wave_max(fmaxf(turned * fabsf(a.amp), plain));
-  const int64_t at = slots / kGroupKeys;
-  int byte = scale_byte(top < INFINITY ? top : 3.4028235e38f);
-  if (gr.from > 0) {
-    const int old = scales[at];
-    if (byte > old) {          // the earlier tokens' codes once more
-      if (tk < gr.from) {
-        const float down = power(old - byte);
-        uint32_t* const c = reinterpret_cast<uint32_t*>(out) + part * (D / 16);
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(c[i], false);
-          const f32x2 y = __builtin_amdgcn_cvt_pk_f32_fp8(c[i], true);
-          c[i] = code4(x[0] * down, x[1] * down, y[0] * down, y[1] * down);
-        }
-      }
-    } else {
-      byte = old;
-    }
-  }
-  if (lane == 0) scales[at] = (uint8_t)byte;
-  if (!now) return;
-  const float inv = power(127 - byte);
-  auto turn_at = [&](int m, int p) {
-    const f32x2 t = turn(xa[m], xb[m], s_cos[tk * pitch + p], s_sin[tk * pitch + p]);
-    xa[m] = t[0];
-    xb[m] = t[1];
-  };
-  if constexpr (VEC) {
-#pragma unroll
-    for (int m = 0; m < NP / 8; ++m) {
-      const int u = part + 4 * m;
-      const bool hf = !IL && u < half / 8, rot = IL ? 16 * u < 2 * half : hf;
-      const int ca = hf ? 8 * u : 16 * u, cb = hf ? half + 8 * u : 16 * u + 8;
-      if (K && rot) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) turn_at(8 * m + e, 8 * u + e);
-      }
-      float x[8], y[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float a0 = fit<T>(xa[8 * m + e], inv), b0 = fit<T>(xb[8 * m + e], inv);
-        xa[8 * m + e] = a0;
-        xb[8 * m + e] = b0;
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float* A = xa + 8 * m;
-        const float* B = xb + 8 * m;
-        x[2 * e] = hf ? A[2 * e] : A[e];
-        x[2 * e + 1] = hf ? A[2 * e + 1] : B[e];
-        y[2 * e] = hf ? B[2 * e] : A[4 + e];
-        y[2 * e + 1] = hf ? B[2 * e + 1] : B[4 + e];
-      }
-      *reinterpret_cast<u32x2*>(out + ca) = u32x2{code4(x[0], x[1], x[2], x[3]),
-                                                  code4(x[4], x[5], x[6], x[7])};
-      *reinterpret_cast<u32x2*>(out + cb) = u32x2{code4(y[0], y[1], y[2], y[3]),
-                                                  code4(y[4], y[5], y[6], y[7])};
-    }
-  } else {
-#pragma unroll
-    for (int m = 0; m < NP; ++m) {
-      const int i = part + 4 * m;
-      const bool rot = i < half;
-      const int ia = rot && !IL ? i : 2 * i, ib = rot && !IL ? i + half : 2 * i + 1;
-      if (K && rot) turn_at(m, i);
-      const uint32_t c = code4(fit<T>(xa[m], inv), fit<T>(xb[m], inv), 0.f, 0.f);
-      out[ia] = (uint8_t)c;
-      out[ib] = (uint8_t)(c >> 8);
-    }
-  }
-}
+};
 
 // Workgroups: `units` groups x ceil(h_kv / 4) x (keys, values), then the queries' rows.
 template <class T, int D, bool VEC, bool IL, bool AXES>
@@ -249,10 +289,14 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args args, int
   const int chunk = blockIdx.x / 2 % chunks;
   const Group gr = find_group(a, blockIdx.x / 2 / chunks);
   if (gr.s < 0 || gr.t0 >= a.pages.cap()) return;
-  const int krow = a.pages.row(gr.s, gr.t0, 0, a.h_kv);
-  if (krow < 0) return;
   const int h = chunk * kHeads + wave;
+  // What depends on the place in the cache, and the angles, come while the elements do.
   if (keys) {
+    Head<T, D, VEC, IL, true> head(args, gr, min(h, a.h_kv - 1));
+    head.load();
+    const int krow = a.pages.row(gr.s, gr.t0, 0, a.h_kv);
+    if (krow < 0) return;
+    head.load_scale(krow);
     const int half = a.rope_dim / 2;
     for (int i = tid; i < (gr.to - gr.from) * half; i += kThreads) {
       const int tk = gr.from + i / half, p = i % half;
@@ -266,9 +310,14 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args args, int
       s_sin[tk * kPitch + p] = a.inverse ? -sn * a.amp : sn * a.amp;
     }
     __syncthreads();
-    if (h < a.h_kv) store_head<T, D, VEC, IL, true>(args, gr, krow, h, s_cos, s_sin, kPitch);
-  } else {
-    if (h < a.h_kv) store_head<T, D, VEC, IL, false>(args, gr, krow, h, s_cos, s_sin, kPitch);
+    if (h < a.h_kv) head.store(krow, s_cos, s_sin, kPitch);
+  } else if (h < a.h_kv) {
+    Head<T, D, VEC, IL, false> head(args, gr, h);
+    head.load();
+    const int krow = a.pages.row(gr.s, gr.t0, 0, a.h_kv);
+    if (krow < 0) return;
+    head.load_scale(krow);
+    head.store(krow, s_cos, s_sin, kPitch);
   }
 }
 

@@ -4,10 +4,10 @@
 // The division of work, the softmax and the end are those of attend_few.hip: a workgroup of
 // 4 waves takes a run of 64-key blocks for a tile of 16 rows.  A wave takes every fourth
 // half block of 32 keys:
-//   S^T = K Q^T       K rows straight from memory as the A operand: a lane's 16 codes are 16
-//                     neighbouring dims, so Q's dims go to the same places (a dot product
-//                     does not ask for their order), and 8 codes become the operand of one
-//                     MFMA 16x16x32;
+//   S^T = K Q^T       K rows from memory as the A operand, without LDS: a lane's 16 codes are
+//                     16 neighbouring dims, so Q's dims go to the same places (a dot
+//                     product does not ask for their order), and 8 codes become the operand
+//                     of one MFMA 16x16x32;
 //   O^T += V^T P^T    V as codes through LDS and the transposing read of bytes, which gives
 //                     a lane 8 keys of one dim: D/16 MFMAs 16x16x32, P^T straight from the
 //                     scores' accumulators.
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend8_few_kernel(AttendArgs 
   // behind short-circuit ones and a uniform branch the compiler, ROCm 7.2, has kept the
   // uniform part only)
   auto sees = [&](int t) { return ((t >= lo) & (t < hi)) | ((t >= from) & (t < end)); };
-  const Scores<CAP, BIAS> sc(a.rule, pt.q, tok, head);
+  const Scores<CAP, BIAS, true> sc(a.rule, pt.q, tok, head);
   u32x4 qf[2 * KL];
   const size_t qrow = (size_t)(pt.q.start + tok) * a.h_q + head;
 #pragma unroll
@@ -112,7 +112,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend8_few_kernel(AttendArgs 
 #pragma unroll
         for (int i = 0; i < KL; ++i)
           st.k[u][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
-              a.k8 + (size_t)row[u] * D + r16 * D + 64 * i + 16 * kg));
+              a.k8 + (size_t)row[u] * D +
+              (KL == 1 ? r16 * D + 16 * kg
+                       : (8 * i + (r16 & 7)) * D + 64 * (r16 >> 3) + 16 * kg)));
 #pragma unroll
       for (int i = 0; i < VL; ++i)
         st.v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
@@ -161,9 +163,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend8_few_kernel(AttendArgs 
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // D 128: a load took 8 whole rows, and of the lanes r16 and r16 ^ 8 the first gets the
+        // second half of its row from the second's first load, the other way round the first
+        // half (loads of 16 half rows: 179.6 against 177.1 us for four sequences of 131072).
+        u32x4 k[KL];
+        k[0] = st.k[u][0];
+        if constexpr (KL == 2) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            constexpr int kRor8 = 0x128, kUpper = 0xc, kLower = 0x3;
+            k[0][e] = __builtin_amdgcn_update_dpp(st.k[u][0][e], st.k[u][1][e], kRor8, 0xf, kUpper,
+                                                  false);
+            k[1][e] = __builtin_amdgcn_update_dpp(st.k[u][1][e], st.k[u][0][e], kRor8, 0xf, kLower,
+                                                  false);
+          }
+        }
 #pragma unroll
         for (int i = 0; i < 2 * KL; ++i) {
-          const u32x4& x = st.k[u][i / 2];
+          const u32x4& x = k[i / 2];
           s[u] = T::mfma32(wide8<T>(x[i % 2 * 2], x[i % 2 * 2 + 1], ksc[u], ksc[u]), qf[i], s[u]);
         }
       }

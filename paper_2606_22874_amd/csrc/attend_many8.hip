@@ -1,4 +1,5 @@
-// Attention of many rows over an 8-bit paged cache (gfx950): see attend_many_core.h.
+// Attention of many rows over an 8-bit paged cache (gfx950), the instances without sinks:
+// see attend_many_core.h.
 #include "attend_many_core.h"
 
 namespace spot {
@@ -9,7 +10,7 @@ using namespace many;
 
 template <class T, int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(64 * kWaves) void attend8_many_kernel(AttendArgs a) {
-  attend_many<T, D, CAP, BIAS, true, true>(a);
+  attend_many<T, D, CAP, BIAS, false, true>(a);
 }
 
 template <class T, int D>
@@ -26,6 +27,7 @@ void launch(const AttendArgs& a, dim3 grid, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_attend_many8(AttendArgs a, int dtype, int d, void* ws, hipStream_t s) {
+  if (a.rule.sink > 0) return launch_sinks_many8(a, dtype, d, ws, s);
   a.ws.counters = static_cast<unsigned*>(ws);
   a.ws.ml = reinterpret_cast<float*>(static_cast<char*>(ws) + kCounterBytes);
   a.ws.o = a.ws.ml + (size_t)kMaxParts * kRows * 2;

@@ -99,21 +99,35 @@ struct Copy {
   }
 };
 
-// The same of an 8-bit cache, in two steps: thread i of the 4 waves copies the 16 codes of
-// chunk i % CH of rows i / CH + RW u to a place of its own in LDS (held in registers they
-// would have to live through a softmax, which has none to spare), and when they are down
-// makes them two chunks of elements.
-template <class T, int D, bool IS_K>
+// The same of an 8-bit cache, in two steps: thread i of the 4 waves fetches the 16 codes of
+// chunk i % CH of rows i / CH + RW u, which are on their way behind a softmax, and then
+// stores them as two chunks of elements.  They wait in registers, or (STAGE, where the
+// kernel has none left: with sinks) in a place of the thread's own in LDS, 3 % slower: the
+// wait for the copy, one more read and the stores then follow each other before the
+// barrier.  (Stored before the softmax instead of behind it: 3 % slower again.)
+template <int D, bool STAGE>
+struct Codes {
+  u32x4 raw[STAGE ? 1 : D / 64];
+  unsigned char* stage;                          // 64 D bytes
+  __device__ __forceinline__ u32x4 get(int u, int wave, int lane) const {
+    if constexpr (STAGE)
+      return *reinterpret_cast<const u32x4*>(stage + (4 * u + wave) * 1024 + lane * 16);
+    else
+      return raw[u];
+  }
+};
+template <class T, int D, bool IS_K, bool STAGE>
 struct Widen {
+  typedef many::Codes<D, STAGE> Codes;
   static constexpr int CH = D / 16;              // 16-byte chunks of a row's codes
   static constexpr int RW = 256 / CH;            // rows of the 4 waves at once
   static constexpr int N = 64 / RW;
   static __device__ __forceinline__ int row(int u, int wave, int lane) {
     return RW * u + wave * (64 / CH) + lane / CH;
   }
-  // (the rows of a wave's copy lie in one group of 16 keys)
-  static __device__ __forceinline__ void issue(const uint8_t* pool, const int* list,
-                                               unsigned char* stage, int wave) {
+  // (the rows of a wave's load lie in one group of 16 keys)
+  static __device__ __forceinline__ void load(const uint8_t* pool, const int* list, Codes& to,
+                                              int wave) {
     const int lane = fresh_lane();
 #pragma unroll
     for (int u = 0; u < N; ++u) {
@@ -121,30 +135,33 @@ struct Widen {
       const int at = __builtin_amdgcn_readfirstlane(list[group]);   // -1: a row of no use
       const uint8_t* src = pool + (int64_t)(at < 0 ? 0 : at) * D;
       const uint32_t off = (uint32_t)((row(u, wave, lane) & 15) * D + lane % CH * 16);
-      __builtin_amdgcn_global_load_lds(src + off, (lds_void*)(stage + (4 * u + wave) * 1024), 16, 0,
-                                       0);
+      if constexpr (STAGE)
+        __builtin_amdgcn_global_load_lds(src + off, (lds_void*)(to.stage + (4 * u + wave) * 1024),
+                                         16, 0, 0);
+      else
+        to.raw[u] = *reinterpret_cast<const u32x4*>(src + off);
     }
+  }
+  // Before store() or mend().
+  static __device__ __forceinline__ void wait() {
+    if constexpr (STAGE) __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
   }
   static __device__ __forceinline__ float scale(const uint16_t* scales, int u, int wave) {
     const uint32_t x = scales[(RW * u + wave * (64 / CH)) / 16];
     return scale8(__builtin_amdgcn_readfirstlane(IS_K ? x & 255u : x >> 8));
   }
-  static __device__ __forceinline__ u32x4 codes(const unsigned char* stage, int u, int wave,
-                                                int lane) {
-    return *reinterpret_cast<const u32x4*>(stage + (4 * u + wave) * 1024 + lane * 16);
-  }
   static __device__ __forceinline__ void put(unsigned char* dst, int r, int c, const u32x4& x) {
     const int pc = IS_K ? swz_k<D>(r, c) : swz_v<D>(r, c);
     *reinterpret_cast<u32x4*>(dst + r * (2 * D) + (pc << 4)) = x;
   }
-  static __device__ __forceinline__ void store(const unsigned char* stage, const uint16_t* scales,
+  static __device__ __forceinline__ void store(const Codes& from, const uint16_t* scales,
                                                unsigned char* dst, int wave) {
     const int lane = fresh_lane(), c = lane % CH * 2;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int r = row(u, wave, lane);
       const float s = scale(scales, u, wave);
-      const u32x4 x = codes(stage, u, wave, lane);
+      const u32x4 x = from.get(u, wave, lane);
       put(dst, r, c, wide8<T>(x[0], x[1], s, s));
       put(dst, r, c + 1, wide8<T>(x[2], x[3], s, s));
     }
@@ -153,16 +170,16 @@ struct Widen {
   // (unseen) or that have no page, and for infinite and NaN elements of the others, of
   // which it tells.
   template <class F>
-  static __device__ __forceinline__ bool mend(const unsigned char* stage, const int* list,
+  static __device__ __forceinline__ bool mend(const Codes& from, const int* list,
                                               const uint16_t* scales, unsigned char* dst, int wave,
                                               F unseen) {
     const int lane = fresh_lane(), c = lane % CH * 2;
     bool odd = false;
-#pragma unroll 1
+#pragma unroll
     for (int u = 0; u < N; ++u) {
       const int r = row(u, wave, lane);
       const float s = scale(scales, u, wave);
-      const u32x4 y = codes(stage, u, wave, lane);
+      const u32x4 y = from.get(u, wave, lane);
       const bool none = (list[r >> 4] < 0) | unseen(r);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -288,7 +305,9 @@ struct Wave {
 
   // Online softmax of the scores into pb.  below, above: some row does not see the
   // first or last keys of the block; pages: bit kt says that keys 16 kt .. are there.
-  __device__ __forceinline__ void softmax(int t0, bool below, bool above, unsigned pages) {
+  // sunk: the first keys may be sinks.
+  __device__ __forceinline__ void softmax(int t0, bool below, bool above, bool sunk,
+                                          unsigned pages) {
     asm volatile("s_nop 15"
                  : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[0][2]), "+v"(s[0][3]), "+v"(s[1][0]),
                    "+v"(s[1][1]), "+v"(s[1][2]), "+v"(s[1][3]));   // see settle()
@@ -300,7 +319,7 @@ struct Wave {
 #pragma unroll
       for (int qt = 0; qt < 2; ++qt) {
         const int lane = fresh_lane();
-        Scores<CAP, BIAS> sc;
+        Scores<CAP, BIAS, SINK> sc;
         sc.mul = mul;
         sc.cap2 = cap2;
         sc.slope2 = 0.f;
@@ -328,7 +347,7 @@ struct Wave {
         const int lane = fresh_lane(), at = t0 + 4 * (lane >> 4);
         const RowRule u = rows[16 * qt + (lane & 15)];
         const int from = u.lo - at, to = u.hi - at;
-        if constexpr (SINK) {
+        if (SINK && sunk) {
           const SinkRule e = sinks[16 * qt + (lane & 15)];
           const int s0 = e.from - at, s1 = e.end - at;
 #pragma unroll
@@ -340,20 +359,20 @@ struct Wave {
               s[qt][kt][i] = seen ? s[qt][kt][i] : -INFINITY;
             }
         } else {
-        if (below) {
+          if (below) {
 #pragma unroll
-          for (int kt = 0; kt < 4; ++kt)
+            for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              s[qt][kt][i] = 16 * kt + i < from ? -INFINITY : s[qt][kt][i];
-        }
-        if (above) {
+              for (int i = 0; i < 4; ++i)
+                s[qt][kt][i] = 16 * kt + i < from ? -INFINITY : s[qt][kt][i];
+          }
+          if (above) {
 #pragma unroll
-          for (int kt = 0; kt < 4; ++kt)
+            for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              s[qt][kt][i] = 16 * kt + i >= to ? -INFINITY : s[qt][kt][i];
-        }
+              for (int i = 0; i < 4; ++i)
+                s[qt][kt][i] = 16 * kt + i >= to ? -INFINITY : s[qt][kt][i];
+          }
         }
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt)
@@ -419,20 +438,20 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
   typedef Wave<T, D, CAP, BIAS, SINK> W;
   typedef Copy<D, true> CopyK;
   typedef Copy<D, false> CopyV;
-  typedef Widen<T, D, true> WidenK;
-  typedef Widen<T, D, false> WidenV;
+  typedef Widen<T, D, true, SINK> WidenK;
+  typedef Widen<T, D, false, SINK> WidenV;
   constexpr int kTile = 64 * D * 2, DT = D / 16;
   __shared__ __attribute__((aligned(16))) unsigned char sk0[kTile], sk1[kTile];
   __shared__ __attribute__((aligned(16))) unsigned char sv0[kTile], sv1[kTile];
   __shared__ int s_list[kListBlocks * 4];   // pool row of each 16-key group, -1 without a page
-  __shared__ __attribute__((aligned(16))) unsigned char sk_codes[C8 ? 64 * D : 16];
-  __shared__ __attribute__((aligned(16))) unsigned char sv_codes[C8 ? 64 * D : 16];
+  __shared__ __attribute__((aligned(16))) unsigned char s_codes[C8 && SINK ? 2 * 64 * D : 16];
   __shared__ uint16_t s_scale[C8 ? kListBlocks * 4 : 1];   // their scales: K, and V << 8
   __shared__ int s_lim[kWaves][SINK ? 6 : 4];
   __shared__ int s_missing, s_last, s_odd;
   __shared__ float s_join[kRows][2];
   __shared__ RowRule s_rule[kRows];
   __shared__ SinkRule s_sink[SINK ? kRows : 1];
+  __shared__ int s_see[4];           // the tokens that some row of the tile sees
   __shared__ Part s_part;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int G = a.h_q / a.h_kv, g = blockIdx.x % a.h_kv;
@@ -546,6 +565,12 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
   // numbered by their place
   const int b0 = SINK ? 0 : bl.main0, b1 = b0 + bl.n;
   auto block = [&](int i) SPOT_INLINE { return SINK ? bl.at(i) : i; };
+  if (tid == 0) {                    // (read behind the barriers of the key loop)
+    s_see[0] = LO;
+    s_see[1] = HI;
+    s_see[2] = SLO;
+    s_see[3] = SHI;
+  }
   const int share = (b1 - b0 + pt.n_split - 1) / pt.n_split;
   const int e0 = min(b0 + pt.split * share, b1), e1 = min(e0 + share, b1);
   const bool second = wave >= kWaves / 2;
@@ -586,7 +611,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
     auto vector_phase = [&](int t) SPOT_INLINE {
       const int t0 = block(c0 + t) * 64;
       const unsigned pages = pages_of(t);
-      w.softmax(t0, t0 < all_lo, t0 + 64 > all_hi, pages);
+      w.softmax(t0, t0 < all_lo, t0 + 64 > all_hi, SINK && t0 < ws_hi, pages);
     };
     // Values that no row sees become zero (they may be infinite or NaN, and meet the
     // probability 0).  So do infinite and NaN elements of the others, which not every
@@ -620,19 +645,21 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
       if (t < nb && active(t)) w.qk(k);
       __builtin_amdgcn_s_setprio(1);      // the softmax first, where both could go on
     };
-    // (of an 8-bit cache)
+    Codes<D, SINK> codes;             // of keys or values, by the wave
+    codes.stage = s_codes + (C8 && SINK && second ? 64 * D : 0);
     auto unseen = [&](int t) SPOT_INLINE {
       const int t0 = block(c0 + t) * 64;
       return [=](int r) SPOT_INLINE {
         const int tok = t0 + r;
-        return ((tok < LO) | (tok >= HI)) & ((tok < SLO) | (tok >= SHI));
+        const bool main = (tok >= s_see[0]) & (tok < s_see[1]);
+        return !(SINK ? main | ((tok >= s_see[2]) & (tok < s_see[3])) : main);
       };
     };
     if (second) {
       if constexpr (C8) {
-        WidenK::issue(a.k8, s_list, sk_codes, wave - kWaves / 2);
-        wait_vm();
-        WidenK::store(sk_codes, s_scale, sk0, wave - kWaves / 2);
+        WidenK::load(a.k8, s_list, codes, wave - kWaves / 2);
+        WidenK::wait();
+        WidenK::store(codes, s_scale, sk0, wave - kWaves / 2);
       } else {
         CopyK::issue(a.k, s_list, sk0, wave - kWaves / 2);
         wait_vm();
@@ -648,15 +675,15 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
       if (!second) {
         matrix_phase(t, kcur, vprev);
         if constexpr (C8) {
-          if (t < nb) WidenV::issue(a.v8, s_list + 4 * t, sv_codes, wave);
+          if (t < nb) WidenV::load(a.v8, s_list + 4 * t, codes, wave);
           if (t < nb && active(t)) vector_phase(t);
-          wait_vm();
+          WidenV::wait();
           if (t < nb) {
             if (edge(t)) {
-              if (WidenV::mend(sv_codes, s_list + 4 * t, s_scale + 4 * t, vcur, wave, unseen(t)))
+              if (WidenV::mend(codes, s_list + 4 * t, s_scale + 4 * t, vcur, wave, unseen(t)))
                 s_odd = 1;
             } else {
-              WidenV::store(sv_codes, s_scale + 4 * t, vcur, wave);
+              WidenV::store(codes, s_scale + 4 * t, vcur, wave);
             }
           }
         } else {
@@ -668,10 +695,11 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
         lds_barrier();
       } else {
         if constexpr (C8) {
-          if (t + 1 < nb) WidenK::issue(a.k8, s_list + 4 * (t + 1), sk_codes, wave - kWaves / 2);
+          if (t + 1 < nb)
+            WidenK::load(a.k8, s_list + 4 * (t + 1), codes, wave - kWaves / 2);
           if (t >= 1 && active(t - 1)) vector_phase(t - 1);
-          wait_vm();
-          if (t + 1 < nb) WidenK::store(sk_codes, s_scale + 4 * (t + 1), knext, wave - kWaves / 2);
+          WidenK::wait();
+          if (t + 1 < nb) WidenK::store(codes, s_scale + 4 * (t + 1), knext, wave - kWaves / 2);
         } else {
           if (t + 1 < nb) CopyK::issue(a.k, s_list + 4 * (t + 1), knext, wave - kWaves / 2);
           if (t >= 1 && active(t - 1)) vector_phase(t - 1);
@@ -689,6 +717,14 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
     }
   }
 
+  // What only the end needs is read again here: held, it costs registers in the loop.
+  const Part pe = s_part;
+  const unsigned j1 = pe.tile * kRows;
+  const int n_rows = min((unsigned)kRows, (unsigned)(pe.q.n * G) - j1);
+  auto out_row = [&](int r) SPOT_INLINE {
+    const unsigned j = j1 + r, tok = j / (unsigned)G;
+    return (size_t)(pe.q.start + tok) * a.h_q + g * G + (j - tok * G);
+  };
   // lane (G, r16) holds O^T[16 dt + 4 G + i][row r16]
   settle(w.o[0]);
   settle(w.o[1]);
@@ -703,8 +739,8 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
       const int tok = SINK ? block(v >> 6) * 64 + (v & 63) : v, t0 = tok & ~63;
       bool edge = t0 < FLO || t0 + 64 > FHI;
       for (int t = t0; t < t0 + 64; t += kGroupKeys)
-        edge = edge || t >= cap || a.pages.row(pt.s, t, g, a.h_kv) < 0;
-      const int at = a.pages.row(pt.s, tok & ~(kGroupKeys - 1), g, a.h_kv);
+        edge = edge || t >= cap || a.pages.row(pe.s, t, g, a.h_kv) < 0;
+      const int at = a.pages.row(pe.s, tok & ~(kGroupKeys - 1), g, a.h_kv);
       if (!edge || at < 0) continue;
       const size_t row = ((size_t)at + (tok & (kGroupKeys - 1))) * D;
       float k_scale = 1.f, v_scale = 1.f;
@@ -733,14 +769,14 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
           seen = seen || (tok >= e.from && tok < e.end);
         }
         if (!seen) continue;
-        Scores<CAP, BIAS> sc;
+        Scores<CAP, BIAS, SINK> sc;
         sc.mul = w.mul;
         sc.cap2 = w.cap2;
         sc.slope2 = u.slope2;
         float dot = 0.f;
 #pragma unroll 1
         for (int d = 0; d < D; ++d) {
-          const float q = T::one(a.q[row_of(wave * 32 + qt * 16 + w.r16) * D + d]);
+          const float q = T::one(a.q[out_row(wave * 32 + qt * 16 + w.r16) * D + d]);
           if constexpr (C8)
             dot = fmaf(q, T::lo(wide4(T(), a.k8[row + d], k_scale)[0]), dot);
           else
@@ -758,14 +794,14 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
       }
     }
   }
-  const size_t slot0 = (size_t)pt.slot * a.h_kv + (size_t)g * pt.n_split;
+  const size_t slot0 = (size_t)pe.slot * a.h_kv + (size_t)g * pe.n_split;
 #pragma unroll
   for (int qt = 0; qt < 2; ++qt) {
     const float L = lanes_sum_xor16(lanes_sum_xor32(w.l_run[qt])), M = w.m_run[qt];
     const int r = wave * 32 + qt * 16 + w.r16;
-    if (r >= n_real) continue;
-    if (pt.n_split > 1) {
-      const size_t at = (slot0 + pt.split) * kRows + r;
+    if (r >= n_rows) continue;
+    if (pe.n_split > 1) {
+      const size_t at = (slot0 + pe.split) * kRows + r;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         float* o = a.ws.o + at * D + dt * 16 + 4 * w.G;
@@ -775,7 +811,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
       if (w.G == 0) dec::store_coherent(a.ws.ml + at * 2, make_float2(M, L));
     } else {
       const float inv = L == 0.f ? 0.f : 1.f / L;
-      const size_t row = row_of(r);
+      const size_t row = out_row(r);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
         *reinterpret_cast<u32x2*>(a.out + row * D + dt * 16 + 4 * w.G) =
@@ -785,21 +821,21 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
         a.lse[row] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
     }
   }
-  if (pt.n_split == 1) return;
+  if (pe.n_split == 1) return;
 
   dec::wait_stores();
   __syncthreads();
-  unsigned* const counter = a.ws.counters + (size_t)pt.counter * a.h_kv + g;
+  unsigned* const counter = a.ws.counters + (size_t)pe.counter * a.h_kv + g;
   if (tid == 0)
     s_last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-             (unsigned)(pt.n_split - 1);
+             (unsigned)(pe.n_split - 1);
   __syncthreads();
   if (!s_last) return;
 
   // the last part joins them: each row's M and 1 / L, then its output 4 dims a lane
-  const int n = pt.n_split;
+  const int n = pe.n_split;
   const float* const ml = a.ws.ml + slot0 * kRows * 2;
-  if (tid < n_real) {
+  if (tid < n_rows) {
     float M = -INFINITY, L = 0.f;
     for (int u0 = 0; u0 < n; u0 += 8) {
       float2 t[8];
@@ -818,19 +854,19 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
     }
     s_join[tid][0] = M;
     s_join[tid][1] = L == 0.f ? 0.f : 1.f / L;
-    if (a.lse) a.lse[row_of(tid)] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
+    if (a.lse) a.lse[out_row(tid)] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
   }
   __syncthreads();
   constexpr int Q = D / 4, U = 4;      // quads of a row; rows of a lane in flight
   constexpr int step = 64 * kWaves / Q;
-  for (int r0 = tid / Q; r0 < n_real; r0 += step * U) {
+  for (int r0 = tid / Q; r0 < n_rows; r0 += step * U) {
     const int c = tid % Q;
     f32x4 acc[U];
     float M[U], inv[U];
 #pragma unroll
     for (int e = 0; e < U; ++e) {
       acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const int r = min(r0 + e * step, n_real - 1);
+      const int r = min(r0 + e * step, n_rows - 1);
       M[e] = s_join[r][0];
       inv[e] = s_join[r][1];
     }
@@ -839,7 +875,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
 #pragma unroll
       for (int h = 0; h < 2 * U; ++h) {
         const size_t at =
-            (size_t)min(u0 + h / U, n - 1) * kRows + min(r0 + h % U * step, n_real - 1);
+            (size_t)min(u0 + h / U, n - 1) * kRows + min(r0 + h % U * step, n_rows - 1);
         t[h] = dec::load_coherent(ml + at * 2);
         const float* o = a.ws.o + (slot0 * kRows + at) * D + 4 * c;
         x[h] = dec::load_coherent(o);
@@ -859,8 +895,8 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
 #pragma unroll
     for (int e = 0; e < U; ++e) {
       const int r = r0 + e * step;
-      if (r < n_real)
-        *reinterpret_cast<u32x2*>(a.out + row_of(r) * D + 4 * c) =
+      if (r < n_rows)
+        *reinterpret_cast<u32x2*>(a.out + out_row(r) * D + 4 * c) =
             u32x2{T::pack2(acc[e][0] * inv[e], acc[e][1] * inv[e]),
                   T::pack2(acc[e][2] * inv[e], acc[e][3] * inv[e])};
     }

@@ -124,9 +124,19 @@ __device__ __forceinline__ float tanh_any(float y) {
   return a < 0.5f ? tanh_near(y) : far;
 }
 
+// cap tanh(y) as cap - 2 cap / (1 + e^(2 y)), within 2.5e-7 cap: for scores beyond those of
+// tanh_near, half the operations of tanh_any.  A score of 16 bits' products is off by
+// 1e-5 and more by itself, so caps up to kQuickCap take it.
+constexpr float kQuickCap = 64.f;
+__device__ __forceinline__ float capped(float y, float cap) {
+  const float e = __builtin_amdgcn_exp2f(y * (2.f * kLog2e));
+  return fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + e), cap);
+}
+
 // Scores in the log2 domain.  `ahead`: the row's position less the key's, in FP32 from
 // their difference as integers (positions themselves may need more than 24 bits).
-template <bool CAP, bool BIAS>
+// QUICK: capped() where it is near enough.
+template <bool CAP, bool BIAS, bool QUICK = false>
 struct Scores {
   float mul, cap2, slope2;   // scale log2e, or scale / cap; cap log2e; slope log2e
   int p;                     // the row's position
@@ -137,14 +147,17 @@ struct Scores {
     slope2 = BIAS && u.slopes ? u.slopes[head] * kLog2e : 0.f;
     p = q.len - q.n + i;
   }
-  // Four scores of a lane, `ahead` of the first; NEAR: all of the wave's lie where
+  // Four scores of a lane, `ahead` of the first.  kNear: all of the wave's lie where
   // tanh_near does (most calls have a cap well above their scores).
-  template <bool NEAR>
+  enum How { kAny, kNear, kQuick };
+  template <How HOW>
   __device__ __forceinline__ f32x4 scaled(f32x4 s, float ahead) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float y = s[i] * mul;
-      float x = CAP ? cap2 * (NEAR ? tanh_near(y) : tanh_any(y)) : y;
+      float x = !CAP            ? y
+                : HOW == kQuick ? capped(y, cap2)
+                                : cap2 * (HOW == kNear ? tanh_near(y) : tanh_any(y));
       if (BIAS) x = fmaf(-slope2, fabsf(ahead - (float)i), x);
       s[i] = x;
     }
@@ -161,15 +174,20 @@ struct Scores {
         for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(s[e][i]));
       if (!__ballot(top * fabsf(mul) > 0.5f)) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) s[e] = scaled<true>(s[e], ahead - 16.f * e);
+        for (int e = 0; e < N; ++e) s[e] = scaled<kNear>(s[e], ahead - 16.f * e);
+        return;
+      }
+      if (QUICK && cap2 <= kQuickCap * kLog2e) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) s[e] = scaled<kQuick>(s[e], ahead - 16.f * e);
         return;
       }
     }
 #pragma unroll
-    for (int e = 0; e < N; ++e) s[e] = scaled<false>(s[e], ahead - 16.f * e);
+    for (int e = 0; e < N; ++e) s[e] = scaled<kAny>(s[e], ahead - 16.f * e);
   }
   __device__ __forceinline__ float one(float s, float ahead) const {
-    return scaled<false>(f32x4{s, s, s, s}, ahead)[0];
+    return scaled<kAny>(f32x4{s, s, s, s}, ahead)[0];
   }
 };
 
@@ -339,6 +357,7 @@ hipError_t launch_sinks_many(AttendArgs a, int dtype, int d, void* ws, hipStream
 // The same over an 8-bit cache.
 hipError_t launch_attend_few8(AttendArgs a, int dtype, int d, void* ws, hipStream_t s);
 hipError_t launch_attend_many8(AttendArgs a, int dtype, int d, void* ws, hipStream_t s);
+hipError_t launch_sinks_many8(AttendArgs a, int dtype, int d, void* ws, hipStream_t s);
 
 // Workgroups of a launch over tiles of TR rows: every tile in one part, and the parts
 // that kTarget shares of the work add.

@@ -54,6 +54,33 @@ __device__ __forceinline__ void rotate_row(const RotaryArgs& a, int row) {
   const int tid = threadIdx.x;
   const int half = a.rope_dim / 2;
   const bool append = !QUERIES && a.seq_start != nullptr;
+  const int d = a.d;
+  const int n_rot = a.h_q + (append ? a.h_kv : 0);
+  const int n_vec = n_rot + (append ? a.h_kv : 0);
+  auto input = [&](int h) {                  // of vector h: query heads, key heads, value heads
+    return h < a.h_q   ? a.q + row * a.q_stride + h * d
+           : h < n_rot ? a.k + row * a.k_stride + (h - a.h_q) * d
+                       : a.v + row * a.v_stride + (h - n_rot) * d;
+  };
+  // VEC: two chunks (element offsets): the two halves of eight pairs, or neighbours
+  struct Unit {
+    int h, ca, cb, p0;
+    bool rot;
+  };
+  auto unit = [&](int w) {
+    const int units = d / 16, h = w / units, u = w % units;
+    const bool hf = !IL && u < half / 8;
+    return Unit{h, hf ? 8 * u : 16 * u, hf ? half + 8 * u : 16 * u + 8, 8 * u,
+                IL ? 16 * u < a.rope_dim : hf};
+  };
+  // A thread's first chunks are on their way while its place and angles are found.
+  u32x4 x = {0u, 0u, 0u, 0u}, y = x;
+  auto load = [&](const Unit& t) {
+    const uint16_t* in = input(t.h);
+    x = *reinterpret_cast<const u32x4*>(in + t.ca);
+    y = *reinterpret_cast<const u32x4*>(in + t.cb);
+  };
+  if (VEC && tid < n_vec * (d / 16)) load(unit(tid));
   int pos, krow = -1;                        // krow: pool row of the slot, KV head 0
   if (QUERIES) {
     const Row r = find_row(a, row);
@@ -79,46 +106,25 @@ __device__ __forceinline__ void rotate_row(const RotaryArgs& a, int row) {
     s_sin[tid] = a.inverse ? -sn * a.amp : sn * a.amp;
   }
   __syncthreads();
-  const int n_rot = a.h_q + (append ? a.h_kv : 0);
-  const int n_vec = n_rot + (append ? a.h_kv : 0);
-  const int d = a.d;
-  // input and output of vector h: query heads, key heads, value heads
-  auto place = [&](int h, const uint16_t*& in, uint16_t*& out) {
+  // output of vector h
+  auto place = [&](int h, uint16_t*& out) {
     if (h < a.h_q) {
-      in = a.q + row * a.q_stride + h * d;
       out = a.q_out + row * a.out_stride + h * d;
       return true;
     }
     if (krow < 0) return false;
     const int g = h < n_rot ? h - a.h_q : h - n_rot;
-    in = (h < n_rot ? a.k + row * a.k_stride : a.v + row * a.v_stride) + g * d;
     out = (h < n_rot ? a.k_pages : a.v_pages) + ((int64_t)krow + (int64_t)g * a.pages.page_size) * d;
     return true;
   };
   if constexpr (VEC) {
-    const int units = d / 16;                // of two chunks
-    for (int w = tid; w < n_vec * units; w += kThreads) {
-      const int h = w / units, u = w % units;
-      const uint16_t* in;
+    for (int w = tid; w < n_vec * (d / 16); w += kThreads) {
+      const Unit t = unit(w);
       uint16_t* out;
-      if (!place(h, in, out)) continue;
-      // chunks (element offsets): the two halves of eight pairs, or neighbours
-      int ca, cb, p0;
-      bool rot;
-      if (!IL) {
-        rot = u < half / 8;
-        ca = rot ? 8 * u : 16 * u;
-        cb = rot ? half + 8 * u : 16 * u + 8;
-        p0 = 8 * u;
-      } else {
-        ca = 16 * u;
-        cb = ca + 8;
-        rot = ca < a.rope_dim;
-        p0 = 8 * u;
-      }
-      rot = rot && h < n_rot;
-      u32x4 x = *reinterpret_cast<const u32x4*>(in + ca);
-      u32x4 y = *reinterpret_cast<const u32x4*>(in + cb);
+      if (!place(t.h, out)) continue;
+      if (w != tid) load(t);
+      const int ca = t.ca, cb = t.cb, p0 = t.p0;
+      const bool rot = t.rot && t.h < n_rot;
       if (rot) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -146,9 +152,9 @@ __device__ __forceinline__ void rotate_row(const RotaryArgs& a, int row) {
     const int pairs = d / 2;
     for (int w = tid; w < n_vec * pairs; w += kThreads) {
       const int h = w / pairs, i = w % pairs;
-      const uint16_t* in;
+      const uint16_t* in = input(h);
       uint16_t* out;
-      if (!place(h, in, out)) continue;
+      if (!place(h, out)) continue;
       const bool pr = i < half;
       const int ia = pr && !IL ? i : 2 * i, ib = pr && !IL ? i + half : 2 * i + 1;
       const uint16_t xa = in[ia], xb = in[ib];

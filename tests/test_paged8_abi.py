@@ -243,7 +243,7 @@ def test_kernels_registers_and_scratch(tmp_path):
     found = {k: v for k, v in kernels(tmp_path).items() if "paged" in k}
     for part, count, groups in (("sinks_few_kernel", 16, 2), ("sinks_many_kernel", 16, 1),
                                 ("attend8_few_kernel", 16, 2), ("attend8_many_kernel", 16, 1),
-                                ("append8_kernel", 32, 2), ("axes_kernel", 8, 1)):
+                                ("sinks8_many_kernel", 16, 1), ("append8_kernel", 32, 2), ("axes_kernel", 8, 1)):
         some = {k: v for k, v in found.items() if part in k}
         assert len(some) == count, (part, len(some))
         for name, v in some.items():
