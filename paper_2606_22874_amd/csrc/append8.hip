@@ -100,19 +100,23 @@ __device__ __forceinline__ uint32_t code4(float a, float b, float c, float d) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
 }
 
-// A head's 16 tokens, keys (K) or values; lane l: token l / 4, pairs of elements.
-// VEC: pairs of 16-byte chunks, l % 4 and 4 further on; otherwise every fourth pair.
+// A head's 16 tokens, keys (K) or values, in rounds of 64 / kLanes tokens: a lane has four
+// pairs of elements of one.  A round without new tokens is passed over, so that a decode
+// step's one token costs a quarter of a group's instructions (the wave's own chain of them
+// is what a small append waits for).
+// VEC: four neighbouring pairs, two loads of 8 bytes; otherwise every kLanes-th pair.
 template <class T, int D, bool VEC, bool IL, bool K>
 struct Head {
-  static constexpr int NP = D / 8;           // pairs of a lane
+  static constexpr int kLanes = D / 8;       // of a token
+  static constexpr int kTokens = 64 / kLanes, kRounds = kGroupKeys / kTokens;
   // (values alone: a reference to the arguments would put them all into scratch memory)
   uint8_t *pool, *scales;
   int64_t head_rows;                         // from KV head 0 to this one
+  int64_t stride;
   float amp;
-  int half, from, tk, part, old;
-  bool now;
-  const uint16_t* in;
-  u32x4 raw[VEC ? NP / 4 : 1];
+  int half, from, to, tk, part, old;
+  const uint16_t* in;                        // of the first new token
+  u32x2 raw[VEC ? 2 * kRounds : 1];
 
   __device__ __forceinline__ Head(const Append8Args& args, const Group& gr, int h) {
     const RotaryArgs& a = args.r;
@@ -123,32 +127,77 @@ struct Head {
     amp = fabsf(a.amp);
     half = K ? a.rope_dim / 2 : 0;
     from = gr.from;
-    tk = lane >> 2;
-    part = lane & 3;
-    now = tk >= from && tk < gr.to;
-    const int64_t row = gr.row + (now ? tk - from : 0);
-    in = (K ? a.k + row * a.k_stride : a.v + row * a.v_stride) + h * D;
+    to = gr.to;
+    tk = lane / kLanes;
+    part = lane % kLanes;
+    stride = K ? a.k_stride : a.v_stride;
+    in = (K ? a.k : a.v) + gr.row * stride + h * D;
   }
+  // Four pairs from element ca and cb on: the two halves of them, or neighbours.
   struct Unit {
-    int u, ca, cb;
+    int ca, cb;
     bool hf, rot;
   };
-  __device__ __forceinline__ Unit unit(int m) const {
-    const int u = part + 4 * m;
-    const bool hf = !IL && u < half / 8;
-    return Unit{u, hf ? 8 * u : 16 * u, hf ? half + 8 * u : 16 * u + 8, hf,
-                IL ? 16 * u < 2 * half : hf};
+  __device__ __forceinline__ Unit unit() const {
+    const bool hf = !IL && 4 * part < half;
+    return Unit{hf ? 4 * part : 8 * part, hf ? half + 4 * part : 8 * part + 4, hf,
+                4 * part < half};
+  }
+  // The elements of pair m of four, in other forms than VEC.
+  struct Pair {
+    int i, a, b;
+    bool rot;
+  };
+  __device__ __forceinline__ Pair pair(int m) const {
+    const int i = part + kLanes * m;
+    const bool rot = i < half;
+    return Pair{i, rot && !IL ? i : 2 * i, rot && !IL ? i + half : 2 * i + 1, rot};
+  }
+  __device__ __forceinline__ bool round_has(int r) const {       // (the same in all lanes)
+    return r * kTokens < to && (r + 1) * kTokens > from;
+  }
+  __device__ __forceinline__ bool now(int r) const {
+    const int t = r * kTokens + tk;
+    return t >= from && t < to;
+  }
+  __device__ __forceinline__ const uint16_t* row(int r) const {
+    return in + (r * kTokens + tk - from) * stride;
   }
   // The new tokens' elements, on their way.
   __device__ __forceinline__ void load() {
     if constexpr (VEC) {
+      const Unit t = unit();
 #pragma unroll
-      for (int m = 0; m < NP / 8; ++m) {
-        raw[2 * m] = raw[2 * m + 1] = u32x4{0u, 0u, 0u, 0u};
-        if (now) {
-          const Unit t = unit(m);
-          raw[2 * m] = *reinterpret_cast<const u32x4*>(in + t.ca);
-          raw[2 * m + 1] = *reinterpret_cast<const u32x4*>(in + t.cb);
+      for (int r = 0; r < kRounds; ++r) {
+        raw[2 * r] = raw[2 * r + 1] = u32x2{0u, 0u};
+        if (now(r)) {
+          raw[2 * r] = *reinterpret_cast<const u32x2*>(row(r) + t.ca);
+          raw[2 * r + 1] = *reinterpret_cast<const u32x2*>(row(r) + t.cb);
+        }
+      }
+    }
+  }
+  // A lane's four pairs of a round.
+  __device__ __forceinline__ void values(int r, float (&a)[4], float (&b)[4]) const {
+    if constexpr (VEC) {
+      const bool hf = unit().hf;
+      const u32x2 x = raw[2 * r], y = raw[2 * r + 1];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t n = e < 2 ? x[e] : y[e - 2];
+        const float fx = e & 1 ? T::hi(x[e / 2]) : T::lo(x[e / 2]);
+        const float fy = e & 1 ? T::hi(y[e / 2]) : T::lo(y[e / 2]);
+        const float nx = T::lo(n), ny = T::hi(n);
+        a[e] = hf ? fx : nx;
+        b[e] = hf ? fy : ny;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        a[e] = b[e] = 0.f;
+        if (now(r)) {
+          a[e] = T::one(row(r)[pair(e).a]);
+          b[e] = T::one(row(r)[pair(e).b]);
         }
       }
     }
@@ -161,45 +210,20 @@ struct Head {
     old = 0;
     if (from > 0) old = scales[slots(krow) / kGroupKeys];
   }
-  __device__ __forceinline__ void store(int krow, const float* s_cos, const float* s_sin,
-                                        int pitch) {
-    float xa[NP], xb[NP];
+  __device__ __forceinline__ void store(int krow, const float* s_cos, const float* s_sin) {
     float turned = 0.f, plain = 0.f;         // largest magnitudes of finite values
-    auto count = [&](float a, float b, bool rot) {
-      if (rot) {
-        const float x = fabsf(a) + fabsf(b);
-        turned = x < INFINITY ? fmaxf(turned, x) : turned;
-      } else {
-        plain = fabsf(a) < INFINITY ? fmaxf(plain, fabsf(a)) : plain;
-        plain = fabsf(b) < INFINITY ? fmaxf(plain, fabsf(b)) : plain;
-      }
-    };
-    if (now) {
-      if constexpr (VEC) {
 #pragma unroll
-        for (int m = 0; m < NP / 8; ++m) {
-          const Unit t = unit(m);
-          const u32x4 x = raw[2 * m], y = raw[2 * m + 1];
+    for (int r = 0; r < kRounds; ++r) {
+      if (!round_has(r)) continue;
+      float a[4], b[4];
+      values(r, a, b);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float nx = T::lo(e < 4 ? x[e] : y[e - 4]), ny = T::hi(e < 4 ? x[e] : y[e - 4]);
-            const float fx = e & 1 ? T::hi(x[e / 2]) : T::lo(x[e / 2]);
-            const float fy = e & 1 ? T::hi(y[e / 2]) : T::lo(y[e / 2]);
-            xa[8 * m + e] = t.hf ? fx : nx;
-            xb[8 * m + e] = t.hf ? fy : ny;
-            count(xa[8 * m + e], xb[8 * m + e], t.rot);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int m = 0; m < NP; ++m) {
-          const int i = part + 4 * m;
-          const bool rot = i < half;
-          const int ia = rot && !IL ? i : 2 * i, ib = rot && !IL ? i + half : 2 * i + 1;
-          xa[m] = T::one(in[ia]);
-          xb[m] = T::one(in[ib]);
-          count(xa[m], xb[m], rot);
-        }
+      for (int e = 0; e < 4; ++e) {
+        const bool rot = VEC ? unit().rot : pair(e).rot;
+        const float x = fabsf(a[e]), y = fabsf(b[e]), z = x + y;
+        turned = (rot & (z < INFINITY)) ? fmaxf(turned, z) : turned;
+        plain = (!rot & (x < INFINITY)) ? fmaxf(plain, x) : plain;
+        plain = (!rot & (y < INFINITY)) ? fmaxf(plain, y) : plain;
       }
     }
     const float top = wave_max(fmaxf(turned * amp, plain));
@@ -208,68 +232,70 @@ struct Head {
     int byte = scale_byte(top < INFINITY ? top : 3.4028235e38f);
     if (from > 0) {
       if (byte > old) {          // the earlier tokens' codes once more
-        if (tk < from) {
-          const float down = power(old - byte);
-          uint32_t* const c = reinterpret_cast<uint32_t*>(out) + part * (D / 16);
+        const float down = power(old - byte);
+#pragma unroll 1
+        for (int r = 0; r * kTokens < from; ++r) {
+          if (r * kTokens + tk >= from) continue;
+          u32x2* const c = reinterpret_cast<u32x2*>(out + r * kTokens * D) + part;
+          u32x2 z = *c;
 #pragma unroll
-          for (int i = 0; i < D / 16; ++i) {
-            const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(c[i], false);
-            const f32x2 y = __builtin_amdgcn_cvt_pk_f32_fp8(c[i], true);
-            c[i] = code4(x[0] * down, x[1] * down, y[0] * down, y[1] * down);
+          for (int i = 0; i < 2; ++i) {
+            const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(z[i], false);
+            const f32x2 y = __builtin_amdgcn_cvt_pk_f32_fp8(z[i], true);
+            z[i] = code4(x[0] * down, x[1] * down, y[0] * down, y[1] * down);
           }
+          *c = z;
         }
       } else {
         byte = old;
       }
     }
     if ((threadIdx.x & 63) == 0) scales[at] = (uint8_t)byte;
-    if (!now) return;
     const float inv = power(127 - byte);
-    auto turn_at = [&](int m, int p) {
-      const f32x2 t = turn(xa[m], xb[m], s_cos[tk * pitch + p], s_sin[tk * pitch + p]);
-      xa[m] = t[0];
-      xb[m] = t[1];
-    };
-    if constexpr (VEC) {
 #pragma unroll
-      for (int m = 0; m < NP / 8; ++m) {
-        const Unit t = unit(m);
-        if (K && t.rot) {
+    for (int r = 0; r < kRounds; ++r) {
+      if (!round_has(r)) continue;
+      float a[4], b[4];
+      values(r, a, b);
+      const int t = r * kTokens + tk;
+      if constexpr (K) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) turn_at(8 * m + e, 8 * t.u + e);
+        for (int e = 0; e < 4; ++e) {
+          // (sines of pairs that are not rotated: whatever lies there, and not used)
+          const int p = VEC ? 4 * part + e : pair(e).i;
+          const bool rot = VEC ? unit().rot : pair(e).rot;
+          const f32x2 w = turn(a[e], b[e], s_cos[t * kPitch + p], s_sin[t * kPitch + p]);
+          a[e] = rot ? w[0] : a[e];
+          b[e] = rot ? w[1] : b[e];
         }
-        float x[8], y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          xa[8 * m + e] = fit<T>(xa[8 * m + e], inv);
-          xb[8 * m + e] = fit<T>(xb[8 * m + e], inv);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float a0 = xa[8 * m + e], b0 = xb[8 * m + e];
-          const float a1 = xa[8 * m + e / 2], b1 = xb[8 * m + e / 2];
-          const float a2 = xa[8 * m + 4 + e / 2], b2 = xb[8 * m + 4 + e / 2];
-          x[e] = t.hf ? a0 : e & 1 ? b1 : a1;
-          y[e] = t.hf ? b0 : e & 1 ? b2 : a2;
-        }
-        *reinterpret_cast<u32x2*>(out + t.ca) = u32x2{code4(x[0], x[1], x[2], x[3]),
-                                                      code4(x[4], x[5], x[6], x[7])};
-        *reinterpret_cast<u32x2*>(out + t.cb) = u32x2{code4(y[0], y[1], y[2], y[3]),
-                                                      code4(y[4], y[5], y[6], y[7])};
       }
-    } else {
 #pragma unroll
-      for (int m = 0; m < NP; ++m) {
-        const int i = part + 4 * m;
-        const bool rot = i < half;
-        const int ia = rot && !IL ? i : 2 * i, ib = rot && !IL ? i + half : 2 * i + 1;
-        if (K && rot) turn_at(m, i);
-        const uint32_t c = code4(fit<T>(xa[m], inv), fit<T>(xb[m], inv), 0.f, 0.f);
-        out[ia] = (uint8_t)c;
-        out[ib] = (uint8_t)(c >> 8);
+      for (int e = 0; e < 4; ++e) {
+        a[e] = fit<T>(a[e], inv);
+        b[e] = fit<T>(b[e], inv);
+      }
+      uint8_t* const o = out + r * kTokens * D;
+      if constexpr (VEC) {
+        const Unit u = unit();
+        const float x1 = u.hf ? a[1] : b[0], x2 = u.hf ? a[2] : a[1], x3 = u.hf ? a[3] : b[1];
+        const float y0 = u.hf ? b[0] : a[2], y1 = u.hf ? b[1] : b[2], y2 = u.hf ? b[2] : a[3];
+        if (now(r)) {
+          *reinterpret_cast<uint32_t*>(o + u.ca) = code4(a[0], x1, x2, x3);
+          *reinterpret_cast<uint32_t*>(o + u.cb) = code4(y0, y1, y2, b[3]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t c = code4(a[e], b[e], 0.f, 0.f);
+          if (now(r)) {
+            o[pair(e).a] = (uint8_t)c;
+            o[pair(e).b] = (uint8_t)(c >> 8);
+          }
+        }
       }
     }
   }
+  static constexpr int kPitch = D / 2 + 4;   // rows of sines, in other banks
 };
 
 // Workgroups: `units` groups x ceil(h_kv / 4) x (keys, values), then the queries' rows.
@@ -282,8 +308,9 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args args, int
     rotate_row<T, VEC, IL, AXES, true>(a, (int)(blockIdx.x - first));
     return;
   }
-  constexpr int kPitch = D / 2 + 1;          // rows of sines in other banks
-  __shared__ float s_cos[kGroupKeys * kPitch], s_sin[kGroupKeys * kPitch];
+  constexpr int kPitch = Head<T, D, VEC, IL, true>::kPitch;
+  __shared__ __attribute__((aligned(16))) float s_cos[kGroupKeys * kPitch];
+  __shared__ __attribute__((aligned(16))) float s_sin[kGroupKeys * kPitch];
   const int tid = threadIdx.x, wave = tid >> 6;
   const bool keys = blockIdx.x % 2 == 0;
   const int chunk = blockIdx.x / 2 % chunks;
@@ -310,14 +337,14 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args args, int
       s_sin[tk * kPitch + p] = a.inverse ? -sn * a.amp : sn * a.amp;
     }
     __syncthreads();
-    if (h < a.h_kv) head.store(krow, s_cos, s_sin, kPitch);
+    if (h < a.h_kv) head.store(krow, s_cos, s_sin);
   } else if (h < a.h_kv) {
     Head<T, D, VEC, IL, false> head(args, gr, h);
     head.load();
     const int krow = a.pages.row(gr.s, gr.t0, 0, a.h_kv);
     if (krow < 0) return;
     head.load_scale(krow);
-    head.store(krow, s_cos, s_sin, kPitch);
+    head.store(krow, s_cos, s_sin);
   }
 }
 

@@ -47,7 +47,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a) {
   const int G = a.h_q / a.h_kv, g = blockIdx.x % a.h_kv;
   const int cap = a.pages.cap();
   if (wave == 0) {
-    const Part p = find_part<kRows, 0>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len, a.n_seq,
+    const Part p = find_part<kRows, 0, SINK ? kFit<D> : 0>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len, a.n_seq,
                                        a.rows, G, a.h_kv, a.rule.window, SINK ? a.rule.sink : 0,
                                        cap, a.from, a.to);
     if (lane == 0) sm.part = p;
@@ -183,7 +183,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a) {
         for (int i = 0; i < 4; ++i) {
           const int t = t0 + 4 * kg + i;
           if constexpr (SINK)
-            x[i] = page & sees(t) ? x[i] : -INFINITY;
+            x[i] = (page & sees(t)) ? x[i] : -INFINITY;
           else if (!page || t < lo || t >= hi)
             x[i] = -INFINITY;
         }

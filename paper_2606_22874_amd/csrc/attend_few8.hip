@@ -43,7 +43,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend8_few_kernel(AttendArgs 
   const int G = a.h_q / a.h_kv, g = blockIdx.x % a.h_kv;
   const int cap = a.pages.cap();
   if (wave == 0) {
-    const Part p = find_part<kRows, 0>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len, a.n_seq,
+    const Part p = find_part<kRows, 0, kFit<D>>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len, a.n_seq,
                                        a.rows, G, a.h_kv, a.rule.window, a.rule.sink, cap, a.from,
                                        a.to);
     if (lane == 0) sm.part = p;
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend8_few_kernel(AttendArgs 
           const bool page = row_of(n, u) >= 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            s[u][i] = page & sees(t0 + 16 * u + 4 * kg + i) ? s[u][i] : -INFINITY;
+            s[u][i] = (page & sees(t0 + 16 * u + 4 * kg + i)) ? s[u][i] : -INFINITY;
         }
       }
       float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),

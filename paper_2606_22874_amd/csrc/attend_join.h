@@ -19,6 +19,10 @@ constexpr int kRows = 16;          // rows of a tile
 constexpr int kWaves = 4;
 constexpr int kListBlocks = 512;   // blocks whose pages are looked up at once
 
+// Workgroups that run at once, two or (D 64) three on a CU.
+template <int D>
+constexpr int kFit = D == 64 ? 768 : 512;
+
 // KV: bytes of K and V rows that a wave holds.
 template <int D, int KV>
 struct Smem {

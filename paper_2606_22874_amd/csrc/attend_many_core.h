@@ -99,26 +99,15 @@ struct Copy {
   }
 };
 
-// The same of an 8-bit cache, in two steps: thread i of the 4 waves fetches the 16 codes of
+// The same of an 8-bit cache, in two steps: thread i of the 4 waves loads the 16 codes of
 // chunk i % CH of rows i / CH + RW u, which are on their way behind a softmax, and then
-// stores them as two chunks of elements.  They wait in registers, or (STAGE, where the
-// kernel has none left: with sinks) in a place of the thread's own in LDS, 3 % slower: the
-// wait for the copy, one more read and the stores then follow each other before the
-// barrier.  (Stored before the softmax instead of behind it: 3 % slower again.)
-template <int D, bool STAGE>
-struct Codes {
-  u32x4 raw[STAGE ? 1 : D / 64];
-  unsigned char* stage;                          // 64 D bytes
-  __device__ __forceinline__ u32x4 get(int u, int wave, int lane) const {
-    if constexpr (STAGE)
-      return *reinterpret_cast<const u32x4*>(stage + (4 * u + wave) * 1024 + lane * 16);
-    else
-      return raw[u];
-  }
-};
-template <class T, int D, bool IS_K, bool STAGE>
+// stores them as two chunks of elements.  (By way of a place of the thread's own in LDS,
+// which needs no registers meanwhile: 3 % slower, and with sinks, where some then go to
+// scratch memory, still 2 %: the wait for the copy, one more read and the stores follow each
+// other before the barrier.  Stored before the softmax instead of behind it: 3 % again.
+// Stored in an order that keeps eight lanes off each other's banks, by selects: 1.5 %.)
+template <class T, int D, bool IS_K>
 struct Widen {
-  typedef many::Codes<D, STAGE> Codes;
   static constexpr int CH = D / 16;              // 16-byte chunks of a row's codes
   static constexpr int RW = 256 / CH;            // rows of the 4 waves at once
   static constexpr int N = 64 / RW;
@@ -126,8 +115,8 @@ struct Widen {
     return RW * u + wave * (64 / CH) + lane / CH;
   }
   // (the rows of a wave's load lie in one group of 16 keys)
-  static __device__ __forceinline__ void load(const uint8_t* pool, const int* list, Codes& to,
-                                              int wave) {
+  static __device__ __forceinline__ void load(const uint8_t* pool, const int* list,
+                                              u32x4 (&raw)[N], int wave) {
     const int lane = fresh_lane();
 #pragma unroll
     for (int u = 0; u < N; ++u) {
@@ -135,16 +124,8 @@ struct Widen {
       const int at = __builtin_amdgcn_readfirstlane(list[group]);   // -1: a row of no use
       const uint8_t* src = pool + (int64_t)(at < 0 ? 0 : at) * D;
       const uint32_t off = (uint32_t)((row(u, wave, lane) & 15) * D + lane % CH * 16);
-      if constexpr (STAGE)
-        __builtin_amdgcn_global_load_lds(src + off, (lds_void*)(to.stage + (4 * u + wave) * 1024),
-                                         16, 0, 0);
-      else
-        to.raw[u] = *reinterpret_cast<const u32x4*>(src + off);
+      raw[u] = *reinterpret_cast<const u32x4*>(src + off);
     }
-  }
-  // Before store() or mend().
-  static __device__ __forceinline__ void wait() {
-    if constexpr (STAGE) __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
   }
   static __device__ __forceinline__ float scale(const uint16_t* scales, int u, int wave) {
     const uint32_t x = scales[(RW * u + wave * (64 / CH)) / 16];
@@ -154,14 +135,14 @@ struct Widen {
     const int pc = IS_K ? swz_k<D>(r, c) : swz_v<D>(r, c);
     *reinterpret_cast<u32x4*>(dst + r * (2 * D) + (pc << 4)) = x;
   }
-  static __device__ __forceinline__ void store(const Codes& from, const uint16_t* scales,
+  static __device__ __forceinline__ void store(const u32x4 (&raw)[N], const uint16_t* scales,
                                                unsigned char* dst, int wave) {
     const int lane = fresh_lane(), c = lane % CH * 2;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int r = row(u, wave, lane);
       const float s = scale(scales, u, wave);
-      const u32x4 x = from.get(u, wave, lane);
+      const u32x4& x = raw[u];
       put(dst, r, c, wide8<T>(x[0], x[1], s, s));
       put(dst, r, c + 1, wide8<T>(x[2], x[3], s, s));
     }
@@ -170,7 +151,7 @@ struct Widen {
   // (unseen) or that have no page, and for infinite and NaN elements of the others, of
   // which it tells.
   template <class F>
-  static __device__ __forceinline__ bool mend(const Codes& from, const int* list,
+  static __device__ __forceinline__ bool mend(const u32x4 (&raw)[N], const int* list,
                                               const uint16_t* scales, unsigned char* dst, int wave,
                                               F unseen) {
     const int lane = fresh_lane(), c = lane % CH * 2;
@@ -179,7 +160,7 @@ struct Widen {
     for (int u = 0; u < N; ++u) {
       const int r = row(u, wave, lane);
       const float s = scale(scales, u, wave);
-      const u32x4 y = from.get(u, wave, lane);
+      const u32x4& y = raw[u];
       const bool none = (list[r >> 4] < 0) | unseen(r);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -438,13 +419,12 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
   typedef Wave<T, D, CAP, BIAS, SINK> W;
   typedef Copy<D, true> CopyK;
   typedef Copy<D, false> CopyV;
-  typedef Widen<T, D, true, SINK> WidenK;
-  typedef Widen<T, D, false, SINK> WidenV;
+  typedef Widen<T, D, true> WidenK;
+  typedef Widen<T, D, false> WidenV;
   constexpr int kTile = 64 * D * 2, DT = D / 16;
   __shared__ __attribute__((aligned(16))) unsigned char sk0[kTile], sk1[kTile];
   __shared__ __attribute__((aligned(16))) unsigned char sv0[kTile], sv1[kTile];
   __shared__ int s_list[kListBlocks * 4];   // pool row of each 16-key group, -1 without a page
-  __shared__ __attribute__((aligned(16))) unsigned char s_codes[C8 && SINK ? 2 * 64 * D : 16];
   __shared__ uint16_t s_scale[C8 ? kListBlocks * 4 : 1];   // their scales: K, and V << 8
   __shared__ int s_lim[kWaves][SINK ? 6 : 4];
   __shared__ int s_missing, s_last, s_odd;
@@ -645,8 +625,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
       if (t < nb && active(t)) w.qk(k);
       __builtin_amdgcn_s_setprio(1);      // the softmax first, where both could go on
     };
-    Codes<D, SINK> codes;             // of keys or values, by the wave
-    codes.stage = s_codes + (C8 && SINK && second ? 64 * D : 0);
+    u32x4 raw[WidenK::N];             // codes of keys or of values, by the wave
     auto unseen = [&](int t) SPOT_INLINE {
       const int t0 = block(c0 + t) * 64;
       return [=](int r) SPOT_INLINE {
@@ -657,9 +636,8 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
     };
     if (second) {
       if constexpr (C8) {
-        WidenK::load(a.k8, s_list, codes, wave - kWaves / 2);
-        WidenK::wait();
-        WidenK::store(codes, s_scale, sk0, wave - kWaves / 2);
+        WidenK::load(a.k8, s_list, raw, wave - kWaves / 2);
+        WidenK::store(raw, s_scale, sk0, wave - kWaves / 2);
       } else {
         CopyK::issue(a.k, s_list, sk0, wave - kWaves / 2);
         wait_vm();
@@ -675,15 +653,14 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
       if (!second) {
         matrix_phase(t, kcur, vprev);
         if constexpr (C8) {
-          if (t < nb) WidenV::load(a.v8, s_list + 4 * t, codes, wave);
+          if (t < nb) WidenV::load(a.v8, s_list + 4 * t, raw, wave);
           if (t < nb && active(t)) vector_phase(t);
-          WidenV::wait();
           if (t < nb) {
             if (edge(t)) {
-              if (WidenV::mend(codes, s_list + 4 * t, s_scale + 4 * t, vcur, wave, unseen(t)))
+              if (WidenV::mend(raw, s_list + 4 * t, s_scale + 4 * t, vcur, wave, unseen(t)))
                 s_odd = 1;
             } else {
-              WidenV::store(codes, s_scale + 4 * t, vcur, wave);
+              WidenV::store(raw, s_scale + 4 * t, vcur, wave);
             }
           }
         } else {
@@ -696,10 +673,9 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
       } else {
         if constexpr (C8) {
           if (t + 1 < nb)
-            WidenK::load(a.k8, s_list + 4 * (t + 1), codes, wave - kWaves / 2);
+            WidenK::load(a.k8, s_list + 4 * (t + 1), raw, wave - kWaves / 2);
           if (t >= 1 && active(t - 1)) vector_phase(t - 1);
-          WidenK::wait();
-          if (t + 1 < nb) WidenK::store(codes, s_scale + 4 * (t + 1), knext, wave - kWaves / 2);
+            if (t + 1 < nb) WidenK::store(raw, s_scale + 4 * (t + 1), knext, wave - kWaves / 2);
         } else {
           if (t + 1 < nb) CopyK::issue(a.k, s_list + 4 * (t + 1), knext, wave - kWaves / 2);
           if (t >= 1 && active(t - 1)) vector_phase(t - 1);
