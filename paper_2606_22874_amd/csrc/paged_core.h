@@ -234,7 +234,7 @@ __device__ __forceinline__ int span_blocks(const Seq& q, int window, int sink, i
 // them), and a join, about a block for each part.
 // FIT > 0: so many workgroups run at once; where the parts are a few more, those that start
 // last run alone, so the blocks of a part grow to at most twice their number until all fit
-// (a mixed batch's 11 single sequences of up to 24000 tokens, 8-bit cache: 82 -> 69 us).
+// (a mixed batch's 11 single sequences of up to 24000 tokens, 8-bit cache: 82 -> 63 us).
 constexpr int kMaxJoin = 64;
 template <int TR, int ROUND, int FIT = 0>
 __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,

@@ -161,9 +161,9 @@ def test_attend_scales(d, dtype, kind):
 
 
 def test_every_code_and_scale():
-    """One token whose values are every code, under every scale that the element type has
-    room for: it is the output."""
-    for dtype, scales in ((BF, range(27, 247, 11)), (FP, range(103, 135))):
+    """One token whose values are every code, under every scale and to beyond what the element
+    type has room for: it is the output (rounded, or infinite)."""
+    for dtype, scales in ((BF, range(1, 255)), (FP, range(90, 150))):
         for d in (64, 128):
             q = torch.ones((1, 1, d), dtype=dtype, device=DEV)
             starts, length, table = i32([0, 1]), i32([1]), i32([[0]])
@@ -327,6 +327,32 @@ def test_attend_replayed(kind):
                 assert torch.equal(a.view(torch.int16), b.view(torch.int16))
             for a, b in ((lse, wl), (l2, wl)):
                 assert torch.equal(a.view(torch.int32), b.view(torch.int32))
+
+
+def test_pools_past_four_gibibytes():
+    """Codes, their rows and their scales beyond 2^32 bytes: appended and read there as in a
+    small pool."""
+    h, page, d = 8, 64, 128
+    n_pages = 2 ** 32 // (h * page * d) + 40
+    big = [torch.zeros((n_pages, h, page, d), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    bs = [torch.zeros((n_pages, h, page // 16), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    f = freqs(d // 2)
+    for n, length in (([1, 300], [200, 900]), ([1, 1], [33, 1000])):
+        a = Append(n[1], n, length, 2 * h, h, d, page, BF)
+        small = [x.clone() for x in (a.k8, a.v8, a.ks, a.vs)]
+        m = small[0].shape[0]
+        for x, y in zip(big + bs, small):
+            x[n_pages - m:] = y
+        out = []
+        for pools, table in ((small, a.table), (big + bs, torch.where(a.table < 0, -1,
+                                                                     a.table + n_pages - m))):
+            q = spot.rotary_append8(a.q, a.k, a.v, *pools, table, a.starts, a.len, f)
+            out.append((q, *spot.paged_attend8(q, *pools, table, a.starts, a.len, window=500,
+                                               n_sink=3)))
+        for x, y in zip(*out):
+            assert torch.equal(x, y)
+        for x, y in zip(big + bs, small):
+            assert torch.equal(x[n_pages - m:], y)
 
 
 # ------------------------------------------------------------------ appends
