@@ -70,7 +70,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a) {
   // (with sinks, comparisons are joined without branches: of a select behind short-circuit
   // ones and a uniform branch the compiler, ROCm 7.2, has kept the uniform part only)
   auto sees = [&](int t) { return ((t >= lo) & (t < hi)) | ((t >= from) & (t < end)); };
-  const Scores<CAP, BIAS, SINK> sc(a.rule, pt.q, tok, head);
+  Scores<CAP, BIAS, SINK> sc(a.rule, pt.q, tok, head);
   u32x4 qf[D / 32];
   const size_t qrow = (size_t)(pt.q.start + tok) * a.h_q + head;
 #pragma unroll

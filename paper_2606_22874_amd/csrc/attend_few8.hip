@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend8_few_kernel(AttendArgs 
   // behind short-circuit ones and a uniform branch the compiler, ROCm 7.2, has kept the
   // uniform part only)
   auto sees = [&](int t) { return ((t >= lo) & (t < hi)) | ((t >= from) & (t < end)); };
-  const Scores<CAP, BIAS, true> sc(a.rule, pt.q, tok, head);
+  Scores<CAP, BIAS, true> sc(a.rule, pt.q, tok, head);
   u32x4 qf[2 * KL];
   const size_t qrow = (size_t)(pt.q.start + tok) * a.h_q + head;
 #pragma unroll

@@ -197,7 +197,7 @@ struct SinkRule {
   int from, end;
 };
 
-template <class T, int D, bool CAP, bool BIAS, bool SINK>
+template <class T, int D, bool CAP, bool BIAS, bool SINK, bool QUICK>
 struct Wave {
   static constexpr int RB = D * 2, KS = D / 32, DT = D / 16;
   u32x4 qf[KS][2];            // Q^T as the B operand [dims][16 rows]
@@ -208,6 +208,7 @@ struct Wave {
   const RowRule* rows;        // the wave's 32
   const SinkRule* sinks;
   float mul, cap2;            // see Scores
+  bool hot;
   int G, r16;
 
   // S^T of one block; the K fragments of a step are read one step ahead.  The chunks'
@@ -300,10 +301,11 @@ struct Wave {
 #pragma unroll
       for (int qt = 0; qt < 2; ++qt) {
         const int lane = fresh_lane();
-        Scores<CAP, BIAS, SINK> sc;
+        Scores<CAP, BIAS, QUICK> sc;
         sc.mul = mul;
         sc.cap2 = cap2;
         sc.slope2 = 0.f;
+        sc.hot = hot;
         float ahead = 0.f;
         if (BIAS) {
           const RowRule u = rows[16 * qt + (lane & 15)];
@@ -319,6 +321,7 @@ struct Wave {
               s[qt][kt][i] = fmaf(m, fabsf(ahead - (float)(16 * kt + i)), s[qt][kt][i]);
         } else {
           sc(s[qt], ahead);
+          if (QUICK) hot = sc.hot;
         }
       }
     }
@@ -416,7 +419,7 @@ struct Wave {
 // 8-bit cache.
 template <class T, int D, bool CAP, bool BIAS, bool SINK, bool C8>
 __device__ __forceinline__ void attend_many(const AttendArgs& a) {
-  typedef Wave<T, D, CAP, BIAS, SINK> W;
+  typedef Wave<T, D, CAP, BIAS, SINK, SINK || C8> W;
   typedef Copy<D, true> CopyK;
   typedef Copy<D, false> CopyV;
   typedef Widen<T, D, true> WidenK;
@@ -461,6 +464,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
   };
   w.rows = s_rule + wave * 32;
   w.sinks = s_sink + (SINK ? wave * 32 : 0);
+  w.hot = false;
   int lo[2], hi[2], from[2], end[2];
 #pragma unroll
   for (int qt = 0; qt < 2; ++qt) {

@@ -124,22 +124,24 @@ __device__ __forceinline__ float tanh_any(float y) {
   return a < 0.5f ? tanh_near(y) : far;
 }
 
-// cap tanh(y) as cap - 2 cap / (1 + e^(2 y)), within 2.5e-7 cap: for scores beyond those of
-// tanh_near, half the operations of tanh_any.  A score of 16 bits' products is off by
-// 1e-5 and more by itself, so caps up to kQuickCap take it.
+// cap tanh(y) as cap - 2 cap / (1 + e^(2 y)), within 2.5e-7 cap, of y2 = 2 y log2(e): for
+// scores beyond those of tanh_near, half the operations of tanh_any.  A score of 16 bits'
+// products is off by 1e-5 and more by itself, so caps up to kQuickCap take it (900 tokens
+// over an 8-bit cache of 7500, cap 30, scores of both kinds: 259 us with tanh_any, 212).
 constexpr float kQuickCap = 64.f;
-__device__ __forceinline__ float capped(float y, float cap) {
-  const float e = __builtin_amdgcn_exp2f(y * (2.f * kLog2e));
-  return fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + e), cap);
+__device__ __forceinline__ float capped(float y2, float cap) {
+  return fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(y2)), cap);
 }
 
 // Scores in the log2 domain.  `ahead`: the row's position less the key's, in FP32 from
 // their difference as integers (positions themselves may need more than 24 bits).
-// QUICK: capped() where it is near enough.
+// QUICK: capped() where it is near enough, and from a block that needs it on in all of the
+// wave's (hot), which saves the look at each score's size.
 template <bool CAP, bool BIAS, bool QUICK = false>
 struct Scores {
   float mul, cap2, slope2;   // scale log2e, or scale / cap; cap log2e; slope log2e
   int p;                     // the row's position
+  bool hot = false;
   __device__ __forceinline__ Scores() {}
   __device__ __forceinline__ Scores(const Rule& u, const Seq& q, int i, int head) {
     mul = CAP ? u.scale / u.cap : u.scale * kLog2e;
@@ -156,7 +158,7 @@ struct Scores {
     for (int i = 0; i < 4; ++i) {
       const float y = s[i] * mul;
       float x = !CAP            ? y
-                : HOW == kQuick ? capped(y, cap2)
+                : HOW == kQuick ? capped(s[i] * (mul * (2.f * kLog2e)), cap2)
                                 : cap2 * (HOW == kNear ? tanh_near(y) : tanh_any(y));
       if (BIAS) x = fmaf(-slope2, fabsf(ahead - (float)i), x);
       s[i] = x;
@@ -165,19 +167,22 @@ struct Scores {
   }
   // N such quads, 16 keys from one to the next.
   template <int N>
-  __device__ __forceinline__ void operator()(f32x4 (&s)[N], float ahead) const {
+  __device__ __forceinline__ void operator()(f32x4 (&s)[N], float ahead) {
     if constexpr (CAP) {
-      float top = 0.f;
+      if (!QUICK || !hot) {
+        float top = 0.f;
 #pragma unroll
-      for (int e = 0; e < N; ++e)
+        for (int e = 0; e < N; ++e)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(s[e][i]));
-      if (!__ballot(top * fabsf(mul) > 0.5f)) {
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(s[e][i]));
+        if (!__ballot(top * fabsf(mul) > 0.5f)) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) s[e] = scaled<kNear>(s[e], ahead - 16.f * e);
-        return;
+          for (int e = 0; e < N; ++e) s[e] = scaled<kNear>(s[e], ahead - 16.f * e);
+          return;
+        }
+        hot = cap2 <= kQuickCap * kLog2e;
       }
-      if (QUICK && cap2 <= kQuickCap * kLog2e) {
+      if (QUICK && hot) {
 #pragma unroll
         for (int e = 0; e < N; ++e) s[e] = scaled<kQuick>(s[e], ahead - 16.f * e);
         return;

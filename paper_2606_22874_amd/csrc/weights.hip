@@ -124,7 +124,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weights_kernel(WeightArgs a) {
             ks + (16 * kt + r16) * RB + (((4 * kc + kg) ^ (r16 & (CH - 1))) << 4));
     for (int n = 0; n < steps; ++n) {
       if (n + 1 < steps) load(nxt);
-      const Scores<CAP, BIAS> sc(a.rule, q, cur.tok, g * G + cur.hd);
+      Scores<CAP, BIAS> sc(a.rule, q, cur.tok, g * G + cur.hd);
       const float mul = CAP || BIAS ? 1.f : sc.mul;
       const bool counts = cur.lse != -INFINITY;
       const bool part = __ballot(cur.lo > t0 || cur.hi < t0 + kKeys || !counts) != 0ull ||
