@@ -1,12 +1,16 @@
 """Attention over an 8-bit paged cache, attention with sinks, and appends to an 8-bit cache
 against their definitions in 64 bits (MI355X)."""
 import math
+import os
+import re
+import textwrap
 
 import pytest
 import torch
 
 import paged8ref as ref8
 import pagedref as ref
+from conftest import ROOT
 from paper_2606_22874_amd import spot
 from test_gpu_paged import BF, DEV, FP, SHAPES, Cache, i32, rule_of
 
@@ -613,6 +617,41 @@ def test_axes_in_place_gradient_and_replay():
 
 
 # ------------------------------------------------------------------ together
+def test_readme_loop():
+    """The README's loop on an 8-bit cache, a step of chunks and some of single tokens."""
+    with open(os.path.join(ROOT, "README.md")) as f:
+        text = f.read()
+    block = textwrap.dedent(re.search(r"(?m)^    k8, v8 = (?:.*\n)(?:(?:    .*)?\n)*", text).group(0))
+    assert "rotary_append8" in block and "paged_attend8" in block
+    g = torch.Generator(device=DEV).manual_seed(1)
+    h_q, h_kv, d, page, n_seq = 8, 2, 64, 16, 2
+    f, amp = spot.rope_frequencies(d, 1e6)
+    ns = dict(spot=spot, torch=torch, h_q=h_q, h_kv=h_kv, d=d, page=page, n_pages=2 * 8 * n_seq,
+              table=torch.arange(n_seq * 8, dtype=torch.int32, device=DEV).view(n_seq, 8), freq=f, amp=amp,
+              axis=(torch.arange(d // 2) % 3).to(torch.uint8), window=20, n_sink=4,
+              ws=spot.paged_workspace(n_seq, 90, h_q, h_kv, d), seq_len=i32([0, 0]))
+    checked = 0
+
+    def steps():
+        nonlocal checked
+        for new in [(50, 30), (1, 1), (1, 1), (7, 0), (1, 2)]:
+            x = torch.randn((sum(new), h_q + 2 * h_kv, d), device=DEV, generator=g).to(BF)
+            pos = torch.randint(0, 99, (sum(new), 3), device=DEV, generator=g, dtype=torch.int32)
+            start = i32([0, new[0], sum(new)])
+            yield *x.split([h_q, h_kv, h_kv], dim=1), start, i32(list(new)), pos
+            k = ref8.values(ns["k8"].view(torch.uint8), ns["k_scale"])
+            v = ref8.values(ns["v8"].view(torch.uint8), ns["v_scale"])
+            o, l, tol, ltol = ref8.attend(ns["q"], k, v, ns["table"], start, ns["seq_len"], d ** -0.5,
+                                          window=20, n_sink=4)
+            assert torch.all((ns["out"].double() - o).abs() <= tol)
+            assert torch.all((ns["lse"].double() - l).abs() <= ltol)
+            checked += 1
+
+    ns["steps"] = steps()
+    exec(block, ns)
+    assert checked == 5 and ns["seq_len"].tolist() == [60, 34]
+
+
 @pytest.mark.parametrize("dtype", [BF, FP])
 def test_serving_loop(dtype):
     """Prompts of text and images in two chunks, then single tokens, with a window and sinks:
