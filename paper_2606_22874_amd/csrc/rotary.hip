@@ -10,6 +10,8 @@
 // head.  8000 new tokens of 64 + 8 + 8 heads of 128, 314 MB read and written: 64 us,
 // 4.9 TB/s, what a copy reaches; a decode step of 8 tokens 6 us between replayed
 // launches, 4.5 of them the kernel: its chain of lengths, page, sines and stores.
+// With positions of several axes a pair's angle is pos[axis of the pair] f_i: three axes, 12001
+// tokens of 32 heads of 64, 98 MB, 20.6 us, 4.8 TB/s.
 #include "rotary_core.h"
 
 namespace spot {

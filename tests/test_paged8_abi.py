@@ -3,6 +3,7 @@ positions with several axes, what a row with sinks sees, and the built kernels' 
 (CPU: no kernel is launched)."""
 import ctypes
 import os
+import re
 import shutil
 import subprocess
 
@@ -10,7 +11,8 @@ import pytest
 import torch
 
 from paper_2606_22874_amd import build, spot
-from test_kernel_resources import READELF, kernels
+from test_kernel_resources import MARK, READELF, kernels
+from test_matrix_waits import OBJDUMP
 from test_paged_abi import FREQ, INF, NAN, P, call, lib, nz  # noqa: F401
 from test_wrappers import calls, i32, log, t  # noqa: F401
 
@@ -252,3 +254,34 @@ def test_kernels_registers_and_scratch(tmp_path):
             assert v["vgpr_count"] <= 256, (name, v)
             assert groups * v["group_segment_fixed_size"] <= 160 * 1024, (name, v)
             assert v["private_segment_fixed_size"] <= 48 * (part == "sinks8_many_kernel"), (name, v)
+
+
+EMPTY = re.compile(r"s_and_saveexec_b64 (s\[\d+:\d+\]), .*\n\s*s_or_b64 exec, exec, \1")
+
+
+@pytest.mark.skipif(not os.path.exists(OBJDUMP), reason="needs llvm-objdump")
+def test_no_region_has_lost_its_body(tmp_path):
+    """A conditional assignment of lanes that came out as a region without instructions: so
+    the compiler (ROCm 7.2) has dropped masks behind a uniform and short-circuit conditions."""
+    assert EMPTY.search("\ts_and_saveexec_b64 s[30:31], s[2:3]\n\ts_or_b64 exec, exec, s[30:31]\n")
+    if not os.path.exists(build.SO):
+        build.build()
+    with open(build.SO, "rb") as f:
+        data = f.read()
+    regions = 0
+    for m in re.finditer(re.escape(MARK), data):
+        at, nxt = data.find(b"\x7fELF", m.start()), data.find(MARK, m.start() + 1)
+        if at < 0 or (nxt > 0 and at > nxt):
+            continue
+        code = data[at:nxt if nxt > 0 else len(data)]
+        if b"paged" not in code:
+            continue
+        obj = tmp_path / "code.o"
+        obj.write_bytes(code)
+        listing = subprocess.run([OBJDUMP, "-d", "--no-show-raw-insn", "--no-leading-addr", str(obj)],
+                                 capture_output=True, text=True, check=True).stdout
+        listing = re.sub(r"\s*//.*", "", listing)
+        regions += listing.count("s_and_saveexec_b64")
+        found = EMPTY.search(listing)
+        assert not found, found.group(0)
+    assert regions > 1000
