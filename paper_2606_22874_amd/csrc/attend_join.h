@@ -28,7 +28,8 @@ template <int D, int KV>
 struct Smem {
   struct Merge {
     float ml[kWaves][kRows][2];
-    alignas(16) float o[kWaves][kRows][D];
+    // (rows 16 bytes apart in the banks: 16 of them are written at once)
+    alignas(16) float o[kWaves][kRows][D + 4];
   };
   struct Join {
     float weight[kMaxJoin][kRows];  // of part and row: 2^(m - M) / L
