@@ -743,8 +743,9 @@ spot_status spot_rotary_append(const void *q, int64_t q_stride, const void *k, i
 /*
  * spot_rotary_axes -- spot_rotary with positions of several axes (of images and video:
  * time, row, column; text has the same number on all; Section 2.1 and Appendix A for the
- * rotation): pair i takes its angle from pos[row, axis[i]] * freq[i].  Which pairs belong to which axis is the caller's (runs of
- * pairs, or the axes in turn).  Other arguments, numerics and errors as spot_rotary.
+ * rotation): pair i takes its angle from pos[row, axis[i]] * freq[i].  Which pairs belong
+ * to which axis is the caller's (runs of pairs, or the axes in turn).  Other arguments,
+ * numerics and errors as spot_rotary.
  *
  *  pos      device int32 [rows, n_axes]
  *  axis     host uint8 [rope_dim / 2], each below n_axes (read during the call; may be
@@ -768,9 +769,9 @@ spot_status spot_rotary_axes(const void *x, int64_t x_stride, const int32_t *pos
  *
  * spot_rotary_append8 -- spot_rotary_append into an 8-bit cache, with positions of one axis
  * or several (Section 2.1 and Appendix A for the rotation; Section 5.3 quantizes the
- * selector's cache, this the attention's).  The scale of 16 tokens and a head is the least power of two, from 2^-100 on,
- * with which no value of the new ones among them exceeds 448; a rotated pair (a, b) of a key
- * counts as |amp| (|a| + |b|), whatever its position.  Where earlier tokens of the 16 are in
+ * selector's cache, this the attention's).  The scale of 16 tokens and a head is the least
+ * power of two, from 2^-100 on, with which no value of the new ones among them exceeds 448; a
+ * rotated pair (a, b) of a key counts as |amp| (|a| + |b|), whatever its position.  Where earlier tokens of the 16 are in
  * the cache, the scale is at least theirs (as the scales hold it), and if it grows, their
  * codes are rounded again (to nearest even, as all are).  Values are rounded once, from
  * FP32.  Infinite values become the largest that the cache and the element type have (up to
@@ -781,8 +782,9 @@ spot_status spot_rotary_axes(const void *x, int64_t x_stride, const int32_t *pos
  *           not read); otherwise as spot_rotary_axes
  *  k_pages, v_pages    device uint8 [n_pages, h_kv, page_size, d], 16-byte aligned
  *  k_scale, v_scale    device uint8 [n_pages, h_kv, page_size / 16]
- * The rest as spot_rotary_append.  d 64 or 128 (SPOT_ERR_UNSUPPORTED).  Two sequences must
- * not write to one page in one call.
+ * The rest as spot_rotary_append.  d 64 or 128 (SPOT_ERR_UNSUPPORTED); rows + 2 ceil(h_kv / 4)
+ * min(rows, rows / 16 + 2 n_seq) < 2^24 (SPOT_ERR_SHAPE).  Two sequences must not write to
+ * one page in one call.
  */
 spot_status spot_rotary_append8(const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                                 const void *v, int64_t v_stride, int dtype, const int32_t *pos,
@@ -849,7 +851,7 @@ spot_status spot_paged_attend(const void *q, int dtype, const void *k_pages, con
 
 /*
  * spot_paged_attend_sinks -- spot_paged_attend with first tokens that stay visible behind a
- * window (Section 2.3 always keeps a sink prefix): a row also sees the tokens t, up to its own and below hi, of
+ * window (Section 2.3 always keeps a sink prefix): a row also sees the tokens t below hi of
  *     [max(0, first[row]), max(0, first[row]) + n_sink)
  * that lie before its window.  Bias and positions count as for any token.  n_sink >= 0
  * (SPOT_ERR_SHAPE); 0, or no window, is spot_paged_attend.
@@ -866,8 +868,8 @@ spot_status spot_paged_attend_sinks(const void *q, int dtype, const void *k_page
 /*
  * spot_paged_attend8 -- spot_paged_attend_sinks over an 8-bit cache (see
  * spot_rotary_append8; Section 3 for dense attention, Section 5.3 for a quantized cache):
- * attention over the elements code * 2^(scale - 127), with the same
- * arguments, workspace, numerics and errors, and
+ * attention over the elements code * 2^(scale - 127), with the same arguments, workspace,
+ * numerics and errors, and
  *
  *  k_pages, v_pages   device uint8 [n_pages, h_kv, page_size, d], 16-byte aligned
  *  k_scale, v_scale   device uint8 [n_pages, h_kv, page_size / 16]

@@ -14,10 +14,10 @@
 //   M = max m,  L = sum l 2^(m - M),  out = sum O 2^(m - M) / L.
 // The keys' bytes bound it: each is read once for all 16 rows (decode, four sequences of
 // 131072 tokens, 8 KV heads of 128: 334 us, 6.4 TB/s).  On one short sequence the chain of
-// lengths, pages, keys and join does: 700 tokens 9.8 us, two blocks of keys a part.
+// lengths, pages, keys and join does: 700 tokens 9.2 us, two blocks of keys a part.
 // With sinks a tile goes through two runs of blocks, numbered through (paged_map.h); its
-// masks look at both.  Eight sequences of 20000 .. 60000 tokens, window 4096 and 4 sinks: 32
-// us, 4.2 TB/s.
+// masks look at both.  Eight sequences of 20000 .. 60000 tokens, window 4096 and 4 sinks: 31
+// us, 4.3 TB/s.
 #include "attend_join.h"
 
 namespace spot {

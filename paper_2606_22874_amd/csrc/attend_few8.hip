@@ -13,8 +13,8 @@
 //                     scores' accumulators.
 // The codes' bytes bound it (2 D + 1/8 a key and KV head): decode, four sequences of 131072
 // tokens, 8 KV heads of 128, 177 us, 6.1 TB/s; 48 of up to 40000 with a window of 8192, heads
-// of 64, 77 us, 4.9 TB/s.  On one short sequence the chain of lengths, pages, keys and join
-// does: 600 tokens 10.2 us.
+// of 64, 76 us, 4.9 TB/s.  On one short sequence the chain of lengths, pages, keys and join
+// does: 600 tokens 9.6 us.
 #include "attend_join.h"
 #include "cache8.h"
 
