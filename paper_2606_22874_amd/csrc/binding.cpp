@@ -805,6 +805,127 @@ PyObject* paged_attend_sinks(Args a) {
   });
 }
 
+// Sizes that the wrappers read off the tensors: those of a tensor of `dims` dims, each an int,
+// or a reason for the Python path.
+struct Shape {
+  int n[4] = {0, 0, 0, 0};
+  const at::Tensor* t = nullptr;
+  Shape(Args& a, const Dev& d, int dims) {
+    if (!a.ok || !THPVariable_CheckExact(d.o)) {
+      a.ok = false;
+      return;
+    }
+    t = &THPVariable_Unpack(d.o);
+    if (t->dim() != dims) {
+      a.ok = false;
+      return;
+    }
+    for (int i = 0; i < dims; ++i) {
+      if (t->size(i) > INT32_MAX) a.ok = false;
+      n[i] = (int)t->size(i);
+    }
+  }
+  // Row stride of [rows, heads, d] whose heads lie one after the other.
+  int64_t stride(Args& a) const {
+    if (!a.ok) return 0;
+    if ((n[2] > 1 && t->stride(2) != 1) || (n[1] > 1 && t->stride(1) != n[2])) a.ok = false;
+    return n[0] > 1 ? t->stride(0) : (int64_t)n[1] * n[2];
+  }
+};
+
+// The axis of each frequency, and the number of axes of positions [*, axes]; without an axis
+// none.
+struct Axes {
+  int n = 0, rope = 0;
+  const uint8_t* of = nullptr;
+  const double* freq = nullptr;
+  Axes(Args& a, const Dev& axis, const Dev& pos, const Dev& freq_) {
+    if (!a.ok || !THPVariable_CheckExact(freq_.o)) {
+      a.ok = false;
+      return;
+    }
+    const int64_t half = THPVariable_Unpack(freq_.o).numel();
+    if (half > 1 << 20) a.ok = false;
+    if (!axis.none()) {
+      const Shape p(a, pos, 2);
+      if (!a.ok || p.n[1] < 1 || !THPVariable_CheckExact(axis.o) ||
+          THPVariable_Unpack(axis.o).numel() != half) {
+        a.ok = false;
+        return;
+      }
+      n = p.n[1];
+    }
+    rope = 2 * (int)half;
+    of = axis_of(a, axis, n, rope);
+    freq = freq_of(a, freq_, rope);
+  }
+};
+
+// rotary() with an axis and an output, sizes read here: x, pos, freq, amp, flags, out, stream, axis
+PyObject* rotary_axes_of(Args a) {
+  Dev x(a), pos(a), freq(a);
+  const float amp = a.real();
+  const int flags = a.integer();
+  Dev out(a);
+  void* st = a.stream();
+  Dev axis(a);
+  const Element el(a, x);
+  const Place place(a, x, pos, out);
+  const Shape sx(a, x, 3), so(a, out, 3);
+  const Axes ax(a, axis, pos, freq);
+  const int rows = sx.n[0], heads = sx.n[1], d = sx.n[2];
+  if (so.n[0] < rows || so.n[1] != heads || so.n[2] != d) a.ok = false;
+  const int64_t xs = sx.stride(a), os = so.stride(a);
+  void *xp = rows_of(a, x, el.bit, rows, xs, (big)heads * d),
+       *pp = pos.ptr(a, I32, (big)rows * ax.n),
+       *op = rows_of(a, out, el.bit, rows, os, (big)heads * d);
+  return finish(a, [&] {
+    return fn(kRotaryAxes, &spot_rotary_axes)(xp, xs, ip(pp), ax.n, ax.of, rows, heads, d, ax.rope,
+                                              ax.freq, amp, flags, el.dtype, op, os, st);
+  });
+}
+
+// rotary_append8() with an output, sizes read here: q, k, v, k_pages, v_pages, k_scale,
+// v_scale, page_table, seq_start, seq_len, freq, amp, flags, pos, q_out, stream, axis
+PyObject* rotary_append8_of(Args a) {
+  Dev q(a), k(a), v(a), kp(a), vp(a), ksc(a), vsc(a), tab(a), start(a), len(a), freq(a);
+  const float amp = a.real();
+  const int flags = a.integer();
+  Dev pos(a), qo(a);
+  void* st = a.stream();
+  Dev axis(a);
+  const Element el(a, q);
+  const Place place(a, q, k, v, pos, tab, start, len, qo, kp, vp, ksc, vsc);
+  const Shape sq(a, q, 3), sk(a, k, 3), sv(a, v, 3), pool(a, kp, 4), vpool(a, vp, 4), s1(a, ksc, 3),
+      s2(a, vsc, 3), table(a, tab, 2), n_len(a, len, 1), so(a, qo, 3);
+  const Axes ax(a, axis, pos, freq);
+  const int rows = sq.n[0], hq = sq.n[1], d = sq.n[2];
+  const int np = pool.n[0], hkv = pool.n[1], ps = pool.n[2], ns = n_len.n[0], mp = table.n[1];
+  for (const Shape* x : {&sk, &sv})
+    if (x->n[0] < rows || x->n[1] != hkv || x->n[2] != d) a.ok = false;
+  for (const Shape* x : {&s1, &s2})
+    if (x->n[0] < np || x->n[1] != hkv || x->n[2] != ps / 16) a.ok = false;
+  if (pool.n[3] != d || vpool.n[0] < np || vpool.n[1] != hkv || vpool.n[2] != ps ||
+      vpool.n[3] != d || so.n[0] < rows || so.n[1] != hq || so.n[2] != d)
+    a.ok = false;
+  const int64_t qs = sq.stride(a), ks = sk.stride(a), vs = sv.stride(a);
+  const big n_pool = (big)np * hkv * ps * d;
+  void *qp = rows_of(a, q, el.bit, rows, qs, (big)hq * d),
+       *kip = rows_of(a, k, el.bit, rows, ks, (big)hkv * d),
+       *vip = rows_of(a, v, el.bit, rows, vs, (big)hkv * d),
+       *pp = pos.opt(a, I32, (big)rows * (ax.n > 1 ? ax.n : 1)), *tp = tab.ptr(a, I32, (big)ns * mp),
+       *sp = start.ptr(a, I32, (big)ns + 1), *lp = len.ptr(a, I32, ns),
+       *qop = qo.ptr(a, el.bit, (big)rows * hq * d), *kpp = kp.ptr(a, U8 | F8, n_pool),
+       *vpp = vp.ptr(a, U8 | F8, n_pool), *ksp = ksc.ptr(a, U8 | E8, pool_scales(np, hkv, ps)),
+       *vsp = vsc.ptr(a, U8 | E8, pool_scales(np, hkv, ps));
+  return finish(a, [&] {
+    return fn(kRotaryAppend8, &spot_rotary_append8)(
+        qp, qs, kip, ks, vip, vs, el.dtype, ip(pp), ax.n, ax.of, ip(tp), np, ps, mp, ip(sp), ip(lp),
+        ns, rows, hq, hkv, d, ax.rope, ax.freq, amp, flags, qop, kpp, vpp,
+        static_cast<uint8_t*>(ksp), static_cast<uint8_t*>(vsp), st);
+  });
+}
+
 // q, k_pages, v_pages, k_scale, v_scale, page_table, n_pages, page_size, max_pages, seq_start, seq_len, n_seq, rows,
 // h_q, h_kv, d, sm_scale, softcap, slopes, window, n_sink, prefix, first, out, lse, ws, stream
 PyObject* paged_attend8(Args a) {
@@ -934,6 +1055,8 @@ PyMethodDef methods[] = {{"init", init, METH_VARARGS, nullptr},
                          SPOT_ENTRY(rotary_append8),
                          SPOT_ENTRY(paged_attend_sinks),
                          SPOT_ENTRY(paged_attend8),
+                         SPOT_ENTRY(rotary_axes_of),
+                         SPOT_ENTRY(rotary_append8_of),
                          SPOT_ENTRY(paged_fits),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods};

@@ -1195,13 +1195,18 @@ def rotary(x, pos, freq, amp=1.0, interleaved=False, inverse=False, out=None, st
     inverse: by the negative angles (also the gradient of the rotation).
     axis (uint8 host tensor, one for every frequency): pair i turns by pos[row, axis[i]] of
     pos [rows, axes]."""
+    flags = (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_INVERSE if inverse else 0)
+    if axis is not None and out is not None and _native is not None:
+        st = _native.rotary_axes_of(x, pos, freq, amp, flags, out, stream, axis)
+        if st is not None:
+            _check("spot_rotary_axes", st)
+            return out
     rows, heads, d = x.shape
     if out is None:
         with _on(stream, x.device):
             out = torch.empty((rows, heads, d), dtype=x.dtype, device=x.device)
     else:
         _fits(x, None, None, out, 0, None, None)
-    flags = (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_INVERSE if inverse else 0)
     n_axes = _axes_of(axis, pos, freq)
     if n_axes:
         spot_rotary_axes(x, _strides(x, "x"), pos, n_axes, axis, rows, heads, d, 2 * freq.numel(),
@@ -1241,6 +1246,14 @@ def rotary_append8(q, k, v, k_pages, v_pages, k_scale, v_scale, page_table, seq_
     page_size, d] (uint8 or float8_e4m3fn) and a power of two for every 16 tokens of a head,
     k_scale, v_scale [n_pages, h_kv, page_size / 16] (uint8 or float8_e8m0fnu).  axis and pos
     [rows, axes] as in rotary.  Returns q_out."""
+    flags = ROPE_INTERLEAVED if interleaved else 0
+    if q_out is not None and _native is not None:
+        st = _native.rotary_append8_of(q, k, v, k_pages, v_pages, k_scale, v_scale, page_table,
+                                       seq_start, seq_len, freq, amp, flags, pos, q_out, stream,
+                                       axis)
+        if st is not None:
+            _check("spot_rotary_append8", st)
+            return q_out
     rows, h_q, d = q.shape
     n_pages, h_kv, page, _ = k_pages.shape
     _fits(q, k, v, q_out, 0, None, None, k_pages, v_pages)
@@ -1251,8 +1264,8 @@ def rotary_append8(q, k, v, k_pages, v_pages, k_scale, v_scale, page_table, seq_
     spot_rotary_append8(q, _strides(q, "q"), k, _strides(k, "k"), v, _strides(v, "v"), pos,
                         _axes_of(axis, pos, freq), axis, page_table, n_pages, page,
                         page_table.shape[1], seq_start, seq_len, seq_len.shape[0], rows, h_q, h_kv,
-                        d, 2 * freq.numel(), freq, amp, ROPE_INTERLEAVED if interleaved else 0,
-                        q_out, k_pages, v_pages, k_scale, v_scale, stream)
+                        d, 2 * freq.numel(), freq, amp, flags, q_out, k_pages, v_pages, k_scale,
+                        v_scale, stream)
     return q_out
 
 

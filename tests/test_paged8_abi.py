@@ -130,6 +130,18 @@ def test_wrappers_refuse():
         spot.rotary_append8(*new)
 
 
+def test_native_leaves_the_rest_to_python():
+    """No arguments, too many, wrong kinds: None from every entry."""
+    spot.load()
+    cpu = torch.zeros(64, dtype=torch.int32)
+    for name in ("rotary_axes", "rotary_append8", "paged_attend_sinks", "paged_attend8",
+                 "rotary_axes_of", "rotary_append8_of"):
+        f = getattr(spot._native, name)
+        for n in (8, 16, 17, 20, 27, 29, 31, 40):
+            for args in ((), (None,) * n, (cpu,) * n, (1,) * n, ("bf16",) * n, (2 ** 70,) * n):
+                assert f(*args) is None, (name, args)
+
+
 def wrapped():
     rows, pool, scale, table = t(3, 4, 64), t(9, 2, 16, 64, dtype=torch.uint8), \
         t(9, 2, 1, dtype=torch.uint8), i32(2, 4)
