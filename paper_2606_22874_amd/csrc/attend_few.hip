@@ -116,7 +116,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a) {
     if (c0 > e0) __syncthreads();       // the list is done with
     for (int i = tid; i < 4 * nb; i += 64 * kWaves) {
       const int t = SINK ? block(c0 + i / 4) * 64 + i % 4 * kGroupKeys : c0 * 64 + i * kGroupKeys;
-      sm.list[i] = t < cap ? a.pages.row(pt.s, t, g, a.h_kv) : -1;
+      sm.list[i] = a.pages.row_below_cap(pt.s, t, g, a.h_kv);
     }
     __syncthreads();
     auto row_of = [&](int n) { return __builtin_amdgcn_readfirstlane(sm.list[4 * n + wave]); };

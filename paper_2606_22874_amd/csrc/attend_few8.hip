@@ -101,7 +101,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend8_few_kernel(AttendArgs 
     if (c0 > e0) __syncthreads();       // the list is done with
     for (int i = tid; i < 4 * nb; i += 64 * kWaves) {
       const int t = bl.at(c0 + i / 4) * 64 + i % 4 * kGroupKeys;
-      sm.list[i] = t < cap ? a.pages.row(pt.s, t, g, a.h_kv) : -1;
+      sm.list[i] = a.pages.row_below_cap(pt.s, t, g, a.h_kv);
     }
     __syncthreads();
     const int steps = (2 * nb - wave + kWaves - 1) / kWaves;    // half blocks wave, wave + 4, ..

@@ -570,7 +570,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
     __syncthreads();
     for (int i = tid; i < 4 * nb; i += 64 * kWaves) {
       const int t = SINK ? block(c0 + i / 4) * 64 + i % 4 * kGroupKeys : c0 * 64 + i * kGroupKeys;
-      const int r = t < cap ? a.pages.row(pt.s, t, g, a.h_kv) : -1;
+      const int r = a.pages.row_below_cap(pt.s, t, g, a.h_kv);
       s_list[i] = r;
       if constexpr (C8) {
         const int at = max(r, 0) / kGroupKeys;
@@ -723,8 +723,8 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
       const int tok = SINK ? block(v >> 6) * 64 + (v & 63) : v, t0 = tok & ~63;
       bool edge = t0 < FLO || t0 + 64 > FHI;
       for (int t = t0; t < t0 + 64; t += kGroupKeys)
-        edge = edge || t >= cap || a.pages.row(pe.s, t, g, a.h_kv) < 0;
-      const int at = a.pages.row(pe.s, tok & ~(kGroupKeys - 1), g, a.h_kv);
+        edge = edge || a.pages.row_below_cap(pe.s, t, g, a.h_kv) < 0;
+      const int at = a.pages.row_below_cap(pe.s, tok & ~(kGroupKeys - 1), g, a.h_kv);
       if (!edge || at < 0) continue;
       const size_t row = ((size_t)at + (tok & (kGroupKeys - 1))) * D;
       float k_scale = 1.f, v_scale = 1.f;

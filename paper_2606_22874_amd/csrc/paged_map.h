@@ -27,6 +27,11 @@ struct Pages {
     return (unsigned)id < (unsigned)n_pages ? (id * h_kv + g) * page_size + (t - p * page_size)
                                             : -1;
   }
+  // The same for any t: -1 too from cap() on.  A block of 64 keys may begin below cap(), a
+  // multiple of 16, and end behind it: who goes over whole blocks looks up this way.
+  __host__ __device__ __forceinline__ int row_below_cap(int s, int t, int g, int h_kv) const {
+    return t < cap() ? row(s, t, g, h_kv) : -1;
+  }
 };
 
 // The new tokens of sequence s: rows [start, start + n) of q.  len counts the

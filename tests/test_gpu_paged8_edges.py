@@ -1,0 +1,40 @@
+"""Attention over an 8-bit paged cache and with sinks where blocks, tables and arguments end
+(MI355X)."""
+import math
+
+import pytest
+import torch
+
+import paged8ref as ref8
+from test_gpu_paged import BF, DEV, FP, Cache
+from test_gpu_paged8 import KINDS, Kind
+
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("page,length", [(16, 330), (48, 330), (16, 336), (80, 395)])
+def test_nan_in_the_last_block_of_a_full_table(page, length, dtype, kind):
+    """The table has no place behind the last sequence's pages, and its room ends inside a
+    block of 64: a NaN value there, and one among the sinks, in the rows that see it only."""
+    for d in (64, 128):
+        for n in ([20, 90], [3, 2]):
+            c = Cache(page + length, n, [100, length], 4, 2, d, page, dtype, spare=0)
+            assert c.table.shape[1] * page % 64 != 0
+            kd = Kind(c, kind)
+            rule = dict(window=40, n_sink=3)
+            o, _, tol, _ = ref8.attend(c.q, kd.k, kd.v, c.table, c.starts, c.len, d ** -0.5, **rule)
+            p = torch.arange(length - n[1], length, device=DEV)
+            for t in (length - 2, 1):
+                v = kd.v8 if kind == "8" else c.v
+                at = (c.table[1, t // page].long(), 0, t % page, 3)
+                was = v[at].clone()
+                v[at] = 0xff if kind == "8" else math.nan
+                out, _ = kd.attend(**rule)
+                v[at] = was
+                bad = torch.zeros(out.shape, dtype=torch.bool, device=DEV)
+                bad[n[0]:, :2, 3] = ((t <= p) & ((t > p - 40) | (t < 3)))[:, None]
+                assert bad.any() and torch.all(torch.isnan(out[bad]))
+                assert torch.all(((out.double() - o).abs() <= tol)[~bad])
