@@ -723,7 +723,8 @@ PyObject* rotary_axes(Args a) {
   void* st = a.stream();
   const Element el(a, x);
   const Place place(a, x, pos, out);
-  void *xp = rows_of(a, x, el.bit, rows, xs, (big)heads * d), *pp = pos.ptr(a, I32, (big)rows * axes),
+  void *xp = rows_of(a, x, el.bit, rows, xs, (big)heads * d),
+       *pp = pos.ptr(a, I32, (big)rows * (axes > 1 ? axes : 1)),   // without axes one a row
        *op = rows_of(a, out, el.bit, rows, os, (big)heads * d);
   const double* fr = freq_of(a, freq, rope);
   const uint8_t* ax = axis_of(a, axis, axes, rope);

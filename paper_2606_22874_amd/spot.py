@@ -837,7 +837,7 @@ def spot_rotary_axes(x, x_stride, pos, n_axes, axis, rows, heads, d, rope_dim, f
             return _check("spot_rotary_axes", st)
     dt = _element(x, "x")
     _row_tensor(x, "x", x.dtype, rows, x_stride, heads * d)
-    _dev(pos, "pos", I32, rows * n_axes)
+    _dev(pos, "pos", I32, rows * max(n_axes, 1))
     _axis(axis, n_axes, rope_dim)
     _freq(freq, rope_dim)
     _row_tensor(out, "out", x.dtype, rows, out_stride, heads * d)

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import paged8ref as ref8
+from paper_2606_22874_amd import spot
 from test_gpu_paged import BF, DEV, FP, Cache
 from test_gpu_paged8 import KINDS, Kind
 
@@ -38,3 +39,20 @@ def test_nan_in_the_last_block_of_a_full_table(page, length, dtype, kind):
                 bad[n[0]:, :2, 3] = ((t <= p) & ((t > p - 40) | (t < 3)))[:, None]
                 assert bad.any() and torch.all(torch.isnan(out[bad]))
                 assert torch.all(((out.double() - o).abs() <= tol)[~bad])
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_rotation_without_axes_needs_a_position_a_row(native, monkeypatch):
+    """n_axes 0 is spot_rotary, and refuses what that refuses."""
+    spot.load()
+    if not native:
+        monkeypatch.setattr(spot, "_native", None)
+    x = torch.randn((6, 2, 64), device=DEV).to(BF)
+    out = torch.zeros_like(x)
+    pos = torch.arange(6, dtype=torch.int32, device=DEV)
+    freq = torch.full((32,), 0.3, dtype=torch.float64)
+    spot.spot_rotary_axes(x, 128, pos, 0, None, 6, 2, 64, 64, freq, 1.0, 0, out, 128)
+    assert torch.equal(out, spot.rotary(x, pos, freq))
+    for short in (pos[:0], pos[:5]):
+        with pytest.raises(ValueError, match="pos: . elements, need 6"):
+            spot.spot_rotary_axes(x, 128, short, 0, None, 6, 2, 64, 64, freq, 1.0, 0, out, 128)
