@@ -79,6 +79,10 @@ bool launch_many(int n_seq, int rows, int G, int64_t cap) {
   return (int64_t)rows * G > (n_seq == 1 ? few_rows(n_seq, cap) : 16 * (int64_t)n_seq);
 }
 
+// Sinks that a call has: without a window a row sees the first tokens anyway, and the call is
+// the one without sinks, its kernels and bits.
+int sinks(int window, int n_sink) { return window > 0 ? n_sink : 0; }
+
 // The launches of an attention over 16-bit pages, or 8-bit ones (a.k8).
 spot_status attend(AttendArgs a, int dtype, int d, void* ws, size_t ws_bytes, hipStream_t s) {
   const int G = a.h_q / a.h_kv;
@@ -349,7 +353,7 @@ spot_status spot_paged_attend_sinks(const void* q, int dtype, const void* k_page
   a.rows = rows;
   a.h_q = h_q;
   a.h_kv = h_kv;
-  a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first, n_sink};
+  a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first, sinks(window, n_sink)};
   a.out = out16(out);
   a.lse = lse;
   return attend(a, dtype, d, ws, ws_bytes, static_cast<hipStream_t>(stream));
@@ -400,7 +404,7 @@ spot_status spot_paged_attend8(const void* q, int dtype, const void* k_pages, co
   a.rows = rows;
   a.h_q = h_q;
   a.h_kv = h_kv;
-  a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first, n_sink};
+  a.rule = Rule{sm_scale, softcap, slopes, window, prefix, first, sinks(window, n_sink)};
   a.out = out16(out);
   a.lse = lse;
   return attend(a, dtype, d, ws, ws_bytes, static_cast<hipStream_t>(stream));

@@ -56,3 +56,17 @@ def test_rotation_without_axes_needs_a_position_a_row(native, monkeypatch):
     for short in (pos[:0], pos[:5]):
         with pytest.raises(ValueError, match="pos: . elements, need 6"):
             spot.spot_rotary_axes(x, 128, short, 0, None, 6, 2, 64, 64, freq, 1.0, 0, out, 128)
+
+
+@pytest.mark.parametrize("n,length", [([1, 1], [700, 3000]), ([300, 5], [900, 77]), ([200], [900])])
+@pytest.mark.parametrize("d,dtype", [(64, FP), (128, BF)])
+def test_sinks_without_a_window_are_none(n, length, d, dtype):
+    """Without a window the first tokens are visible anyway: with caps and a bias too the bits
+    of the call without sinks, over both kinds of cache."""
+    c = Cache(13, n, length, 8, 2, d, 16, dtype, scale=20.0)
+    for kind in KINDS:
+        kd = Kind(c, kind)
+        for rule in (dict(softcap=30.0), dict(softcap=50.0, slopes=c.slopes, first=c.firsts),
+                     dict(slopes=c.slopes, prefix=c.prefix), dict()):
+            a, b = kd.attend(**rule), kd.attend(n_sink=7, **rule)
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]), (kind, rule)
