@@ -128,7 +128,8 @@ __device__ __forceinline__ float tanh_any(float y) {
 // scores beyond those of tanh_near, half the operations of tanh_any.  A score of 16 bits'
 // products is off by 1e-5 and more by itself, so caps up to kQuickCap take it (900 tokens
 // over an 8-bit cache of 7500, cap 30, scores of both kinds: 259 us with tanh_any, 212).
-constexpr float kQuickCap = 64.f;
+// Of y2's factor, 2 log2(e) scale / cap: an infinite one would make NaN of a score of 0.
+constexpr float kQuickCap = 64.f, kQuickMul = 1e38f;
 __device__ __forceinline__ float capped(float y2, float cap) {
   return fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(y2)), cap);
 }
@@ -180,7 +181,7 @@ struct Scores {
           for (int e = 0; e < N; ++e) s[e] = scaled<kNear>(s[e], ahead - 16.f * e);
           return;
         }
-        hot = cap2 <= kQuickCap * kLog2e;
+        hot = (cap2 <= kQuickCap * kLog2e) & (fabsf(mul) <= kQuickMul);
       }
       if (QUICK && hot) {
 #pragma unroll

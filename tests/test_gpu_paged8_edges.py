@@ -70,3 +70,28 @@ def test_sinks_without_a_window_are_none(n, length, d, dtype):
                      dict(slopes=c.slopes, prefix=c.prefix), dict()):
             a, b = kd.attend(**rule), kd.attend(n_sink=7, **rule)
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]), (kind, rule)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("n", [[3, 1], [90, 40]])
+def test_caps_far_below_the_scale(n, dtype, kind):
+    """The largest ratio of scale and cap that is taken: a score of 0 stays 0 beside scores
+    that are at the cap."""
+    for d in (64, 128):
+        c = Cache(5, n, [400, 300], 4, 2, d, 16, dtype)
+        c.q[::3] = 0.0                               # rows whose scores are all 0
+        c.q[1::3, :, d // 2:] = 0.0
+        c.k[:, :, 3::5, :d // 2] = 0.0               # and tokens with a score of 0 among others
+        c.k[torch.isnan(c.v)] = math.nan
+        kd = Kind(c, kind)
+        for scale, cap in ((1.5e38, 1.0), (2e38, 0.625), (3e18, 1e-20)):
+            out, lse = kd.attend(sm_scale=scale, softcap=cap, window=250, n_sink=3)
+            fin = torch.isfinite(lse)
+            assert fin.all() and torch.isfinite(out).all(), (d, scale, cap)
+            # rows of zeros: the mean of the values seen, lse the logarithm of their number
+            o, l, tol, ltol = ref8.attend(c.q, kd.k, kd.v, c.table, c.starts, c.len, 0.0,
+                                          window=250, n_sink=3)
+            zero = torch.arange(c.q.shape[0], device=DEV) % 3 == 0
+            assert torch.all(((out.double() - o).abs() <= tol)[zero])
+            assert torch.all(((lse.double() - l).abs() <= ltol)[zero])
