@@ -178,9 +178,10 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a) {
     auto back = [&](int n, f32x4 s) {
       const int t0 = block(c0 + n) * 64 + wave * 16;
       f32x4 quad[1] = {s};
-      sc(quad, (float)(sc.p - (t0 + 4 * kg)));
+      const bool part = t0 < FLO || t0 + 16 > FHI || row_of(n) < 0;
+      sc(quad, (float)(sc.p - (t0 + 4 * kg)), !part);
       float x[4] = {quad[0][0], quad[0][1], quad[0][2], quad[0][3]};
-      if (t0 < FLO || t0 + 16 > FHI || row_of(n) < 0) {
+      if (part) {
         const bool page = row_of(n) >= 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {

@@ -191,8 +191,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend8_few_kernel(AttendArgs 
     };
     auto back = [&](int n, f32x4(&s)[2]) {
       const int hb = wave + kWaves * n, t0 = bl.at(c0 + hb / 2) * 64 + hb % 2 * kKeys;
-      sc(s, (float)(sc.p - (t0 + 4 * kg)));
-      if (t0 < FLO || t0 + kKeys > FHI || row_of(n, 0) < 0 || row_of(n, 1) < 0) {
+      const bool part = t0 < FLO || t0 + kKeys > FHI || row_of(n, 0) < 0 || row_of(n, 1) < 0;
+      sc(s, (float)(sc.p - (t0 + 4 * kg)), !part);
+      if (part) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const bool page = row_of(n, u) >= 0;

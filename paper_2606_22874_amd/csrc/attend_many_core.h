@@ -324,7 +324,7 @@ struct Wave {
             for (int i = 0; i < 4; ++i)
               s[qt][kt][i] = fmaf(m, fabsf(ahead - (float)(16 * kt + i)), s[qt][kt][i]);
         } else {
-          sc(s[qt], ahead);
+          sc(s[qt], ahead, !(below | above | (pages != 15u)));
           if (QUICK) hot = sc.hot;
         }
       }

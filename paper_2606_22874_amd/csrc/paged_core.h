@@ -137,7 +137,10 @@ __device__ __forceinline__ float capped(float y2, float cap) {
 // Scores in the log2 domain.  `ahead`: the row's position less the key's, in FP32 from
 // their difference as integers (positions themselves may need more than 24 bits).
 // QUICK: capped() where it is near enough, and from a block that needs it on in all of the
-// wave's (hot), which saves the look at each score's size.
+// wave's (hot), which saves the look at each score's size.  Which form is taken follows from
+// keys that the rows see: of blocks that are not `whole` (some row does not see all of it) the
+// scores include those of keys that hold anything, and such a block has tanh_near or tanh_any,
+// which agree to the bit where both do.
 template <bool CAP, bool BIAS, bool QUICK = false>
 struct Scores {
   float mul, cap2, slope2;   // scale log2e, or scale / cap; cap log2e; slope log2e
@@ -168,7 +171,7 @@ struct Scores {
   }
   // N such quads, 16 keys from one to the next.
   template <int N>
-  __device__ __forceinline__ void operator()(f32x4 (&s)[N], float ahead) {
+  __device__ __forceinline__ void operator()(f32x4 (&s)[N], float ahead, bool whole = false) {
     if constexpr (CAP) {
       if (!QUICK || !hot) {
         float top = 0.f;
@@ -176,12 +179,12 @@ struct Scores {
         for (int e = 0; e < N; ++e)
 #pragma unroll
           for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(s[e][i]));
-        if (!__ballot(top * fabsf(mul) > 0.5f)) {
+        if (!__ballot(top * fabsf(mul) >= 0.5f)) {
 #pragma unroll
           for (int e = 0; e < N; ++e) s[e] = scaled<kNear>(s[e], ahead - 16.f * e);
           return;
         }
-        hot = (cap2 <= kQuickCap * kLog2e) & (fabsf(mul) <= kQuickMul);
+        hot = QUICK & whole & (cap2 <= kQuickCap * kLog2e) & (fabsf(mul) <= kQuickMul);
       }
       if (QUICK && hot) {
 #pragma unroll

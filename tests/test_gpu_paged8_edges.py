@@ -95,3 +95,75 @@ def test_caps_far_below_the_scale(n, dtype, kind):
             zero = torch.arange(c.q.shape[0], device=DEV) % 3 == 0
             assert torch.all(((out.double() - o).abs() <= tol)[zero])
             assert torch.all(((lse.double() - l).abs() <= ltol)[zero])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,length", [([1], [300]), ([3, 1], [700, 130]), ([90], [700]),
+                                      ([250, 70], [700, 330])])
+@pytest.mark.parametrize("d,dtype", [(64, FP), (128, BF)])
+def test_unseen_keys_leave_the_bits_alone(n, length, d, dtype, kind):
+    """Whatever lies in places that no row sees (behind a sequence's end, before its windows,
+    on pages of others in place of missing ones): the same bits, with caps too, for scores on
+    both sides of where a cap begins to bend them."""
+    rows = dict(window=100, n_sink=3)
+    for scale, cap in ((1.0, 30.0), (3.0, 50.0), (3.0, 20.0), (1.0, 100.0)):
+        got = []
+        for fill in (0.0, 200.0, math.nan):
+            c = Cache(17, n, length, 4, 2, d, 16, dtype, scale=scale)
+            # what the rows see: from the first window on, and the sinks
+            for s, (m, L) in enumerate(zip(n, length)):
+                t = torch.arange(3, L - m - 99, device=DEV)
+                for x in (c.k, c.v):
+                    x[c.table[s].long()[t // 16], :, t % 16] = math.nan
+            hidden = torch.isnan(c.k)
+            kd = Kind(c, kind)
+            if kind == "8":
+                for x in (kd.k8, kd.v8):
+                    x[hidden] = {0.0: 0, 200.0: 0x7e}.get(fill, 0x7f)     # 0, 448, NaN
+                for x in (kd.ks, kd.vs):
+                    x[x == 255] = 120 if fill == 0.0 else 140
+            else:
+                c.k[hidden] = c.v[hidden] = fill
+            got.append(kd.attend(softcap=cap, **rows))
+            got.append(kd.attend(softcap=cap, slopes=c.slopes, **rows))
+            t = c.table.clone()
+            t[0, 1] = -1                             # page 0 of the pool lies there, unseen
+            c.table = t
+            c.k[0], c.v[0] = (fill, fill) if hidden[0].all() else (c.k[0], c.v[0])
+            got.append(kd.attend(softcap=cap, **rows))
+        for i in range(3, 9):
+            a, b = got[i], got[i % 3]
+            assert torch.isfinite(a[1]).all()
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]), (scale, cap, i)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,length", [([2], [100]), ([150], [190])])
+@pytest.mark.parametrize("rule", [dict(), dict(window=20, n_sink=3), dict(window=20)])
+def test_unseen_keys_beside_scores_at_the_bend(n, length, rule, kind):
+    """Scores of exactly half a cap, between the two forms of the hyperbolic tangent."""
+    d = 64
+    c = Cache(19, n, length, 4, 2, d, 16, BF)
+    c.q.zero_()
+    c.q[:, :, 0] = 1.0
+    seen = ~torch.isnan(c.k)
+    c.k = torch.where(seen, 0.0, c.k)
+    c.k[..., 0] = torch.where(seen[..., 0], torch.where(c.v[..., 1] > 0, 16.0, -16.0).to(BF), math.nan)
+    got = []
+    for fill in (0.0, 256.0):
+        k, v = torch.where(seen, c.k, fill), torch.where(seen, c.v, fill)
+        kd = Kind(c, kind)
+        if kind == "8":
+            kd.k8 = torch.where(seen, kd.k8, 0 if fill == 0.0 else 0x7e)
+            kd.ks = torch.where(kd.ks == 255, 130, kd.ks.int()).to(torch.uint8)
+            got.append(kd.attend(softcap=32.0, sm_scale=1.0, **rule))
+        else:
+            got.append(spot.paged_attend(c.q, k, v, c.table, c.starts, c.len, sm_scale=1.0,
+                                         softcap=32.0, **rule))
+        if kind == "16":
+            got[-1] = (*got[-1], spot.paged_weights(c.q, got[-1][1], k, c.table, c.starts, c.len,
+                                                    sm_scale=1.0, softcap=32.0,
+                                                    window=rule.get("window", 0)))
+    assert torch.isfinite(got[0][1]).all()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
