@@ -835,12 +835,12 @@ struct Shape {
 };
 
 // The axis of each frequency, and the number of axes of positions [*, axes]; without an axis
-// none.
+// none, and positions that have axes are a reason for the Python path.
 struct Axes {
   int n = 0, rope = 0;
   const uint8_t* of = nullptr;
   const double* freq = nullptr;
-  Axes(Args& a, const Dev& axis, const Dev& pos, const Dev& freq_) {
+  Axes(Args& a, const Dev& axis, const Dev& pos, const Dev& freq_, int rows) {
     if (!a.ok || !THPVariable_CheckExact(freq_.o)) {
       a.ok = false;
       return;
@@ -855,6 +855,13 @@ struct Axes {
         return;
       }
       n = p.n[1];
+    } else if (!pos.none()) {
+      if (!THPVariable_CheckExact(pos.o)) {
+        a.ok = false;
+        return;
+      }
+      const at::Tensor& x = THPVariable_Unpack(pos.o);
+      if (x.dim() > 1 && rows > 0 && rows <= x.size(0) && x.size(0) < x.numel()) a.ok = false;
     }
     rope = 2 * (int)half;
     of = axis_of(a, axis, n, rope);
@@ -873,7 +880,7 @@ PyObject* rotary_axes_of(Args a) {
   const Element el(a, x);
   const Place place(a, x, pos, out);
   const Shape sx(a, x, 3), so(a, out, 3);
-  const Axes ax(a, axis, pos, freq);
+  const Axes ax(a, axis, pos, freq, sx.n[0]);
   const int rows = sx.n[0], heads = sx.n[1], d = sx.n[2];
   if (so.n[0] < rows || so.n[1] != heads || so.n[2] != d) a.ok = false;
   const int64_t xs = sx.stride(a), os = so.stride(a);
@@ -899,7 +906,7 @@ PyObject* rotary_append8_of(Args a) {
   const Place place(a, q, k, v, pos, tab, start, len, qo, kp, vp, ksc, vsc);
   const Shape sq(a, q, 3), sk(a, k, 3), sv(a, v, 3), pool(a, kp, 4), vpool(a, vp, 4), s1(a, ksc, 3),
       s2(a, vsc, 3), table(a, tab, 2), n_len(a, len, 1), so(a, qo, 3);
-  const Axes ax(a, axis, pos, freq);
+  const Axes ax(a, axis, pos, freq, sq.n[0]);
   const int rows = sq.n[0], hq = sq.n[1], d = sq.n[2];
   const int np = pool.n[0], hkv = pool.n[1], ps = pool.n[2], ns = n_len.n[0], mp = table.n[1];
   for (const Shape* x : {&sk, &sv})

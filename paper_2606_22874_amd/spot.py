@@ -1179,9 +1179,13 @@ def _strides(t, name):
     return row if rows > 1 else heads * d
 
 
-def _axes_of(axis, pos, freq):
-    """The number of axes of positions [rows, axes] with the axis of each pair."""
+def _axes_of(axis, pos, freq, rows):
+    """The number of axes of positions [rows, axes] with the axis of each pair.  Without an axis
+    there is one number a row, in any shape but that."""
     if axis is None:
+        if pos is not None and pos.dim() > 1 and 0 < rows <= pos.shape[0] < pos.numel():
+            raise ValueError(f"pos: shape {tuple(pos.shape)} for {rows} rows needs the axis of "
+                             "every frequency")
         return 0
     if pos is None or pos.dim() != 2 or axis.numel() != freq.numel():
         raise ValueError("axis: need pos [rows, axes] and an axis for every frequency")
@@ -1194,7 +1198,7 @@ def rotary(x, pos, freq, amp=1.0, interleaved=False, inverse=False, out=None, st
     2 len(freq) elements of each head, pairs (i, i + len(freq)) or neighbours.
     inverse: by the negative angles (also the gradient of the rotation).
     axis (uint8 host tensor, one for every frequency): pair i turns by pos[row, axis[i]] of
-    pos [rows, axes]."""
+    pos [rows, axes], which without it is refused."""
     flags = (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_INVERSE if inverse else 0)
     if axis is not None and out is not None and _native is not None:
         st = _native.rotary_axes_of(x, pos, freq, amp, flags, out, stream, axis)
@@ -1207,7 +1211,7 @@ def rotary(x, pos, freq, amp=1.0, interleaved=False, inverse=False, out=None, st
             out = torch.empty((rows, heads, d), dtype=x.dtype, device=x.device)
     else:
         _fits(x, None, None, out, 0, None, None)
-    n_axes = _axes_of(axis, pos, freq)
+    n_axes = _axes_of(axis, pos, freq, rows)
     if n_axes:
         spot_rotary_axes(x, _strides(x, "x"), pos, n_axes, axis, rows, heads, d, 2 * freq.numel(),
                          freq, amp, flags, out, _strides(out, "out"), stream)
@@ -1224,6 +1228,7 @@ def rotary_append(q, k, v, k_pages, v_pages, page_table, seq_start, seq_len, fre
     rows, h_q, d = q.shape
     n_pages, h_kv, page, _ = k_pages.shape
     _fits(q, k, v, q_out, 0, None, None, k_pages, v_pages)
+    _axes_of(None, pos, freq, rows)
     if q_out is None:
         with _on(stream, q.device):
             q_out = torch.empty((rows, h_q, d), dtype=q.dtype, device=q.device)
@@ -1262,7 +1267,7 @@ def rotary_append8(q, k, v, k_pages, v_pages, k_scale, v_scale, page_table, seq_
         with _on(stream, q.device):
             q_out = torch.empty((rows, h_q, d), dtype=q.dtype, device=q.device)
     spot_rotary_append8(q, _strides(q, "q"), k, _strides(k, "k"), v, _strides(v, "v"), pos,
-                        _axes_of(axis, pos, freq), axis, page_table, n_pages, page,
+                        _axes_of(axis, pos, freq, rows), axis, page_table, n_pages, page,
                         page_table.shape[1], seq_start, seq_len, seq_len.shape[0], rows, h_q, h_kv,
                         d, 2 * freq.numel(), freq, amp, flags, q_out, k_pages, v_pages, k_scale,
                         v_scale, stream)

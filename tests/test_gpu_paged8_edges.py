@@ -167,3 +167,24 @@ def test_unseen_keys_beside_scores_at_the_bend(n, length, rule, kind):
     assert torch.isfinite(got[0][1]).all()
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_append_refuses_positions_with_axes_without_an_axis(native, monkeypatch):
+    """Natively and in the checks behind that; nothing is written."""
+    spot.load()
+    if not native:
+        monkeypatch.setattr(spot, "_native", None)
+    x = torch.randn((3, 8, 64), device=DEV).to(BF)
+    q, k, v = x.split([4, 2, 2], dim=1)
+    pools = [torch.zeros((4, 2, 16, 64), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    pools += [torch.zeros((4, 2, 1), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    place = [torch.tensor(a, dtype=torch.int32, device=DEV) for a in ([[1, 2]], [0, 3], [3])]
+    freq, out = torch.full((32,), 0.3, dtype=torch.float64), torch.zeros((3, 4, 64), dtype=BF, device=DEV)
+    pos = torch.arange(9, dtype=torch.int32, device=DEV).view(3, 3)
+    with pytest.raises(ValueError, match="needs the axis"):
+        spot.rotary_append8(q, k, v, *pools, *place, freq, pos=pos, q_out=out)
+    assert all(torch.all(y == 0) for y in pools + [out])
+    for same in (pos[0].contiguous(), pos[:1], pos[0][:, None].contiguous()):
+        spot.rotary_append8(q, k, v, *pools, *place, freq, pos=same, q_out=out)
+        assert torch.equal(out, spot.rotary(q, pos[0].contiguous(), freq))
