@@ -192,8 +192,9 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a) {
             x[i] = -INFINITY;
         }
       }
-      float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) - T::kShift;
+      float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
       mx = lanes_max_xor32(lanes_max_xor16(mx));
+      mx = reference<T>(mx, mx - T::kShift);
       if (__ballot(mx > m_run + T::kLazy) != 0ull) {
         const float m_new = fmaxf(m_run, mx);
         const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);

@@ -213,6 +213,7 @@ struct Wave {
   const SinkRule* sinks;
   float mul, cap2;            // see Scores
   bool hot;
+  int* far;                   // set where a maximum lies beyond kFarScore
   int G, r16;
 
   // S^T of one block; the K fragments of a step are read one step ahead.  The chunks'
@@ -291,7 +292,8 @@ struct Wave {
 
   // Online softmax of the scores into pb.  below, above: some row does not see the
   // first or last keys of the block; pages: bit kt says that keys 16 kt .. are there.
-  // sunk: the first keys may be sinks.
+  // sunk: the first keys may be sinks.  EXACT: every scaled score is rounded.
+  template <bool EXACT>
   __device__ __forceinline__ void softmax(int t0, bool below, bool above, bool sunk,
                                           unsigned pages) {
     asm volatile("s_nop 15"
@@ -299,9 +301,9 @@ struct Wave {
                    "+v"(s[1][1]), "+v"(s[1][2]), "+v"(s[1][3]));   // see settle()
     // Without a cap a positive scale waits until the exponent (and the bias is taken in
     // its units): an operation less for each score.
-    const bool late = !CAP && mul > 1e-6f;
+    const bool late = !CAP && !EXACT && mul > 1e-6f;
     const float c = late ? mul : 1.f;
-    if (CAP || BIAS) {
+    if (CAP || BIAS || EXACT) {
 #pragma unroll
       for (int qt = 0; qt < 2; ++qt) {
         const int lane = fresh_lane();
@@ -367,6 +369,12 @@ struct Wave {
           if (!(pages >> kt & 1)) s[qt][kt] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
       }
     }
+    if constexpr (EXACT) {               // (not one operation with the subtraction below)
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) asm("" : "+v"(s[qt][kt]));
+    }
     float mt[2];
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
@@ -379,11 +387,17 @@ struct Wave {
       mx = fmaxf(fmaxf(mx, s[qt][2][3]), s[qt][3][0]);
       mx = fmaxf(fmaxf(mx, s[qt][3][1]), s[qt][3][2]);
       mx = fmaxf(mx, s[qt][3][3]);
-      mt[qt] = lanes_max_xor16(lanes_max_xor32(mx)) * c - T::kShift;
+      mx = lanes_max_xor16(lanes_max_xor32(mx));
+      mt[qt] = EXACT || CAP ? reference<T>(mx, mx - T::kShift) : mx * c - T::kShift;
     }
     // The reference maximum moves only when a column's grows by more than kLazy, so
     // that most blocks leave O and l as they are.
     if (__ballot(mt[0] > m_run[0] + T::kLazy || mt[1] > m_run[1] + T::kLazy)) {
+      if constexpr (!CAP && !EXACT) {
+        const float big = fmaxf(mt[0] == -INFINITY ? 0.f : fabsf(mt[0]),
+                                mt[1] == -INFINITY ? 0.f : fabsf(mt[1]));
+        if (big > kFarScore) *far = 1;
+      }
 #pragma unroll
       for (int qt = 0; qt < 2; ++qt) {
         const float m_new = fmaxf(m_run[qt], mt[qt]);
@@ -434,7 +448,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
   __shared__ int s_list[kListBlocks * 4];   // pool row of each 16-key group, -1 without a page
   __shared__ uint16_t s_scale[C8 ? kListBlocks * 4 : 1];   // their scales: K, and V << 8
   __shared__ int s_lim[kWaves][SINK ? 6 : 4];
-  __shared__ int s_missing, s_last, s_odd;
+  __shared__ int s_missing, s_last, s_odd, s_far;
   __shared__ float s_join[kRows][2];
   __shared__ RowRule s_rule[kRows];
   __shared__ SinkRule s_sink[SINK ? kRows : 1];
@@ -449,7 +463,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
                                             SINK ? a.rule.sink : 0, cap, a.from, a.to);
     if (lane == 0) {
       s_part = p;
-      s_odd = 0;
+      s_odd = s_far = 0;
     }
   }
   __syncthreads();
@@ -469,6 +483,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
   w.rows = s_rule + wave * 32;
   w.sinks = s_sink + (SINK ? wave * 32 : 0);
   w.hot = false;
+  w.far = &s_far;
   int lo[2], hi[2], from[2], end[2];
 #pragma unroll
   for (int qt = 0; qt < 2; ++qt) {
@@ -563,141 +578,163 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
   const int e0 = min(b0 + pt.split * share, b1), e1 = min(e0 + share, b1);
   const bool second = wave >= kWaves / 2;
 
-  for (int c0 = e0; c0 < e1; c0 += kListBlocks) {
-    const int nb = min(kListBlocks, e1 - c0);
-    __syncthreads();                   // the list and the buffers are done with
-    if (tid == 0) s_missing = 0;
-    __syncthreads();
-    for (int i = tid; i < 4 * nb; i += 64 * kWaves) {
-      const int t = SINK ? block(c0 + i / 4) * 64 + i % 4 * kGroupKeys : c0 * 64 + i * kGroupKeys;
-      const int r = a.pages.row_below_cap(pt.s, t, g, a.h_kv);
-      s_list[i] = r;
-      if constexpr (C8) {
-        const int at = max(r, 0) / kGroupKeys;
-        s_scale[i] = (uint16_t)(a.k_scale[at] | a.v_scale[at] << 8);
-      }
-      if (r < 0) s_missing = 1;
-    }
-    __syncthreads();
-    const bool missing = __builtin_amdgcn_readfirstlane(s_missing) != 0;
-    auto pages_of = [&](int t) SPOT_INLINE -> unsigned {     // bit kt: the keys 16 kt .. are there
-      if (!missing) return 15u;
-      unsigned m = 0;
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt) m |= s_list[4 * t + kt] >= 0 ? 1u << kt : 0u;
-      return __builtin_amdgcn_readfirstlane(m);
-    };
-    // Blocks that some row of the workgroup sees in part only.
-    auto edge = [&](int t) SPOT_INLINE {
-      const int t0 = block(c0 + t) * 64;
-      return t0 < FLO || t0 + 64 > FHI || pages_of(t) != 15u;
-    };
-    auto active = [&](int t) SPOT_INLINE {
-      const int t0 = block(c0 + t) * 64;
-      return (t0 < w_hi && t0 + 64 > w_lo) || (SINK && t0 < ws_hi && t0 + 64 > ws_lo);
-    };
-    auto vector_phase = [&](int t) SPOT_INLINE {
-      const int t0 = block(c0 + t) * 64;
-      const unsigned pages = pages_of(t);
-      w.softmax(t0, t0 < all_lo, t0 + 64 > all_hi, SINK && t0 < ws_hi, pages);
-    };
-    // Values that no row sees become zero (they may be infinite or NaN, and meet the
-    // probability 0).  So do infinite and NaN elements of the others, which not every
-    // row sees: those that see them get theirs after the loop.  Each lane looks at
-    // what it copied itself.
-    auto mend = [&](int t, unsigned char* v) SPOT_INLINE {
-      const int t0 = block(c0 + t) * 64;
-      const unsigned pages = pages_of(t);
-      const int lane = fresh_lane();
-#pragma unroll 1
-      for (int u = 0; u < CopyV::N; ++u) {
-        const int r = CopyV::row(u, wave, lane), tok = t0 + r;
-        u32x4* at = reinterpret_cast<u32x4*>(v + (4 * u + wave) * 1024 + lane * 16);
-        if (((tok < LO || tok >= HI) && !(SINK && tok >= SLO && tok < SHI)) ||
-            !(pages >> (r >> 4) & 1)) {
-          *at = u32x4{0u, 0u, 0u, 0u};
-        } else {
-          u32x4 x = *at;
-          if (odd2<T>(x[0]) || odd2<T>(x[1]) || odd2<T>(x[2]) || odd2<T>(x[3])) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = clean2<T>(x[e]);
-            *at = x;
-            s_odd = 1;
-          }
-        }
-      }
-    };
-    auto matrix_phase = [&](int t, const unsigned char* k, const unsigned char* v) SPOT_INLINE {
-      __builtin_amdgcn_s_setprio(0);
-      if (t >= 1 && active(t - 1)) w.pv(v);
-      if (t < nb && active(t)) w.qk(k);
-      __builtin_amdgcn_s_setprio(1);      // the softmax first, where both could go on
-    };
-    u32x4 raw[WidenK::N];             // codes of keys or of values, by the wave
-    auto unseen = [&](int t) SPOT_INLINE {
-      const int t0 = block(c0 + t) * 64;
-      return [=](int r) SPOT_INLINE {
-        const int tok = t0 + r;
-        const bool main = (tok >= s_see[0]) & (tok < s_see[1]);
-        return !(SINK ? main | ((tok >= s_see[2]) & (tok < s_see[3])) : main);
-      };
-    };
-    if (second) {
-      if constexpr (C8) {
-        WidenK::load(a.k8, s_list, raw, wave - kWaves / 2);
-        WidenK::store(raw, s_scale, sk0, wave - kWaves / 2);
-      } else {
-        CopyK::issue(a.k, s_list, sk0, wave - kWaves / 2);
-        wait_vm();
-      }
-    }
-    lds_barrier();
-    auto period = [&](auto parity, int t) SPOT_INLINE {
-      constexpr int P = decltype(parity)::value;     // t % 2
-      unsigned char* const kcur = P ? sk1 : sk0;
-      unsigned char* const knext = P ? sk0 : sk1;
-      unsigned char* const vcur = P ? sv1 : sv0;
-      unsigned char* const vprev = P ? sv0 : sv1;
-      if (!second) {
-        matrix_phase(t, kcur, vprev);
+  auto go = [&](auto exact) SPOT_INLINE {
+    constexpr bool EXACT = decltype(exact)::value;
+    for (int c0 = e0; c0 < e1; c0 += kListBlocks) {
+      const int nb = min(kListBlocks, e1 - c0);
+      __syncthreads();                   // the list and the buffers are done with
+      if (tid == 0) s_missing = 0;
+      __syncthreads();
+      for (int i = tid; i < 4 * nb; i += 64 * kWaves) {
+        const int t = SINK ? block(c0 + i / 4) * 64 + i % 4 * kGroupKeys : c0 * 64 + i * kGroupKeys;
+        const int r = a.pages.row_below_cap(pt.s, t, g, a.h_kv);
+        s_list[i] = r;
         if constexpr (C8) {
-          if (t < nb) WidenV::load(a.v8, s_list + 4 * t, raw, wave);
-          if (t < nb && active(t)) vector_phase(t);
-          if (t < nb) {
-            if (edge(t)) {
-              if (WidenV::mend(raw, s_list + 4 * t, s_scale + 4 * t, vcur, wave, unseen(t)))
-                s_odd = 1;
-            } else {
-              WidenV::store(raw, s_scale + 4 * t, vcur, wave);
+          const int at = max(r, 0) / kGroupKeys;
+          s_scale[i] = (uint16_t)(a.k_scale[at] | a.v_scale[at] << 8);
+        }
+        if (r < 0) s_missing = 1;
+      }
+      __syncthreads();
+      const bool missing = __builtin_amdgcn_readfirstlane(s_missing) != 0;
+      auto pages_of = [&](int t) SPOT_INLINE -> unsigned {     // bit kt: the keys 16 kt .. are there
+        if (!missing) return 15u;
+        unsigned m = 0;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) m |= s_list[4 * t + kt] >= 0 ? 1u << kt : 0u;
+        return __builtin_amdgcn_readfirstlane(m);
+      };
+      // Blocks that some row of the workgroup sees in part only.
+      auto edge = [&](int t) SPOT_INLINE {
+        const int t0 = block(c0 + t) * 64;
+        return t0 < FLO || t0 + 64 > FHI || pages_of(t) != 15u;
+      };
+      auto active = [&](int t) SPOT_INLINE {
+        const int t0 = block(c0 + t) * 64;
+        return (t0 < w_hi && t0 + 64 > w_lo) || (SINK && t0 < ws_hi && t0 + 64 > ws_lo);
+      };
+      auto vector_phase = [&](int t) SPOT_INLINE {
+        const int t0 = block(c0 + t) * 64;
+        const unsigned pages = pages_of(t);
+        w.template softmax<EXACT>(t0, t0 < all_lo, t0 + 64 > all_hi, SINK && t0 < ws_hi, pages);
+      };
+      // Values that no row sees become zero (they may be infinite or NaN, and meet the
+      // probability 0).  So do infinite and NaN elements of the others, which not every
+      // row sees: those that see them get theirs after the loop.  Each lane looks at
+      // what it copied itself.
+      auto mend = [&](int t, unsigned char* v) SPOT_INLINE {
+        const int t0 = block(c0 + t) * 64;
+        const unsigned pages = pages_of(t);
+        const int lane = fresh_lane();
+#pragma unroll 1
+        for (int u = 0; u < CopyV::N; ++u) {
+          const int r = CopyV::row(u, wave, lane), tok = t0 + r;
+          u32x4* at = reinterpret_cast<u32x4*>(v + (4 * u + wave) * 1024 + lane * 16);
+          if (((tok < LO || tok >= HI) && !(SINK && tok >= SLO && tok < SHI)) ||
+              !(pages >> (r >> 4) & 1)) {
+            *at = u32x4{0u, 0u, 0u, 0u};
+          } else {
+            u32x4 x = *at;
+            if (odd2<T>(x[0]) || odd2<T>(x[1]) || odd2<T>(x[2]) || odd2<T>(x[3])) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[e] = clean2<T>(x[e]);
+              *at = x;
+              s_odd = 1;
             }
           }
-        } else {
-          if (t < nb) CopyV::issue(a.v, s_list + 4 * t, vcur, wave);
-          if (t < nb && active(t)) vector_phase(t);
-          wait_vm();
-          if (t < nb && edge(t)) mend(t, vcur);
         }
-        lds_barrier();
-      } else {
+      };
+      auto matrix_phase = [&](int t, const unsigned char* k, const unsigned char* v) SPOT_INLINE {
+        __builtin_amdgcn_s_setprio(0);
+        if (t >= 1 && active(t - 1)) w.pv(v);
+        if (t < nb && active(t)) w.qk(k);
+        __builtin_amdgcn_s_setprio(1);      // the softmax first, where both could go on
+      };
+      u32x4 raw[WidenK::N];             // codes of keys or of values, by the wave
+      auto unseen = [&](int t) SPOT_INLINE {
+        const int t0 = block(c0 + t) * 64;
+        return [=](int r) SPOT_INLINE {
+          const int tok = t0 + r;
+          const bool main = (tok >= s_see[0]) & (tok < s_see[1]);
+          return !(SINK ? main | ((tok >= s_see[2]) & (tok < s_see[3])) : main);
+        };
+      };
+      if (second) {
         if constexpr (C8) {
-          if (t + 1 < nb)
-            WidenK::load(a.k8, s_list + 4 * (t + 1), raw, wave - kWaves / 2);
-          if (t >= 1 && active(t - 1)) vector_phase(t - 1);
-            if (t + 1 < nb) WidenK::store(raw, s_scale + 4 * (t + 1), knext, wave - kWaves / 2);
+          WidenK::load(a.k8, s_list, raw, wave - kWaves / 2);
+          WidenK::store(raw, s_scale, sk0, wave - kWaves / 2);
         } else {
-          if (t + 1 < nb) CopyK::issue(a.k, s_list + 4 * (t + 1), knext, wave - kWaves / 2);
-          if (t >= 1 && active(t - 1)) vector_phase(t - 1);
+          CopyK::issue(a.k, s_list, sk0, wave - kWaves / 2);
           wait_vm();
         }
-        matrix_phase(t, kcur, vprev);
-        lds_barrier();
       }
-    };
-    for (int t = 0;; t += 2) {
-      period(std::integral_constant<int, 0>(), t);
-      if (t + 1 > nb) break;
-      period(std::integral_constant<int, 1>(), t + 1);
-      if (t + 2 > nb) break;
+      lds_barrier();
+      auto period = [&](auto parity, int t) SPOT_INLINE {
+        constexpr int P = decltype(parity)::value;     // t % 2
+        unsigned char* const kcur = P ? sk1 : sk0;
+        unsigned char* const knext = P ? sk0 : sk1;
+        unsigned char* const vcur = P ? sv1 : sv0;
+        unsigned char* const vprev = P ? sv0 : sv1;
+        if (!second) {
+          matrix_phase(t, kcur, vprev);
+          if constexpr (C8) {
+            if (t < nb) WidenV::load(a.v8, s_list + 4 * t, raw, wave);
+            if (t < nb && active(t)) vector_phase(t);
+            if (t < nb) {
+              if (edge(t)) {
+                if (WidenV::mend(raw, s_list + 4 * t, s_scale + 4 * t, vcur, wave, unseen(t)))
+                  s_odd = 1;
+              } else {
+                WidenV::store(raw, s_scale + 4 * t, vcur, wave);
+              }
+            }
+          } else {
+            if (t < nb) CopyV::issue(a.v, s_list + 4 * t, vcur, wave);
+            if (t < nb && active(t)) vector_phase(t);
+            wait_vm();
+            if (t < nb && edge(t)) mend(t, vcur);
+          }
+          lds_barrier();
+        } else {
+          if constexpr (C8) {
+            if (t + 1 < nb)
+              WidenK::load(a.k8, s_list + 4 * (t + 1), raw, wave - kWaves / 2);
+            if (t >= 1 && active(t - 1)) vector_phase(t - 1);
+              if (t + 1 < nb) WidenK::store(raw, s_scale + 4 * (t + 1), knext, wave - kWaves / 2);
+          } else {
+            if (t + 1 < nb) CopyK::issue(a.k, s_list + 4 * (t + 1), knext, wave - kWaves / 2);
+            if (t >= 1 && active(t - 1)) vector_phase(t - 1);
+            wait_vm();
+          }
+          matrix_phase(t, kcur, vprev);
+          lds_barrier();
+        }
+      };
+      for (int t = 0;; t += 2) {
+        period(std::integral_constant<int, 0>(), t);
+        if (t + 1 > nb) break;
+        period(std::integral_constant<int, 1>(), t + 1);
+        if (t + 2 > nb) break;
+      }
+    }
+  };
+  go(std::false_type());
+  // The exact product of a score and its scale less the maximum's, which is rounded, is off by
+  // half of that one's last place: beyond 2^24 more than a probability bears.  A tile that has
+  // met such scores is gone through once more, each score rounded as the maximum is.  (Of other
+  // calls that takes nothing over a 16-bit cache, 1.6 % over an 8-bit one; in the one loop, by a
+  // branch of its own or beside the maxima's growth, it took 1 .. 8 %.)
+  if constexpr (!CAP) {
+    __syncthreads();
+    if (__builtin_amdgcn_readfirstlane(s_far)) {
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) w.o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        w.m_run[qt] = -INFINITY;
+        w.l_run[qt] = 0.f;
+      }
+      go(std::true_type());
     }
   }
 

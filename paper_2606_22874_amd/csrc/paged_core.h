@@ -75,6 +75,15 @@ struct Fp16 {
   static constexpr uint32_t kExponent = 0x7c00u;
 };
 
+// The reference for the largest score of a block: kShift below it (`shifted`), in the log2
+// domain.  Beyond 2^24 scores are whole numbers of more than 2, and the shift, rounded with
+// them, could become 16: with kLazy's slack more than FP16 holds.  There it is left out.
+constexpr float kFarScore = 16777216.f;
+template <class T>
+__device__ __forceinline__ float reference(float top, float shifted) {
+  return T::kShift == 0.f || fabsf(top) > kFarScore ? top : shifted;
+}
+
 // Wait states between matrix instructions and the ordinary ones that read their
 // results: 8 are needed (4 passes).  Where a branch lies between, the compiler (ROCm 7.2)
 // counts them along one path only, and around a block that is skipped 1 to 3 were left:

@@ -188,3 +188,83 @@ def test_append_refuses_positions_with_axes_without_an_axis(native, monkeypatch)
     for same in (pos[0].contiguous(), pos[:1], pos[0][:, None].contiguous()):
         spot.rotary_append8(q, k, v, *pools, *place, freq, pos=same, q_out=out)
         assert torch.equal(out, spot.rotary(q, pos[0].contiguous(), freq))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,length", [([3], [100]), ([150], [190]), ([90, 2], [300, 80])])
+@pytest.mark.parametrize("dtype,size", [(BF, 3e4), (BF, 1e6), (BF, 1e15), (FP, 3e4)])
+def test_scores_of_any_size(n, length, dtype, size, kind):
+    """Scores far beyond 2^24, where a scaled score is off by more than the exponent's unit: a
+    row of one token is its value, equal scores give the mean, and the largest of scores that
+    lie apart its token's value."""
+    d = 64
+    for sign in (1.0, -1.0):
+        c = Cache(23, n, length, 4, 2, d, 16, dtype)
+        c.q.zero_()
+        c.q[:, :, 0] = size
+        seen = ~torch.isnan(c.k)
+        c.k = torch.where(seen, 0.0, c.k)
+        c.k[..., 0] = torch.where(seen[..., 0], sign * size, math.nan)
+        kd = Kind(c, kind)
+        u = torch.finfo(dtype).eps / 2
+        for rule in (dict(), dict(slopes=c.slopes * 0.0), dict(softcap=1e9)):
+            for more in (dict(window=1), dict(window=1, n_sink=1), dict(), dict(window=40)):
+                out, lse = kd.attend(sm_scale=0.3, **rule, **more)
+                assert torch.isfinite(out).all() and torch.isfinite(lse).all(), (rule, more)
+                o, l, _, _ = ref8.attend(c.q, kd.k, kd.v, c.table, c.starts, c.len, 0.3,
+                                         cap=rule.get("softcap", 0.0), **more)
+                # scores that are equal stay equal: the mean, by probabilities that are one
+                # rounded number (half a step each), and the output's rounding
+                A, _, _, _ = ref8.attend(c.q, kd.k, kd.v.abs(), c.table, c.starts, c.len, 0.3,
+                                         cap=rule.get("softcap", 0.0), **more)
+                seen_n = max(length)
+                assert torch.all((out.double() - o).abs() <= 2 * u * A + 4 * seen_n * 2.0 ** -24 * A)
+                # scores of 1e8 and more: a handful of roundings of one such number
+                assert torch.all((lse.double() - l).abs() <= 16 * 2.0 ** -24 * l.abs())
+        # one token of the largest score, far above
+        if sign > 0:
+            p = length[0] - n[0] - 1                 # seen by every row of sequence 0
+            page, off = c.table[0, p // 16].long(), p % 16
+            for x in (kd.k8, c.k) if kind == "8" else (c.k,):
+                if x is c.k:
+                    x[page, :, off, 0] = 2 * size if dtype == BF else 60000.0
+                else:
+                    x[page, :, off, 0] = 0x7e        # 448, the others 448 / 2 or less
+            if kind == "8":
+                kd.k = ref8.values(kd.k8, kd.ks)
+            out, lse = kd.attend(sm_scale=0.3)
+            v = kd.v[page, :, off].repeat_interleave(2, 0)[None]
+            assert torch.all((out[:n[0]].double() - v).abs() <= u * v.abs())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("n,length", [([3], [700]), ([150], [500]), ([90, 2], [300, 800])])
+def test_large_scores_that_grow_by_little(n, length, dtype, kind):
+    """Scores of every octave from 2^20 to 2^31 that differ in their last places and grow along
+    the keys: probabilities stay numbers, and the rows within their values."""
+    d = 64
+    c = Cache(29, n, length, 4, 2, d, 16, dtype)
+    c.q.zero_()
+    c.q[:, :, 0], c.q[:, :, 1] = 4096.0, 1.0
+    seen = ~torch.isnan(c.k)
+    for s, L in enumerate(length):
+        t = torch.arange(L, device=DEV)
+        row = torch.zeros((L, 2, d), device=DEV)
+        row[:, :, 0], row[:, :, 1] = 4096.0, (t * 440 // L)[:, None].float()
+        c.k[c.table[s].long()[t // 16], :, t % 16] = row.to(dtype)
+    kd = Kind(c, kind)
+    top = torch.where(seen, kd.v, 0.0).abs().amax((0, 2))          # [h_kv, d]
+    top = top.repeat_interleave(2, 0)[None] * (1 + 4 * torch.finfo(dtype).eps)
+    for sign in (1.0, -1.0):
+        for e in range(12):
+            scale = sign * 2.0 ** (e - 4) * 0.8
+            for rule in (dict(), dict(slopes=c.slopes), dict(window=90, n_sink=3)):
+                out, lse = kd.attend(sm_scale=scale, **rule)
+                assert torch.isfinite(out).all() and torch.isfinite(lse).all(), (scale, rule)
+                assert torch.all(out.double().abs() <= top), (scale, rule)
+                o, l, _, _ = ref8.attend(c.q, kd.k, kd.v, c.table, c.starts, c.len, scale, **rule)
+                # the score's rounding as a sum, as a multiple, in the log2 domain, a bias', and
+                # lse's own; up to log(length) of the spread of probabilities so far off
+                err = (lse.double() - l).abs()
+                assert torch.all(err <= 16 * 2.0 ** -24 * l.abs() + math.log(max(length)))
