@@ -771,12 +771,13 @@ spot_status spot_rotary_axes(const void *x, int64_t x_stride, const int32_t *pos
  * or several (Section 2.1 and Appendix A for the rotation; Section 5.3 quantizes the
  * selector's cache, this the attention's).  The scale of 16 tokens and a head is the least
  * power of two, from 2^-100 on, with which no value of the new ones among them exceeds 448; a
- * rotated pair (a, b) of a key counts as |amp| (|a| + |b|), whatever its position.  Where earlier tokens of the 16 are in
- * the cache, the scale is at least theirs (as the scales hold it), and if it grows, their
- * codes are rounded again (to nearest even, as all are).  Values are rounded once, from
- * FP32.  Infinite values become the largest that the cache and the element type have (up to
- * 448 2^(scale - 127); FP16: 61440), NaN stays NaN; neither, nor a pair whose sum is not
- * finite, counts for the scale.  Slots behind the last new token keep their codes.
+ * rotated pair (a, b) of a key counts as |amp| (|a| + |b|), whatever its position.  Where
+ * earlier tokens of the 16 are in the cache, the scale is at least theirs (as the scales hold
+ * it), and if it grows, their codes are rounded again (to nearest even, as all are).  Values
+ * are rounded once, from FP32.  Infinite values, and those beyond it, become the largest that
+ * the cache and the element type have (up to 448 2^(scale - 127); BF16: 240 2^120, FP16:
+ * 61440), NaN stays NaN; neither infinite values nor NaN, nor a pair whose sum is not finite,
+ * count for the scale.  Slots behind the last new token keep their codes.
  *
  *  pos, n_axes, axis   n_axes 0: pos [rows] or NULL as spot_rotary_append has it (axis is
  *           not read); otherwise as spot_rotary_axes
@@ -854,7 +855,8 @@ spot_status spot_paged_attend(const void *q, int dtype, const void *k_pages, con
  * window (Section 2.3 always keeps a sink prefix): a row also sees the tokens t below hi of
  *     [max(0, first[row]), max(0, first[row]) + n_sink)
  * that lie before its window.  Bias and positions count as for any token.  n_sink >= 0
- * (SPOT_ERR_SHAPE); 0, or no window, is spot_paged_attend.
+ * (SPOT_ERR_SHAPE); 0, or no window, is spot_paged_attend.  A softcap of at most 64 is within
+ * 4e-7 softcap (spot_paged_attend: 2e-7 of the capped score).
  */
 spot_status spot_paged_attend_sinks(const void *q, int dtype, const void *k_pages,
                                     const void *v_pages, const int32_t *page_table, int n_pages,
@@ -869,7 +871,7 @@ spot_status spot_paged_attend_sinks(const void *q, int dtype, const void *k_page
  * spot_paged_attend8 -- spot_paged_attend_sinks over an 8-bit cache (see
  * spot_rotary_append8; Section 3 for dense attention, Section 5.3 for a quantized cache):
  * attention over the elements code * 2^(scale - 127), with the same arguments, workspace,
- * numerics and errors, and
+ * numerics (with or without sinks) and errors, and
  *
  *  k_pages, v_pages   device uint8 [n_pages, h_kv, page_size, d], 16-byte aligned
  *  k_scale, v_scale   device uint8 [n_pages, h_kv, page_size / 16]
@@ -878,8 +880,8 @@ spot_status spot_paged_attend_sinks(const void *q, int dtype, const void *k_page
 spot_status spot_paged_attend8(const void *q, int dtype, const void *k_pages, const void *v_pages,
                                const uint8_t *k_scale, const uint8_t *v_scale,
                                const int32_t *page_table, int n_pages, int page_size, int max_pages,
-                               const int32_t *seq_start, const int32_t *seq_len, int n_seq, int rows,
-                               int h_q, int h_kv, int d, float sm_scale, float softcap,
+                               const int32_t *seq_start, const int32_t *seq_len, int n_seq,
+                               int rows, int h_q, int h_kv, int d, float sm_scale, float softcap,
                                const float *slopes, int window, int n_sink, const int32_t *prefix,
                                const int32_t *first, void *out, float *lse, void *ws,
                                size_t ws_bytes, void *stream);
@@ -892,14 +894,17 @@ spot_status spot_paged_attend8(const void *q, int dtype, const void *k_pages, co
  *                        + sum over rows i of s and heads h of g of exp(x_t - lse[row, h])
  * with x_t, the tokens a row sees and all arguments as in spot_paged_attend, whose lse
  * this takes (rows with lse = -inf add nothing).  Every t < max_pages * page_size is
- * written; a token that no row sees gets decay * acc.
+ * written; a token that no row sees gets decay * acc.  It knows no sinks and no 8-bit cache:
+ * with the lse of spot_paged_attend_sinks the first tokens before a window, which that call
+ * sees, get decay * acc all the same, and the others what they have beside them.
  *
  *  lse      device float [rows, h_q]
  *  acc      device float [n_seq, h_kv, max_pages * page_size] or NULL (0)
  *  decay    finite
  *  acc_out  device float, of acc's shape (output); may be acc itself
  *
- * FP32 sums in a fixed order (deterministic).  n_seq <= 65535
+ * FP32 sums in a fixed order (deterministic).  Of scores beyond 2^24 lse holds no fraction,
+ * so that their weights are no more than an order of magnitude.  n_seq <= 65535
  * (SPOT_ERR_UNSUPPORTED).
  */
 spot_status spot_paged_weights(const void *q, const float *lse, int dtype, const void *k_pages,

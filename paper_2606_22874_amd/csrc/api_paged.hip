@@ -106,7 +106,8 @@ spot_status attend(AttendArgs a, int dtype, int d, void* ws, size_t ws_bytes, hi
 }
 
 // Axes of the pairs: none (one position a row), or of n_axes.
-spot_status check_axes(int n_axes, const uint8_t* axis, const int32_t* pos, int rows, int rope_dim) {
+spot_status check_axes(int n_axes, const uint8_t* axis, const int32_t* pos, int rows,
+                       int rope_dim) {
   if (n_axes < 0 || n_axes > SPOT_ROPE_AXES) return SPOT_ERR_UNSUPPORTED;
   if (n_axes > 0) {
     if ((rope_dim > 0 && !axis) || (rows > 0 && !pos)) return SPOT_ERR_NULL;
@@ -375,8 +376,8 @@ spot_status spot_paged_attend(const void* q, int dtype, const void* k_pages, con
 spot_status spot_paged_attend8(const void* q, int dtype, const void* k_pages, const void* v_pages,
                                const uint8_t* k_scale, const uint8_t* v_scale,
                                const int32_t* page_table, int n_pages, int page_size, int max_pages,
-                               const int32_t* seq_start, const int32_t* seq_len, int n_seq, int rows,
-                               int h_q, int h_kv, int d, float sm_scale, float softcap,
+                               const int32_t* seq_start, const int32_t* seq_len, int n_seq,
+                               int rows, int h_q, int h_kv, int d, float sm_scale, float softcap,
                                const float* slopes, int window, int n_sink, const int32_t* prefix,
                                const int32_t* first, void* out, float* lse, void* ws,
                                size_t ws_bytes, void* stream) {

@@ -52,9 +52,10 @@ __device__ __forceinline__ Group find_group(const RotaryArgs& a, int unit) {
     Seq q = {0, 0, 0};
     if (base + lane < a.n_seq) q = sequence(a.seq_start, a.seq_len, base + lane, a.rows);
     // tokens at negative places are not there
-    const int first = max(q.len - q.n, 0), n = q.n > 0 && q.len > first
-                                                   ? (q.len - 1) / kGroupKeys - first / kGroupKeys + 1
-                                                   : 0;
+    const int first = max(q.len - q.n, 0);
+    const int n = q.n > 0 && q.len > first
+                      ? (q.len - 1) / kGroupKeys - first / kGroupKeys + 1
+                      : 0;
     const int incl = wave_incl_scan_i(n);
     const uint64_t hit = __ballot(unit >= at + incl - n && unit < at + incl);
     if (hit) {
@@ -363,7 +364,8 @@ void launch(const Append8Args& a, int units, dim3 grid, bool vec, bool il, hipSt
 hipError_t launch_append8(const Append8Args& args, int dtype, bool interleaved, hipStream_t s) {
   const RotaryArgs& a = args.r;
   // groups that new tokens of ascending starts can belong to
-  const int64_t units = std::min((int64_t)a.rows, (int64_t)a.rows / kGroupKeys + 2 * (int64_t)a.n_seq);
+  const int64_t units =
+      std::min((int64_t)a.rows, (int64_t)a.rows / kGroupKeys + 2 * (int64_t)a.n_seq);
   const int64_t groups = units * ((a.h_kv + kHeads - 1) / kHeads) * 2 + a.rows;
   if (!launchable(groups, kThreads)) return hipErrorInvalidConfiguration;
   auto whole = [](const void* p, int64_t stride) {

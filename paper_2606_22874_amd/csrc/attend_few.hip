@@ -9,6 +9,8 @@
 //   x = cap, bias, mask of S^T;  p = 2^(x - m);  l += p
 //   O^T += V^T P^T    D/16 MFMAs 16x16x16, P^T straight from the accumulators,
 //                     V^T through the transposing LDS read.
+// P is rounded to the element type (a matrix instruction has one for both operands); l is
+// summed before that, in FP32.
 // The four states meet in LDS; a tile split along its keys leaves (m, l, O) in the
 // workspace, and the part that finishes last joins them:
 //   M = max m,  L = sum l 2^(m - M),  out = sum O 2^(m - M) / L.
@@ -50,9 +52,9 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a) {
   const int G = a.h_q / a.h_kv, g = blockIdx.x % a.h_kv;
   const int cap = a.pages.cap();
   if (wave == 0) {
-    const Part p = find_part<kRows, 0, SINK ? kFit<D> : 0>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len, a.n_seq,
-                                       a.rows, G, a.h_kv, a.rule.window, SINK ? a.rule.sink : 0,
-                                       cap, a.from, a.to);
+    const Part p = find_part<kRows, 0, SINK ? kFit<D> : 0>(
+        blockIdx.x / a.h_kv, a.seq_start, a.seq_len, a.n_seq, a.rows, G, a.h_kv, a.rule.window,
+        SINK ? a.rule.sink : 0, cap, a.from, a.to);
     if (lane == 0) sm.part = p;
   }
   __syncthreads();

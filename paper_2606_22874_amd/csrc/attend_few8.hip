@@ -46,9 +46,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend8_few_kernel(AttendArgs 
   const int G = a.h_q / a.h_kv, g = blockIdx.x % a.h_kv;
   const int cap = a.pages.cap();
   if (wave == 0) {
-    const Part p = find_part<kRows, 0, kFit<D>>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len, a.n_seq,
-                                       a.rows, G, a.h_kv, a.rule.window, a.rule.sink, cap, a.from,
-                                       a.to);
+    const Part p = find_part<kRows, 0, kFit<D>>(blockIdx.x / a.h_kv, a.seq_start, a.seq_len,
+                                                a.n_seq, a.rows, G, a.h_kv, a.rule.window,
+                                                a.rule.sink, cap, a.from, a.to);
     if (lane == 0) sm.part = p;
   }
   __syncthreads();

@@ -18,7 +18,8 @@ void launch(const AttendArgs& a, dim3 grid, hipStream_t s) {
   // the plain form takes maxima before it scales: it needs a positive scale
   const bool cap = a.rule.cap > 0.f;
   const bool bias = a.rule.slopes || (!cap && !(a.rule.scale * kLog2e > 1e-6f));
-  auto f = cap ? (bias ? attend8_many_kernel<T, D, true, true> : attend8_many_kernel<T, D, true, false>)
+  auto f = cap ? (bias ? attend8_many_kernel<T, D, true, true>
+                       : attend8_many_kernel<T, D, true, false>)
                : (bias ? attend8_many_kernel<T, D, false, true>
                        : attend8_many_kernel<T, D, false, false>);
   hipLaunchKernelGGL(f, grid, dim3(64 * kWaves), 0, s, a);

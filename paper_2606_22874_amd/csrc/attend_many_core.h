@@ -597,7 +597,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
       }
       __syncthreads();
       const bool missing = __builtin_amdgcn_readfirstlane(s_missing) != 0;
-      auto pages_of = [&](int t) SPOT_INLINE -> unsigned {     // bit kt: the keys 16 kt .. are there
+      auto pages_of = [&](int t) SPOT_INLINE -> unsigned {   // bit kt: the keys 16 kt .. are there
         if (!missing) return 15u;
         unsigned m = 0;
 #pragma unroll
@@ -700,7 +700,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs& a) {
             if (t + 1 < nb)
               WidenK::load(a.k8, s_list + 4 * (t + 1), raw, wave - kWaves / 2);
             if (t >= 1 && active(t - 1)) vector_phase(t - 1);
-              if (t + 1 < nb) WidenK::store(raw, s_scale + 4 * (t + 1), knext, wave - kWaves / 2);
+            if (t + 1 < nb) WidenK::store(raw, s_scale + 4 * (t + 1), knext, wave - kWaves / 2);
           } else {
             if (t + 1 < nb) CopyK::issue(a.k, s_list + 4 * (t + 1), knext, wave - kWaves / 2);
             if (t >= 1 && active(t - 1)) vector_phase(t - 1);

@@ -704,7 +704,9 @@ const uint8_t* axis_of(Args& a, const Dev& t, int axes, int rope_dim) {
 }
 
 // Scales of an 8-bit pool.
-big pool_scales(int n_pages, int h_kv, int page_size) { return (big)n_pages * h_kv * page_size / 16; }
+big pool_scales(int n_pages, int h_kv, int page_size) {
+  return (big)n_pages * h_kv * page_size / 16;
+}
 
 // x, x_stride, pos, n_axes, axis, rows, heads, d, rope_dim, freq, amp, flags, out, out_stride,
 // stream
@@ -729,8 +731,8 @@ PyObject* rotary_axes(Args a) {
   const double* fr = freq_of(a, freq, rope);
   const uint8_t* ax = axis_of(a, axis, axes, rope);
   return finish(a, [&] {
-    return fn(kRotaryAxes, &spot_rotary_axes)(xp, xs, ip(pp), axes, ax, rows, heads, d, rope, fr, amp,
-                                              flags, el.dtype, op, os, st);
+    return fn(kRotaryAxes, &spot_rotary_axes)(xp, xs, ip(pp), axes, ax, rows, heads, d, rope, fr,
+                                              amp, flags, el.dtype, op, os, st);
   });
 }
 
@@ -761,7 +763,8 @@ PyObject* rotary_append8(Args a) {
   const big pool = (big)np * hkv * ps * d;
   void *qp = rows_of(a, q, el.bit, rows, qs, (big)hq * d),
        *kip = rows_of(a, k, el.bit, rows, ks, (big)hkv * d),
-       *vip = rows_of(a, v, el.bit, rows, vs, (big)hkv * d), *pp = pos.opt(a, I32, (big)rows * (axes > 1 ? axes : 1)),
+       *vip = rows_of(a, v, el.bit, rows, vs, (big)hkv * d),
+       *pp = pos.opt(a, I32, (big)rows * (axes > 1 ? axes : 1)),
        *tp = tab.ptr(a, I32, (big)ns * mp), *sp = start.ptr(a, I32, (big)ns + 1),
        *lp = len.ptr(a, I32, ns), *qop = qo.ptr(a, el.bit, (big)rows * hq * d),
        *kpp = kp.ptr(a, U8 | F8, pool), *vpp = vp.ptr(a, U8 | F8, pool),
@@ -771,9 +774,9 @@ PyObject* rotary_append8(Args a) {
   const uint8_t* ax = axis_of(a, axis, axes, rope);
   return finish(a, [&] {
     return fn(kRotaryAppend8, &spot_rotary_append8)(
-        qp, qs, kip, ks, vip, vs, el.dtype, ip(pp), axes, ax, ip(tp), np, ps, mp, ip(sp), ip(lp), ns, rows, hq,
-        hkv, d, rope, fr, amp, flags, qop, kpp, vpp,
-        static_cast<uint8_t*>(ksp), static_cast<uint8_t*>(vsp), st);
+        qp, qs, kip, ks, vip, vs, el.dtype, ip(pp), axes, ax, ip(tp), np, ps, mp, ip(sp), ip(lp),
+        ns, rows, hq, hkv, d, rope, fr, amp, flags, qop, kpp, vpp, static_cast<uint8_t*>(ksp),
+        static_cast<uint8_t*>(vsp), st);
   });
 }
 
@@ -921,7 +924,8 @@ PyObject* rotary_append8_of(Args a) {
   void *qp = rows_of(a, q, el.bit, rows, qs, (big)hq * d),
        *kip = rows_of(a, k, el.bit, rows, ks, (big)hkv * d),
        *vip = rows_of(a, v, el.bit, rows, vs, (big)hkv * d),
-       *pp = pos.opt(a, I32, (big)rows * (ax.n > 1 ? ax.n : 1)), *tp = tab.ptr(a, I32, (big)ns * mp),
+       *pp = pos.opt(a, I32, (big)rows * (ax.n > 1 ? ax.n : 1)),
+       *tp = tab.ptr(a, I32, (big)ns * mp),
        *sp = start.ptr(a, I32, (big)ns + 1), *lp = len.ptr(a, I32, ns),
        *qop = qo.ptr(a, el.bit, (big)rows * hq * d), *kpp = kp.ptr(a, U8 | F8, n_pool),
        *vpp = vp.ptr(a, U8 | F8, n_pool), *ksp = ksc.ptr(a, U8 | E8, pool_scales(np, hkv, ps)),
@@ -934,8 +938,9 @@ PyObject* rotary_append8_of(Args a) {
   });
 }
 
-// q, k_pages, v_pages, k_scale, v_scale, page_table, n_pages, page_size, max_pages, seq_start, seq_len, n_seq, rows,
-// h_q, h_kv, d, sm_scale, softcap, slopes, window, n_sink, prefix, first, out, lse, ws, stream
+// q, k_pages, v_pages, k_scale, v_scale, page_table, n_pages, page_size, max_pages, seq_start,
+// seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes, window, n_sink, prefix, first,
+// out, lse, ws, stream
 PyObject* paged_attend8(Args a) {
   Dev q(a), kp(a), vp(a), ksc(a), vsc(a), tab(a);
   const int np = a.integer(), ps = a.integer(), mp = a.integer();
@@ -960,8 +965,9 @@ PyObject* paged_attend8(Args a) {
   const size_t wb = a.ok ? ws.bytes() : 0;
   return finish(a, [&] {
     return fn(kAttend8, &spot_paged_attend8)(
-        qp, el.dtype, kpp, vpp, static_cast<uint8_t*>(ksp), static_cast<uint8_t*>(vsp), ip(tp), np, ps, mp, ip(sp), ip(lp), ns, rows, hq, hkv, d, scale,
-        softcap, fp(slp), window, sink, ip(prp), ip(fp_), op, static_cast<float*>(lsp), wp, wb, st);
+        qp, el.dtype, kpp, vpp, static_cast<uint8_t*>(ksp), static_cast<uint8_t*>(vsp), ip(tp), np,
+        ps, mp, ip(sp), ip(lp), ns, rows, hq, hkv, d, scale, softcap, fp(slp), window, sink,
+        ip(prp), ip(fp_), op, static_cast<float*>(lsp), wp, wb, st);
   });
 }
 

@@ -133,8 +133,9 @@ __device__ __forceinline__ float tanh_any(float y) {
   return a < 0.5f ? tanh_near(y) : far;
 }
 
-// cap tanh(y) as cap - 2 cap / (1 + e^(2 y)), within 2.5e-7 cap, of y2 = 2 y log2(e): for
-// scores beyond those of tanh_near, half the operations of tanh_any.  A score of 16 bits'
+// cap tanh(y) as cap - 2 cap / (1 + e^(2 y)), of y2 = 2 y log2(e), within 4e-7 cap (exponential
+// and reciprocal to one place, four roundings; 2.2e-7 measured, lse's included): for scores
+// beyond those of tanh_near, half the operations of tanh_any.  A score of 16 bits'
 // products is off by 1e-5 and more by itself, so caps up to kQuickCap take it (900 tokens
 // over an 8-bit cache of 7500, cap 30, scores of both kinds: 259 us with tanh_any, 212).
 // Of y2's factor, 2 log2(e) scale / cap: an infinite one would make NaN of a score of 0.
@@ -252,7 +253,9 @@ __device__ __forceinline__ int span_blocks(const Seq& q, int window, int sink, i
 // them), and a join, about a block for each part.
 // FIT > 0: so many workgroups run at once; where the parts are a few more, those that start
 // last run alone, so the blocks of a part grow to at most twice their number until all fit
-// (a mixed batch's 11 single sequences of up to 24000 tokens, 8-bit cache: 82 -> 63 us).
+// (a mixed batch's 11 single sequences of up to 24000 tokens, 8-bit cache: 82 -> 63 us).  Not
+// for a 16-bit cache without sinks, whose division of work, and so whose bits, this would
+// change; what it would gain there has not been measured.
 constexpr int kMaxJoin = 64;
 template <int TR, int ROUND, int FIT = 0>
 __device__ __forceinline__ Part find_part(int unit, const int32_t* seq_start,

@@ -117,7 +117,8 @@ __device__ __forceinline__ void rotate_row(const RotaryArgs& a, int row) {
     }
     if (krow < 0) return false;
     const int g = h < n_rot ? h - a.h_q : h - n_rot;
-    out = (h < n_rot ? a.k_pages : a.v_pages) + ((int64_t)krow + (int64_t)g * a.pages.page_size) * d;
+    out = (h < n_rot ? a.k_pages : a.v_pages) +
+          ((int64_t)krow + (int64_t)g * a.pages.page_size) * d;
     return true;
   };
   if constexpr (VEC) {

@@ -828,8 +828,8 @@ def spot_cache_evict(acc, k_pages, v_pages, page_table, n_pages, page_size, max_
             _ptr(acc_out), out_cap, s))
 
 
-def spot_rotary_axes(x, x_stride, pos, n_axes, axis, rows, heads, d, rope_dim, freq, amp, flags, out,
-                     out_stride, stream=None):
+def spot_rotary_axes(x, x_stride, pos, n_axes, axis, rows, heads, d, rope_dim, freq, amp, flags,
+                     out, out_stride, stream=None):
     if _native is not None:
         st = _native.rotary_axes(x, x_stride, pos, n_axes, axis, rows, heads, d, rope_dim, freq,
                                  amp, flags, out, out_stride, stream)
@@ -844,13 +844,13 @@ def spot_rotary_axes(x, x_stride, pos, n_axes, axis, rows, heads, d, rope_dim, f
     dev, s = _same_device(stream, x, pos, out)
     with torch.cuda.device(dev):
         _check("spot_rotary_axes", load().spot_rotary_axes(
-            _ptr(x), x_stride, _ptr(pos), n_axes, _ptr(axis), rows, heads, d, rope_dim, _ptr(freq), float(amp), flags,
-            dt, _ptr(out), out_stride, s))
+            _ptr(x), x_stride, _ptr(pos), n_axes, _ptr(axis), rows, heads, d, rope_dim, _ptr(freq),
+            float(amp), flags, dt, _ptr(out), out_stride, s))
 
 
-def spot_rotary_append8(q, q_stride, k, k_stride, v, v_stride, pos, n_axes, axis, page_table, n_pages,
-                        page_size, max_pages, seq_start, seq_len, n_seq, rows, h_q, h_kv, d,
-                        rope_dim, freq, amp, flags, q_out, k_pages, v_pages, k_scale, v_scale,
+def spot_rotary_append8(q, q_stride, k, k_stride, v, v_stride, pos, n_axes, axis, page_table,
+                        n_pages, page_size, max_pages, seq_start, seq_len, n_seq, rows, h_q, h_kv,
+                        d, rope_dim, freq, amp, flags, q_out, k_pages, v_pages, k_scale, v_scale,
                         stream=None):
     if _native is not None:
         st = _native.rotary_append8(q, q_stride, k, k_stride, v, v_stride, pos, n_axes, axis,
@@ -877,14 +877,14 @@ def spot_rotary_append8(q, q_stride, k, k_stride, v, v_stride, pos, n_axes, axis
     with torch.cuda.device(dev):
         _check("spot_rotary_append8", load().spot_rotary_append8(
             _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, dt, _ptr(pos),
-            n_axes, _ptr(axis), _ptr(page_table), n_pages, page_size, max_pages, _ptr(seq_start), _ptr(seq_len),
-            n_seq, rows, h_q, h_kv, d, rope_dim, _ptr(freq), float(amp), flags, _ptr(q_out),
-            _ptr(k_pages), _ptr(v_pages), _ptr(k_scale), _ptr(v_scale), s))
+            n_axes, _ptr(axis), _ptr(page_table), n_pages, page_size, max_pages, _ptr(seq_start),
+            _ptr(seq_len), n_seq, rows, h_q, h_kv, d, rope_dim, _ptr(freq), float(amp), flags,
+            _ptr(q_out), _ptr(k_pages), _ptr(v_pages), _ptr(k_scale), _ptr(v_scale), s))
 
 
-def spot_paged_attend_sinks(q, k_pages, v_pages, page_table, n_pages, page_size, max_pages, seq_start,
-                            seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes, window,
-                            n_sink, prefix, first, out, lse, ws, stream=None):
+def spot_paged_attend_sinks(q, k_pages, v_pages, page_table, n_pages, page_size, max_pages,
+                            seq_start, seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap,
+                            slopes, window, n_sink, prefix, first, out, lse, ws, stream=None):
     if _native is not None:
         st = _native.paged_attend_sinks(q, k_pages, v_pages, page_table, n_pages, page_size,
                                         max_pages, seq_start, seq_len, n_seq, rows, h_q, h_kv, d,
@@ -912,8 +912,8 @@ def spot_paged_attend_sinks(q, k_pages, v_pages, page_table, n_pages, page_size,
         _check("spot_paged_attend_sinks", load().spot_paged_attend_sinks(
             _ptr(q), dt, _ptr(k_pages), _ptr(v_pages), _ptr(page_table), n_pages, page_size,
             max_pages, _ptr(seq_start), _ptr(seq_len), n_seq, rows, h_q, h_kv, d, float(sm_scale),
-            float(softcap), _ptr(slopes), window, n_sink, _ptr(prefix), _ptr(first), _ptr(out), _ptr(lse),
-            _ptr(ws), ws.numel() * ws.element_size(), s))
+            float(softcap), _ptr(slopes), window, n_sink, _ptr(prefix), _ptr(first), _ptr(out),
+            _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), s))
 
 
 def spot_paged_attend8(q, k_pages, v_pages, k_scale, v_scale, page_table, n_pages, page_size,
@@ -939,14 +939,15 @@ def spot_paged_attend8(q, k_pages, v_pages, k_scale, v_scale, page_table, n_page
     _dev(out, "out", el, rows * h_q * d)
     _opt(lse, "lse", F32, rows * h_q)
     _dev(ws, "ws", None)
-    dev, s = _same_device(stream, q, k_pages, v_pages, k_scale, v_scale, page_table, seq_start, seq_len, slopes,
-                          prefix, first, out, lse, ws)
+    dev, s = _same_device(stream, q, k_pages, v_pages, k_scale, v_scale, page_table, seq_start,
+                          seq_len, slopes, prefix, first, out, lse, ws)
     with torch.cuda.device(dev):
         _check("spot_paged_attend8", load().spot_paged_attend8(
             _ptr(q), dt, _ptr(k_pages), _ptr(v_pages), _ptr(k_scale), _ptr(v_scale),
-            _ptr(page_table), n_pages, page_size, max_pages, _ptr(seq_start), _ptr(seq_len), n_seq, rows, h_q, h_kv, d, float(sm_scale),
-            float(softcap), _ptr(slopes), window, n_sink, _ptr(prefix), _ptr(first), _ptr(out), _ptr(lse),
-            _ptr(ws), ws.numel() * ws.element_size(), s))
+            _ptr(page_table), n_pages, page_size, max_pages, _ptr(seq_start), _ptr(seq_len), n_seq,
+            rows, h_q, h_kv, d, float(sm_scale), float(softcap), _ptr(slopes), window, n_sink,
+            _ptr(prefix), _ptr(first), _ptr(out), _ptr(lse), _ptr(ws),
+            ws.numel() * ws.element_size(), s))
 
 
 def spot_probe_stream_read(buf, sink, stream=None):
@@ -1312,9 +1313,9 @@ def paged_attend(q, k_pages, v_pages, page_table, seq_start, seq_len, sm_scale=N
     if out is None or lse is None or ws is None:
         out, lse, ws = _attend_outputs(q, out, lse, ws, n_seq, h_kv, stream)
     if n_sink:
-        spot_paged_attend_sinks(q, k_pages, v_pages, page_table, n_pages, page, max_pages, seq_start,
-                                seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes,
-                                window, n_sink, prefix, first, out, lse, ws, stream)
+        spot_paged_attend_sinks(q, k_pages, v_pages, page_table, n_pages, page, max_pages,
+                                seq_start, seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap,
+                                slopes, window, n_sink, prefix, first, out, lse, ws, stream)
         return out, lse
     spot_paged_attend(q, k_pages, v_pages, page_table, n_pages, page, max_pages, seq_start,
                       seq_len, n_seq, rows, h_q, h_kv, d, sm_scale, softcap, slopes, window,
@@ -1346,7 +1347,8 @@ def paged_weights(q, lse, k_pages, page_table, seq_start, seq_len, sm_scale=None
                   slopes=None, window=0, prefix=None, first=None, acc=None, decay=1.0, out=None,
                   stream=None):
     """Attention weight each cached token received from q, summed per KV head, on top of
-    decay * acc: [n_seq, h_kv, max_pages * page_size] float32.  lse from paged_attend."""
+    decay * acc: [n_seq, h_kv, max_pages * page_size] float32.  lse from paged_attend (without
+    sinks: what those received is left out)."""
     rows, h_q, d = q.shape
     n_pages, h_kv, page, _ = k_pages.shape
     n_seq, max_pages = page_table.shape

@@ -26,12 +26,12 @@ def bounds(c, k, v, cap, **rule):
     out, lse = (torch.full(s, math.nan, dtype=torch.float64, device=DEV)
                 for s in ((rows, h_q, d), (rows, h_q)))
     tol, ltol = torch.zeros_like(out), torch.zeros_like(lse)
-    for s, h, r, x, seen, dx in ref8.each_row_block(c.q, k, c.table, c.starts, c.len, d ** -0.5, cap,
-                                                    None, prefix=None, **rule):
+    for s, h, r, x, seen, dx in ref8.each_row_block(c.q, k, c.table, c.starts, c.len, d ** -0.5,
+                                                    cap, None, prefix=None, **rule):
         vv, _ = ref.tokens(v, c.table[s], h // G, x.shape[1])
         vv = torch.where(seen.any(0)[:, None], vv, 0.0)
-        # a quick cap is off by 2.5e-7 of the cap
-        dx = torch.where(seen, dx + 2.5e-7 * cap, 0.0)
+        # a quick cap is off by 4e-7 of the cap
+        dx = torch.where(seen, dx + 4e-7 * cap, 0.0)
         l = torch.logsumexp(x, 1)
         p = torch.exp(x - l[:, None])
         n = seen.sum(1, keepdim=True)
@@ -47,8 +47,10 @@ def bounds(c, k, v, cap, **rule):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("n,length,heads", [([1], [40000], (8, 1)), ([1, 1, 1], [9000, 700, 20001], (4, 2)),
-                                            ([64, 1], [12345, 2000], (8, 2)), ([300], [5000], (4, 1))])
+@pytest.mark.parametrize("n,length,heads", [([1], [40000], (8, 1)),
+                                            ([1, 1, 1], [9000, 700, 20001], (4, 2)),
+                                            ([64, 1], [12345, 2000], (8, 2)),
+                                            ([300], [5000], (4, 1))])
 @pytest.mark.parametrize("d,dtype", [(64, FP), (128, BF)])
 def test_sinks_of_long_caches(n, length, heads, d, dtype, kind):
     """Tiles split along their keys, the sinks in their first parts."""

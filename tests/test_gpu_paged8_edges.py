@@ -148,7 +148,8 @@ def test_unseen_keys_beside_scores_at_the_bend(n, length, rule, kind):
     c.q[:, :, 0] = 1.0
     seen = ~torch.isnan(c.k)
     c.k = torch.where(seen, 0.0, c.k)
-    c.k[..., 0] = torch.where(seen[..., 0], torch.where(c.v[..., 1] > 0, 16.0, -16.0).to(BF), math.nan)
+    half = torch.where(c.v[..., 1] > 0, 16.0, -16.0).to(BF)
+    c.k[..., 0] = torch.where(seen[..., 0], half, math.nan)
     got = []
     for fill in (0.0, 256.0):
         k, v = torch.where(seen, c.k, fill), torch.where(seen, c.v, fill)
@@ -180,7 +181,8 @@ def test_append_refuses_positions_with_axes_without_an_axis(native, monkeypatch)
     pools = [torch.zeros((4, 2, 16, 64), dtype=torch.uint8, device=DEV) for _ in range(2)]
     pools += [torch.zeros((4, 2, 1), dtype=torch.uint8, device=DEV) for _ in range(2)]
     place = [torch.tensor(a, dtype=torch.int32, device=DEV) for a in ([[1, 2]], [0, 3], [3])]
-    freq, out = torch.full((32,), 0.3, dtype=torch.float64), torch.zeros((3, 4, 64), dtype=BF, device=DEV)
+    freq = torch.full((32,), 0.3, dtype=torch.float64)
+    out = torch.zeros((3, 4, 64), dtype=BF, device=DEV)
     pos = torch.arange(9, dtype=torch.int32, device=DEV).view(3, 3)
     with pytest.raises(ValueError, match="needs the axis"):
         spot.rotary_append8(q, k, v, *pools, *place, freq, pos=pos, q_out=out)
@@ -217,8 +219,8 @@ def test_scores_of_any_size(n, length, dtype, size, kind):
                 # rounded number (half a step each), and the output's rounding
                 A, _, _, _ = ref8.attend(c.q, kd.k, kd.v.abs(), c.table, c.starts, c.len, 0.3,
                                          cap=rule.get("softcap", 0.0), **more)
-                seen_n = max(length)
-                assert torch.all((out.double() - o).abs() <= 2 * u * A + 4 * seen_n * 2.0 ** -24 * A)
+                sums = 4 * max(length) * 2.0 ** -24
+                assert torch.all((out.double() - o).abs() <= (2 * u + sums) * A)
                 # scores of 1e8 and more: a handful of roundings of one such number
                 assert torch.all((lse.double() - l).abs() <= 16 * 2.0 ** -24 * l.abs())
         # one token of the largest score, far above

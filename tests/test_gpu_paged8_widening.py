@@ -23,7 +23,8 @@ def pools(codes, scales):
 
 def attend(q, k, v, dtype, **rule):
     place = [torch.tensor(a, dtype=torch.int32, device=DEV) for a in ([[0]], [0, TOKENS], [TOKENS])]
-    return spot.paged_attend8(q.to(dtype).to(DEV), k[0], v[0], k[1], v[1], *place, sm_scale=1.0, **rule)
+    return spot.paged_attend8(q.to(dtype).to(DEV), k[0], v[0], k[1], v[1], *place, sm_scale=1.0,
+                              **rule)
 
 
 def rows(x, G):
@@ -102,10 +103,10 @@ def test_keys(rule, dtype, d, G):
         # (all scales of BF16 but the last few, and those that FP16 has numbers for)
         assert there.float().mean() > (0.8 if dtype == BF else 0.4)
         # The product is exact; scale, logarithm and base change: 8 roundings of the score.  Beside
-        # it, of log2 l: l is 2^10 in FP16, whose reference lies 10 below the score (that difference
-        # rounded to 2^-24 of up to 16, the exponential to two places, 3 2^-24 of log2 l, and log2 l,
-        # 10, to two places: 16 + 3 + 20, times log 2: 27 2^-24), and 64 times as much in whole blocks
-        # (log2 l 6 more, 12 2^-24, and 6 additions), 45 with what one place more in each would add.
+        # it those of log2 l.  l is 2^10 in FP16, whose reference lies 10 below the score (the
+        # difference rounded to 2^-24 of up to 16, the exponential to two places, 3 2^-24 of
+        # log2 l, and log2 l, 10, to two places: 16 + 3 + 20, times log 2: 27 2^-24), and 64 times
+        # as much in whole blocks (log2 l 6 more: 12, 4 for the sums, times log 2 and rounded up).
         u = 2.0 ** -24
         beside = 28 * u * (dtype == FP) + 17 * u * (rule == "whole")
         err = (lse.double() - want).abs()

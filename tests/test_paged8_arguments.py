@@ -27,20 +27,22 @@ def test_positions_that_a_call_reads(name, n_axes, monkeypatch):
     monkeypatch.setattr(spot, "_row_tensor", lambda *a: None)
     monkeypatch.setattr(spot, "_same_device", done)
     x = torch.zeros(5, 4, 64).bfloat16()
-    pos, axis, freq = torch.zeros(1, dtype=torch.int32), torch.zeros(8).byte(), torch.zeros(8).double()
+    pos, axis = torch.zeros(1, dtype=torch.int32), torch.zeros(8).byte()
+    freq = torch.zeros(8).double()
     with pytest.raises(Done):
         if name == "spot_rotary_axes":
             spot.spot_rotary_axes(x, 256, pos, n_axes, axis, 5, 4, 64, 16, freq, 1.0, 0, x, 256)
         else:
             i = torch.zeros(9, dtype=torch.int32)
-            spot.spot_rotary_append8(x, 256, x, 256, x, 256, pos, n_axes, axis, i, 1, 16, 1, i, i, 1, 5,
-                                     4, 4, 64, 16, freq, 1.0, 0, x, x, x, x, x)
+            spot.spot_rotary_append8(x, 256, x, 256, x, 256, pos, n_axes, axis, i, 1, 16, 1, i, i,
+                                     1, 5, 4, 4, 64, 16, freq, 1.0, 0, x, x, x, x, x)
     assert need["pos"] == 5 * max(n_axes, 1)
 
 
 def positional():
     """{wrapper: its call with pos, the C ABI calls replaced}"""
-    rows, kv, pool, codes = t(3, 4, 64), t(3, 2, 64), t(9, 2, 16, 64), t(9, 2, 16, 64, dtype=torch.uint8)
+    rows, kv, pool = t(3, 4, 64), t(3, 2, 64), t(9, 2, 16, 64)
+    codes = t(9, 2, 16, 64, dtype=torch.uint8)
     scale, table, freq = t(9, 2, 1, dtype=torch.uint8), i32(2, 4), torch.zeros(32).double()
     return {"rotary": lambda pos, **kw: spot.rotary(rows, pos, freq, out=rows, **kw),
             "rotary_append": lambda pos, **kw: spot.rotary_append(

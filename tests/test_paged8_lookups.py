@@ -45,7 +45,8 @@ int main() {
             if (t >= p.cap()) ++past;
             if (at >= 0) ++found;
             if ((at >= 0) != (t < p.cap())) ++wrong;
-            if (at >= 0 && at != (5 * h_kv + 1) * page + t / kGroupKeys * kGroupKeys % page) ++wrong;
+            const int group = t / kGroupKeys * kGroupKeys;
+            if (at >= 0 && at != (5 * h_kv + 1) * page + group % page) ++wrong;
           }
         }
   std::printf("%ld %d %d\n", wrong, past > 1000, found > 1000);
