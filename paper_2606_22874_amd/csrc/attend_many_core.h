@@ -27,9 +27,9 @@
 // (4 waves, two workgroups a CU) read the keys twice as often: 14 % slower; a third pair
 // of buffers, or touching the next blocks ahead for L2, 3 .. 5 %.
 // With sinks a tile goes through two runs of blocks, numbered through (paged_map.h): a prompt
-// of 12000 tokens, 32 heads of 128 over 8, window 2048 and 16 sinks, 464 us (431 without the
-// sinks).  Over an 8-bit cache the tiles are widened on their way (Widen): a prompt of 14000,
-// 64 heads over 8, 3.13 ms, 1.03 PFLOP/s; 512 tokens over 49152, 790 us.
+// of 12000 tokens, 32 heads of 128 over 8, window 2048 and 16 sinks, 464 .. 475 us (442
+// without the sinks).  Over an 8-bit cache the tiles are widened on their way (Widen): a prompt
+// of 14000, 64 heads over 8, 3.16 ms, 1.01 PFLOP/s; 512 tokens over 49152, 784 .. 797 us.
 // K and V go from memory to LDS 16 bytes a lane (1 KiB a wave instruction), rows
 // swizzled by 16-byte chunks against bank conflicts; each of the buffers is a
 // variable of its own and the loop is unrolled by two, so that the compiler can tell

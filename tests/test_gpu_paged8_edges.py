@@ -241,11 +241,11 @@ def test_scores_of_any_size(n, length, dtype, size, kind):
 
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("n,length", [([3], [700]), ([150], [500]), ([90, 2], [300, 800])])
-def test_large_scores_that_grow_by_little(n, length, dtype, kind):
+def test_large_scores_that_grow_by_little(n, length, d, dtype, kind):
     """Scores of every octave from 2^20 to 2^31 that differ in their last places and grow along
     the keys: probabilities stay numbers, and the rows within their values."""
-    d = 64
     c = Cache(29, n, length, 4, 2, d, 16, dtype)
     c.q.zero_()
     c.q[:, :, 0], c.q[:, :, 1] = 4096.0, 1.0
